@@ -1,4 +1,4 @@
-"""ctypes declarations of the C ABI in include/dasc.h.
+"""ctypes declarations of the C ABI in include/dasc.h and include/dasc/ops.h.
 
 Loading fails loudly: if libdasc.so has not been built, importing this module
 raises ImportError.  There is no fallback implementation.
@@ -32,12 +32,23 @@ DASC_REFRESH_KERNEL_AUTO = 0
 DASC_REFRESH_KERNEL_COLUMN = 1
 DASC_REFRESH_KERNEL_CHANNEL_WY = 2
 
+DASC_DTYPE_BF16 = 0
+DASC_DTYPE_F16 = 1
+DASC_DTYPE_F32 = 2
+DASC_ACT_NONE = 0
+DASC_ACT_SIGMOID = 1
+DASC_ACT_SILU = 2
+
 EXPORTED = (
     "dasc_static_log_decay", "dasc_plan", "dasc_matched_slots", "dasc_strerror",
     "dasc_pack", "dasc_restore", "dasc_pack_q8", "dasc_restore_q8",
     "dasc_refresh_workspace_bytes", "dasc_refresh", "dasc_restore_refresh",
     "dasc_tp_permutation", "dasc_pack_padded", "dasc_restore_padded", "dasc_refresh_select",
     "dasc_refresh_noalloc",
+)
+EXPORTED_OPS = (
+    "dasc_linear_attn_workspace_bytes", "dasc_linear_attn", "dasc_verify_drafts_workspace_bytes",
+    "dasc_verify_drafts", "dasc_block_norm",
 )
 
 
@@ -66,6 +77,21 @@ class PlanOut(C.Structure):
         ("r_max_rows", C.c_int64),
         ("c_ckpt", C.c_double), ("slot_bytes_rank", C.c_int64), ("dense_slot_bytes_rank", C.c_int64),
     ]
+
+
+class LinearIo(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v", "g", "beta", "o")] + [
+        (n, C.c_int64) for n in ("q_tok", "q_head", "k_tok", "k_head", "v_tok", "v_head", "g_tok",
+                                 "g_head", "beta_tok", "beta_head", "o_tok", "o_head")]
+
+
+class NormIo(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("y", "gate", "x", "x_out", "h_out", "w_post", "w_pre",
+                                          "channel_scale")] + [
+        (n, C.c_int64) for n in ("y_out", "y_in", "gate_out", "gate_in", "x_row_out", "x_row_in",
+                                 "xo_out", "xo_in", "h_row_out", "h_row_in", "outer")] + [
+        (n, C.c_int32) for n in ("inner", "dim", "dtype", "res_dtype", "w_dtype", "act")] + [
+        ("scale", C.c_float), ("eps", C.c_float)]
 
 
 def _hip_runtimes() -> set:
@@ -111,6 +137,15 @@ def _load() -> C.CDLL:
                                 I32, P],
         "dasc_restore_refresh": [C.POINTER(Shape), I32, P, I64, P, I32, I64, I64, P, P, I64, P,
                                  P, P, P, P, I32, I32, I32, P, SZ, P],
+        # the io structs go as packed bytes (struct.pack), read during the call only
+        "dasc_linear_attn_workspace_bytes": [C.POINTER(Shape), I32, I64, I32, I32,
+                                             C.POINTER(C.c_size_t)],
+        "dasc_linear_attn": [C.POINTER(Shape), I32, P, I64, P, P, P, P, P, I32, I64, I32, C.c_float,
+                             P, SZ, P],
+        "dasc_verify_drafts_workspace_bytes": [I32, I64, C.POINTER(C.c_size_t)],
+        "dasc_verify_drafts": [I32, I32, I64, I32, P, I64, I64, P, I64, I64, P, P, P, P, P, P, P, SZ,
+                               P],
+        "dasc_block_norm": [P, P],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)

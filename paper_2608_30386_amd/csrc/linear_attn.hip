@@ -1,0 +1,245 @@
+// Linear attention with a decay for each head: the entry point and the token-by-token form.
+//
+//     S~ = e^{g} S;   u = v (plain) or beta (v - S~^T k) (delta);   S' = S~ + k u^T;   o = scale S'^T q
+//
+// The columns of a head's state evolve on their own, so a wave takes all dk rows of 32 columns
+// and needs nothing from another wave: lane (rg, cg) holds rows rg dk/8 .. of the four columns
+// 4 cg.. .  The two sums over the rows that a token needs, S~^T k and S~^T q, are formed before
+// the update and summed over the row groups together; o = S~^T q + (q . k) u.  Everything is
+// fp32.
+
+#include "linear_attn.h"
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "launch_common.h"
+#include "wy_ops.h"
+
+namespace dasc {
+namespace {
+
+using dasc_wy::f32x4;
+
+// R consecutive bf16 (R = 2, 4, 8 or 16), widened
+template <int R>
+__device__ inline void load_bf16(const uint16_t* p, float* x) {
+  uint32_t w[R / 2];
+  if constexpr (R == 2) {
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else if constexpr (R == 4) {
+    *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(p);
+  } else {
+#pragma unroll
+    for (int i = 0; i < R / 8; ++i)
+      reinterpret_cast<uint4*>(w)[i] = reinterpret_cast<const uint4*>(p)[i];
+  }
+#pragma unroll
+  for (int i = 0; i < R / 2; ++i) {
+    x[2 * i] = bf16_lo(w[i]);
+    x[2 * i + 1] = bf16_hi(w[i]);
+  }
+}
+
+__device__ inline uint32_t pack_bf16(float x0, float x1) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(dasc_wy::f32x2{x0, x1}, dasc_wy::bf16x2));
+}
+
+constexpr int kCols = 32;             // columns of a wave
+constexpr int kCG = kCols / 4;        // column groups: lanes side by side on one row
+constexpr int kRG = 64 / kCG;         // row groups
+
+// sum over the row groups; every lane gets it
+__device__ inline float rows_sum(float x) {
+#pragma unroll
+  for (int m = kCG; m < 64; m *= 2) x += __shfl_xor(x, m);
+  return x;
+}
+
+// S e^g.  A decay near one is applied as S + S (e^g - 1): rounded to fp32 itself it would be off
+// by up to 2^-25, the same way for the whole state, token after token.
+template <int R>
+__device__ inline void decay(f32x4 (&S)[R], float g) {
+  if (g > -0.5f) {
+    const float m = expm1f(g);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) S[r][e] = fmaf(S[r][e], m, S[r][e]);
+  } else {
+    const float m = expf(g);
+#pragma unroll
+    for (int r = 0; r < R; ++r) S[r] *= m;
+  }
+}
+
+template <int DK, bool DELTA, bool OUT>
+__global__ __launch_bounds__(256) void linear_steps_kernel(LinearArgs a, int64_t wave0, int64_t waves,
+                                                           int col_blocks) {
+  constexpr int R = DK / kRG;
+  const int64_t w = wave0 + int64_t(blockIdx.x) * 4 + threadIdx.x / 64;
+  if (w >= waves) return;
+  const int lane = threadIdx.x % 64, cg = lane % kCG, rg = lane / kCG;
+  const int cb = int(w % col_blocks);
+  const int64_t rh = w / col_blocks;
+  const int h = int(rh % a.H), i = int(rh / a.H);
+  const int col = cb * kCols + 4 * cg;
+  const bool in = col < a.dv;
+  const int hk = h / a.rep;
+
+  const Span sp = request_span(a, i);
+  const float* from = slot_state(a, a.src, i, h, DK);
+  float* to = slot_state(a, a.dst, i, h, DK);
+  const int64_t at = int64_t(rg) * R * a.dv + col;
+
+  f32x4 S[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    S[r] = from && in ? *reinterpret_cast<const f32x4*>(from + at + int64_t(r) * a.dv) : f32x4{0, 0, 0, 0};
+
+  for (int t = 0; t < sp.len; ++t) {
+    const int64_t row = sp.begin + t;
+    decay(S, a.io.g[row * a.io.g_tok + h * a.io.g_head]);
+    float k[R], q[R];
+    load_bf16<R>(a.io.k + row * a.io.k_tok + hk * a.io.k_head + rg * R, k);
+    if (OUT) load_bf16<R>(a.io.q + row * a.io.q_tok + hk * a.io.q_head + rg * R, q);
+    f32x4 v = {0, 0, 0, 0};
+    if (in) {
+      const uint2 b = *reinterpret_cast<const uint2*>(a.io.v + row * a.io.v_tok + h * a.io.v_head + col);
+      v = f32x4{bf16_lo(b.x), bf16_hi(b.x), bf16_lo(b.y), bf16_hi(b.y)};
+    }
+    f32x4 sk = {0, 0, 0, 0}, sq = {0, 0, 0, 0};
+    float qk = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (DELTA) sk += S[r] * k[r];
+      if (OUT) {
+        sq += S[r] * q[r];
+        qk = fmaf(q[r], k[r], qk);
+      }
+    }
+    f32x4 u = v;
+    if (DELTA) {
+      const float b = a.io.beta[row * a.io.beta_tok + h * a.io.beta_head];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) u[e] = b * (v[e] - rows_sum(sk[e]));
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) S[r] += u * k[r];
+    if (OUT) {
+      const float d = rows_sum(qk);
+      f32x4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = a.scale * (rows_sum(sq[e]) + d * u[e]);
+      if (in && rg == 0)
+        *reinterpret_cast<uint2*>(a.io.o + row * a.io.o_tok + h * a.io.o_head + col) =
+            uint2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+    }
+  }
+  if (to && in && !(from == to && sp.len == 0)) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) *reinterpret_cast<f32x4*>(to + at + int64_t(r) * a.dv) = S[r];
+  }
+}
+
+// waves of one launch: a grid counts threads in 32 bits
+constexpr int64_t kWavesPerLaunch = int64_t(1) << 24;
+
+template <int DK>
+void launch_steps(const LinearArgs& a, hipStream_t st) {
+  const int cb = (a.dv + kCols - 1) / kCols;
+  const int64_t waves = int64_t(a.n_req) * a.H * cb;
+  for (int64_t w0 = 0; w0 < waves; w0 += kWavesPerLaunch) {
+    const int64_t n = waves - w0 < kWavesPerLaunch ? waves - w0 : kWavesPerLaunch;
+    const dim3 grid(uint32_t((n + 3) / 4));
+    const bool delta = a.io.beta, out = a.io.o;
+    auto* f = delta ? (out ? linear_steps_kernel<DK, true, true> : linear_steps_kernel<DK, true, false>)
+                    : (out ? linear_steps_kernel<DK, false, true> : linear_steps_kernel<DK, false, false>);
+    f<<<grid, 256, 0, st>>>(a, w0, w0 + n, cb);
+  }
+}
+
+bool bad_stride(int64_t s, int64_t multiple) { return s < 0 || s % multiple != 0; }
+
+}  // namespace
+
+void launch_linear_steps(const LinearArgs& a, int dk, hipStream_t st) {
+  switch (dk) {
+    case 16: launch_steps<16>(a, st); break;
+    case 32: launch_steps<32>(a, st); break;
+    case 64: launch_steps<64>(a, st); break;
+    default: launch_steps<128>(a, st); break;
+  }
+}
+
+}  // namespace dasc
+
+extern "C" int dasc_linear_attn_workspace_bytes(const dasc_shape* shape, int32_t n_req,
+                                                int64_t n_tokens, int32_t max_len, int32_t delta,
+                                                size_t* bytes) {
+  if (!shape || !bytes || n_req < 1 || n_tokens < 0 || max_len < 0) return DASC_E_INVAL;
+  if (!dasc::valid_shape(shape)) return DASC_E_SHAPE;
+  (void)delta;
+  *bytes = 0;
+  return DASC_OK;
+}
+
+extern "C" int dasc_linear_attn(const dasc_shape* shape, int32_t layer, float* states,
+                                int64_t n_pool, const int32_t* src_slot, const int32_t* dst_slot,
+                                const dasc_linear_io* io, const int32_t* cu_seqlens,
+                                const int32_t* lens, int32_t n_req, int64_t n_tokens,
+                                int32_t max_len, float scale, void* workspace,
+                                size_t workspace_bytes, dasc_stream_t stream) {
+  if (!shape || !io) return DASC_E_INVAL;
+  if (!dasc::valid_shape(shape) || shape->dv % 4 != 0) return DASC_E_SHAPE;
+  if (layer < 0 || layer >= shape->n_layers || n_req < 1 || n_tokens < 0 || n_tokens > INT32_MAX ||
+      max_len < 0 || n_pool < 1 || !std::isfinite(scale))
+    return DASC_E_INVAL;
+  if (!states || !cu_seqlens) return DASC_E_INVAL;
+  if (n_tokens > 0 && (!io->k || !io->v || !io->g)) return DASC_E_INVAL;
+  if (!io->o && !dst_slot) return DASC_E_INVAL;
+  if (io->o && !io->q) return DASC_E_INVAL;
+  using dasc::aligned16;
+  if (!aligned16(states) || (io->o && !aligned16(io->q)) || !aligned16(io->k) || !aligned16(io->v) ||
+      !aligned16(io->o) || (reinterpret_cast<uintptr_t>(io->g) & 3) ||
+      (reinterpret_cast<uintptr_t>(io->beta) & 3))
+    return DASC_E_INVAL;
+  using dasc::bad_stride;
+  if (bad_stride(io->k_tok, 8) || bad_stride(io->k_head, 8) || bad_stride(io->v_tok, 4) ||
+      bad_stride(io->v_head, 4) || bad_stride(io->g_tok, 1) || bad_stride(io->g_head, 1))
+    return DASC_E_INVAL;
+  if (io->o && (bad_stride(io->q_tok, 8) || bad_stride(io->q_head, 8) || bad_stride(io->o_tok, 4) ||
+                bad_stride(io->o_head, 4)))
+    return DASC_E_INVAL;
+  if (io->beta && (bad_stride(io->beta_tok, 1) || bad_stride(io->beta_head, 1))) return DASC_E_INVAL;
+  const int dk = shape->dk, dv = shape->dv;
+  if (shape->arch != DASC_ARCH_GDN || dv > 256 || (dk != 16 && dk != 32 && dk != 64 && dk != 128))
+    return DASC_E_UNSUPPORTED;
+  size_t need = 0;
+  const int rc = dasc_linear_attn_workspace_bytes(shape, n_req, n_tokens, max_len, io->beta != nullptr, &need);
+  if (rc != DASC_OK) return rc;
+  if (workspace_bytes < need || (need > 0 && !workspace)) return DASC_E_WORKSPACE;
+  if (need > 0 && !aligned16(workspace)) return DASC_E_INVAL;
+
+  dasc::LinearArgs a;
+  a.io = *io;
+  a.states = states;
+  a.slot_stride = dasc::rows_per_state(shape) * dv;
+  a.layer_off = int64_t(layer) * shape->n_heads * dk * dv;
+  a.n_pool = n_pool;
+  a.src = src_slot;
+  a.dst = dst_slot;
+  a.cu = cu_seqlens;
+  a.lens = lens;
+  a.n_tokens = n_tokens;
+  a.n_req = n_req;
+  a.H = shape->n_heads;
+  a.rep = shape->n_heads / shape->n_qk_heads;
+  a.dv = dv;
+  a.scale = scale;
+  (void)hipGetLastError();
+  dasc::launch_linear_steps(a, dk, reinterpret_cast<hipStream_t>(stream));
+  return dasc::launch_status();
+}
