@@ -22,7 +22,8 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libdasc.so")
 
 HIP_SOURCES = ["pack_restore.hip", "quant.hip", "refresh.hip", "refresh_wy.hip", "refresh_wy_gdn.hip",
-               "refresh_noalloc.hip", "linear_attn.hip", "verify.hip", "block_norm.hip"]
+               "refresh_noalloc.hip", "linear_attn.hip", "linear_chunk.hip",
+               "verify.hip", "block_norm.hip"]
 HOST_SOURCES = ["plan.cpp"]
 ARCH = "gfx950"
 

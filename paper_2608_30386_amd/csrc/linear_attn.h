@@ -48,6 +48,16 @@ __device__ inline float* slot_state(const LinearArgs& a, const int32_t* slots, i
 __device__ inline float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ inline float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+// What the host knows of a call, for the choice of its form and the size of its workspace
+struct ChunkPlan {
+  int32_t dk, dv, H, n_req, max_len;
+  int64_t n_tokens;
+  bool delta;
+};
+
+bool linear_chunk_supported(const ChunkPlan& c);
+int64_t linear_chunk_workspace(const ChunkPlan& c);
+void launch_linear_chunks(const ChunkPlan& c, const LinearArgs& a, void* ws, hipStream_t st);
 void launch_linear_steps(const LinearArgs& a, int dk, hipStream_t st);
 
 }  // namespace dasc

@@ -161,6 +161,11 @@ void launch_steps(const LinearArgs& a, hipStream_t st) {
   }
 }
 
+// Calls whose longest request has more tokens than this take the chunked form.
+constexpr int kStepTokens = 16;
+
+bool takes_chunks(const ChunkPlan& c) { return c.max_len > kStepTokens && linear_chunk_supported(c); }
+
 bool bad_stride(int64_t s, int64_t multiple) { return s < 0 || s % multiple != 0; }
 
 }  // namespace
@@ -181,8 +186,8 @@ extern "C" int dasc_linear_attn_workspace_bytes(const dasc_shape* shape, int32_t
                                                 size_t* bytes) {
   if (!shape || !bytes || n_req < 1 || n_tokens < 0 || max_len < 0) return DASC_E_INVAL;
   if (!dasc::valid_shape(shape)) return DASC_E_SHAPE;
-  (void)delta;
-  *bytes = 0;
+  const dasc::ChunkPlan c{shape->dk, shape->dv, shape->n_heads, n_req, max_len, n_tokens, delta != 0};
+  *bytes = dasc::takes_chunks(c) ? size_t(dasc::linear_chunk_workspace(c)) : 0;
   return DASC_OK;
 }
 
@@ -240,6 +245,12 @@ extern "C" int dasc_linear_attn(const dasc_shape* shape, int32_t layer, float* s
   a.dv = dv;
   a.scale = scale;
   (void)hipGetLastError();
-  dasc::launch_linear_steps(a, dk, reinterpret_cast<hipStream_t>(stream));
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  // the chunked form loads 16 bytes of a value row at a time and multiplies strides in 32 bits
+  const bool wide = io->v_tok % 8 == 0 && io->v_head % 8 == 0 && io->q_tok <= INT32_MAX &&
+                    io->k_tok <= INT32_MAX && io->v_tok <= INT32_MAX && io->o_tok <= INT32_MAX;
+  const dasc::ChunkPlan plan{dk, dv, shape->n_heads, n_req, max_len, n_tokens, io->beta != nullptr};
+  if (wide && dasc::takes_chunks(plan)) dasc::launch_linear_chunks(plan, a, workspace, st);
+  else dasc::launch_linear_steps(a, dk, st);
   return dasc::launch_status();
 }
