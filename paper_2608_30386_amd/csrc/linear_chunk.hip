@@ -49,8 +49,12 @@ constexpr int kC = 64;                       // tokens of a chunk
 
 struct ChunkArgs {
   LinearArgs a;
-  int32_t q_tok, k_tok, v_tok, o_tok;        // token strides, below 2^31
-  char* packets;                             // delta: what the factor kernel leaves for each chunk and head
+  int32_t q_tok, k_tok, v_tok, o_tok;        // token strides, below 2^24
+  // delta: the call goes in windows of units (numbered chunks), whose packets share a workspace
+  char* packets;                             // what the factor kernel leaves for each chunk and head of a window
+  int64_t u0, u1;                            // this window
+  const float* carry_in;                     // [H, dk, dv]: of the request that began in the window before
+  float* carry_out;                          // and of the one that goes on in the next
   float* seg_state;                          // plain: [segments, H, dk, dv]
   double* seg_log2;                          // plain: [segments, H], the decay over a segment
   int32_t seg_chunks;                        // plain: chunks of a segment
@@ -77,39 +81,58 @@ __device__ inline int unit_request(const LinearArgs& a, int64_t u, int len) {
   return lo;
 }
 
+// What is the same in every lane of a wave, said so: it then lives in scalar registers
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline int64_t uniform(int64_t x) {
+  return int64_t(uint64_t(uint32_t(uniform(int(uint64_t(x) >> 32)))) << 32 | uint32_t(uniform(int(x))));
+}
+
 // ---- operands ------------------------------------------------------------------------------------
 
 __device__ inline int sigma(int t, int m) { return 32 * (t / 2) + 8 * (m / 4) + 4 * (t % 2) + m % 4; }
 
-// Where the 16-byte unit u of a row lies among the row's U units in LDS.  A row of A operands is read
-// by eight lanes at a time (tokens 0 .. 3 and 8 .. 11 of one unit), the transposing read takes four
-// tokens of four units: neither meets a bank twice.
+// Rows in LDS lie 20 (or 12) 16-byte units apart, those of every other group of eight one unit on: the
+// transposing read's four rows of four units meet no bank twice, nor do the eight rows (0 .. 3 and 8 .. 11
+// of one unit) in which a row of A operands is read.  Every address is a lane's base and a constant.
 template <int U>
-__device__ inline int swizzle(int row, int u) {
-  if constexpr (U == 16) return u ^ (((row & 3) << 2) | ((row >> 2) & 3));
-  else if constexpr (U == 8) return u ^ ((((row >> 1) & 1) << 2) | (((row >> 3) & 1) << 1) | ((row >> 2) & 1));
-  else return u;
-}
+constexpr int kStride = U + 4;
+template <int U>
+constexpr int kRowsBytes = (kC * kStride<U> + 1) * 16;   // 64 rows
+// values, of which a wave reads two units of four rows at a time
+template <int U>
+constexpr int kVStride = U + 2;
+
+template <int U>
+__device__ inline int row_at(int row) { return (row * kStride<U> + (row >> 3 & 1)) * 16; }
 
 template <int U>
 __device__ inline bf16x8 row_unit(const char* base, int row, int u) {
-  return *reinterpret_cast<const bf16x8*>(base + (row * U + swizzle<U>(row, u)) * 16);
+  return *reinterpret_cast<const bf16x8*>(base + row_at<U>(row) + u * 16);
 }
 
-// Rows r0 + 8 q .. + 7 of 16 columns as an operand whose lane (q, m) holds eight rows of one column:
-// the columns are four runs of four, run c at 8-byte position `half0 + step c` of a row.
+// Row sigma(t, n) of a matrix in LDS is row sigma(0, n) and a constant on
 template <int U>
-__device__ inline bf16x8 columns(const char* base, int r0, int half0, int step, int lane) {
-  const int q = lane / 16, k = lane % 16 / 4, c = lane % 4;
-  const int half = half0 + step * c;
+__device__ inline bf16x8 sigma_unit(const char* base, int t, int n, int u) {
+  return *reinterpret_cast<const bf16x8*>(base + row_at<U>(sigma(0, n)) + sigma(t, 0) * kStride<U> * 16 + u * 16);
+}
+
+// Rows r0 + 8 q .. + 7 of 16 columns as an operand whose lane (q, m) holds eight rows of one column: the
+// columns are four runs of four, run c at byte step c from `lane_base`, this lane's place in row 8 q + k
+template <int STRIDE>
+__device__ inline bf16x8 columns(const char* lane_base, int r0, int at) {
+  const char* p = lane_base + (r0 * STRIDE + at);
   union { s16x4 h[2]; bf16x8 v; } x;
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int row = r0 + 8 * q + 4 * j + k;
-    const char* p = base + (row * U + swizzle<U>(row, half / 2)) * 16 + (half % 2) * 8;
-    x.h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
-  }
+  x.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
+  x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * STRIDE));
   return x.v;
+}
+template <int U>
+__device__ inline int key_column(int lane) {
+  return row_at<U>(lane / 16 * 8 + lane % 16 / 4) + lane % 4 * 16;
+}
+template <int U>
+__device__ inline int value_column(int lane) {
+  return (lane / 16 * 8 + lane % 16 / 4) * kVStride<U> * 16 + lane % 4 * 8;
 }
 
 __device__ inline uint32_t high_halves(float x0, float x1) {
@@ -162,16 +185,26 @@ struct Decays {
   int32_t pad[2];
 };
 
+// x of the lane that a DPP control names, 0 where there is none or the row is masked out
+template <int CTRL, int ROWS>
+__device__ inline double from_lane(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, int(uint32_t(u)), CTRL, ROWS, 0xF, true);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, int(uint32_t(u >> 32)), CTRL, ROWS, 0xF, true);
+  return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
+
 // One wave fills in a chunk's decays, one token per lane; g: the token's log-decay, 0 past the end.
 // A log-decay below -2000 (in powers of two) is as good as -2000: both are a decay of 0.
 __device__ inline void make_decays(Decays& d, float g, float scale, int lane) {
   double x = double(g) * 1.4426950408889634;
   if (x < -2000.0) x = -2000.0;
-#pragma unroll
-  for (int s = 1; s < kC; s *= 2) {
-    const double y = __shfl_up(x, s);
-    if (lane >= s) x += y;
-  }
+  x += from_lane<0x111, 0xF>(x);            // the lanes before it in a row of 16
+  x += from_lane<0x112, 0xF>(x);
+  x += from_lane<0x114, 0xF>(x);
+  x += from_lane<0x118, 0xF>(x);
+  x += from_lane<0x142, 0xA>(x);            // the last lane of the row before
+  x += from_lane<0x143, 0xC>(x);            // the last lane of the first half
   const double end = __shfl(x, kC - 1);
   const float e = dasc_wy::ex2(float(x));
   d.G[lane] = x;
@@ -179,9 +212,8 @@ __device__ inline void make_decays(Decays& d, float g, float scale, int lane) {
   d.eo[lane] = scale * e;
   d.er[lane] = dasc_wy::ex2(float(end - x));
   if (lane == 0) {
-    const double f = exp2(end);
     const bool near = end > -0.72;
-    d.m = float(near ? f - 1.0 : f);
+    d.m = near ? expm1f(float(end * 0.6931471805599453)) : dasc_wy::ex2(float(end));
     d.near = near;
   }
 }
@@ -214,22 +246,30 @@ __device__ inline constexpr int block_of(int t, int s) { return t < 2 ? t : 2 + 
 constexpr int kBlocks = 6;
 constexpr int kPBytes = 2 * kBlocks * 1024;       // P: two planes
 constexpr int kTBytes = 3 * kBlocks * 1024;       // T: three planes
-constexpr int kPacket = kTBytes + kPBytes + int(sizeof(Decays));
+constexpr int kFBytes = kBlocks * 2048;           // T in fp32
 static_assert(sizeof(Decays) % 16 == 0, "packets are copied in 16-byte units");
 
-// P for one query tile c (tokens 16 c ..) and key group s, written into its A-operand blocks
+// What the factor kernel leaves for a chunk and head of the delta rule: decays and T, as planes and with
+// P for the split walk, which has no instruction to spare; in fp32 and alone for the walk by columns,
+// which is short of memory bandwidth and cuts T, and forms P, once for all its columns.
+template <bool PLANES>
+constexpr int kPacket = int(sizeof(Decays)) + (PLANES ? kTBytes + kPBytes : kFBytes);
+constexpr int kPacketT = int(sizeof(Decays)), kPacketP = kPacketT + kTBytes;
+
+// Block (t, s) of P as an A operand.  The product is formed transposed, keys as rows: its lane (q, n)
+// then holds keys 32 s + 8 q .. + 7 of query sigma(t, n), which is what the operand's lane holds.
 template <int DK, typename LoadK, typename LoadQ>
-__device__ inline void make_p(char* P, const double* G, float scale, int c, int s, int lane, LoadK&& ku, LoadQ&& qu) {
+__device__ inline void make_p(const double* G, float scale, int t, int s, int lane, LoadK&& ku, LoadQ&& qu,
+                              bf16x8& hi, bf16x8& lo) {
   const int q = lane / 16, n = lane % 16;
   f32x4 a0 = {0, 0, 0, 0}, a1 = {0, 0, 0, 0};
 #pragma unroll
   for (int kk = 0; kk < DK / 32; ++kk) {
-    const bf16x8 b = qu(16 * c + n, 4 * kk + q);
-    a0 = mma(ku(sigma(2 * s, n), 4 * kk + q), b, a0);
-    a1 = mma(ku(sigma(2 * s + 1, n), 4 * kk + q), b, a1);
+    const bf16x8 b = qu(kk);
+    a0 = mma(ku(2 * s, 4 * kk + q), b, a0);
+    a1 = mma(ku(2 * s + 1, 4 * kk + q), b, a1);
   }
-  // this lane: query token 16 c + n, key tokens 32 s + 8 q ..
-  const int tq = 16 * c + n, tk = 32 * s + 8 * q;
+  const int tq = sigma(t, n), tk = 32 * s + 8 * q;
   const double gq = G[tq];
   float x[8];
 #pragma unroll
@@ -237,30 +277,501 @@ __device__ inline void make_p(char* P, const double* G, float scale, int c, int 
     const float v = (e < 4 ? a0[e & 3] : a1[e & 3]) * (scale * decay_of(gq, G[tk + e]));
     x[e] = tk + e <= tq ? v : 0.0f;
   }
-  bf16x8 hi, lo;
   dasc_wy::split8(x, hi, lo);
-  const int r = tq % 32, t = 2 * (tq / 32) + (r / 4) % 2, m = 4 * (r / 8) + r % 4;
-  char* at = P + block_of(t, s) * 1024 + (16 * q + m) * 16;
-  *reinterpret_cast<bf16x8*>(at) = hi;
-  *reinterpret_cast<bf16x8*>(at + kBlocks * 1024) = lo;
 }
 
-template <int DK, int NW, bool DELTA, bool OUT>
+// four values cut into planes, as half of an operand's eight
+template <int N>
+__device__ inline void half_planes(f32x4 x, uint2 (&p)[N]) {
+  float r[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    p[j] = uint2{high_halves(r[0], r[1]), high_halves(r[2], r[3])};
+    if (j + 1 < N) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r[e] = rest(r[e]);
+    }
+  }
+}
+
+// Operands that the four waves of a column tile build together: one KB per group of 32 rows and plane,
+// lane l's eight values at 16 l, of which tile 2 s holds the first four and tile 2 s + 1 the others.
+template <int N>
+__device__ inline void put_half(char* base, int t, int lane, const uint2 (&p)[N]) {
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    *reinterpret_cast<uint2*>(base + ((t / 2) * N + j) * 1024 + lane * 16 + (t % 2) * 8) = p[j];
+}
+__device__ inline bf16x8 get(const char* base, int index, int lane) {
+  return *reinterpret_cast<const bf16x8*>(base + index * 1024 + lane * 16);
+}
+
+// The rows of a chunk from row `row` on, of which `left` are left: a buffer resource that ends with
+// the last of them
+__device__ inline __amdgpu_buffer_rsrc_t chunk_rows(const uint16_t* base, int tok, int width, int64_t row, int left) {
+  const int n = left < 0 ? 0 : left < kC ? left : kC;
+  return dasc_wy::rsrc(base + row * tok, n ? ((n - 1) * tok + width) * 2 : 0);
+}
+
+// What a block of either walk works on: a head's request (delta) or segment of one (plain), some columns
+struct Walk {
+  int cb, h, i, chunks, len;                // chunks < 0: nothing; len: tokens from row0 to the request's end
+  int64_t unit, row0, pk0, pk_step;
+  bool first, last;                         // it begins with the request's first token, ends with its last
+
+  // where its state comes from and where it goes; LOCAL: what a segment adds to a state of zero
+  template <bool DELTA, bool LOCAL>
+  __device__ inline const float* start(const ChunkArgs& p, int dk) const {
+    const int64_t head = int64_t(dk) * p.a.dv;
+    if (LOCAL) return nullptr;
+    if (DELTA) return first ? slot_state(p.a, p.a.src, i, h, dk) : p.carry_in + h * head;
+    return p.seg_chunks ? p.seg_state + (unit * p.a.H + h) * head : slot_state(p.a, p.a.src, i, h, dk);
+  }
+  template <bool DELTA, bool LOCAL>
+  __device__ inline float* end(const ChunkArgs& p, int dk) const {
+    const int64_t head = int64_t(dk) * p.a.dv;
+    if (LOCAL) return p.seg_state + (unit * p.a.H + h) * head;
+    if (last) return slot_state(p.a, p.a.dst, i, h, dk);
+    return DELTA ? p.carry_out + h * head : nullptr;
+  }
+
+  // rows of chunk c of a tensor, which end with the request
+  __device__ inline __amdgpu_buffer_rsrc_t rows(const uint16_t* base, int tok, int width, int c) const {
+    return chunk_rows(base, tok, width, row0 + int64_t(c) * kC, len - c * kC);
+  }
+  __device__ inline const char* packet(const ChunkArgs& p, int c) const {
+    return p.packets + pk0 + (c < chunks ? c : chunks - 1) * pk_step;
+  }
+  // this lane's log-decay of chunk c, 0 past the request's end
+  __device__ inline float gate(const LinearArgs& a, int c) const {
+    const int r = c * kC + int(threadIdx.x % 64);
+    const float g = a.io.g[(row0 + (r < len ? r : len - 1)) * a.io.g_tok + h * a.io.g_head];
+    return r < len ? g : 0.0f;
+  }
+};
+
+template <bool DELTA, bool PLANES>
+__device__ inline Walk walk_of(const ChunkArgs& p) {
+  const LinearArgs& a = p.a;
+  Walk w;
+  // blocks go round the eight XCDs: those of a head, and heads that share keys, are put on one
+  uint32_t bid = blockIdx.x;
+  if (gridDim.x % 8 == 0) bid = bid % 8 * (gridDim.x / 8) + bid / 8;
+  w.cb = bid % p.col_blocks;
+  w.h = bid / p.col_blocks % a.H;
+  w.unit = bid / p.col_blocks / a.H;
+  w.first = w.last = true;
+  Span sp;
+  int c0 = 0;
+  if (DELTA || p.seg_chunks == 0) {
+    w.i = int(w.unit);
+    sp = request_span(a, w.i);
+    w.chunks = (sp.len + kC - 1) / kC;
+    if constexpr (DELTA) {                  // the request's part of the window
+      const int64_t u = first_unit(a, w.i, kC);
+      const int all = w.chunks;
+      c0 = u < p.u0 ? int(p.u0 - u) : 0;
+      const int c1 = u + all > p.u1 ? int(p.u1 - u) : all;
+      if (u >= p.u1 || (c0 > 0 && c0 >= all)) {
+        w.chunks = -1;
+        return w;
+      }
+      w.chunks = c1 - c0;
+      w.first = c0 == 0;
+      w.last = c1 == all;
+    }
+  } else {
+    const int seg = p.seg_chunks;
+    w.i = uniform(unit_request(a, w.unit, seg * kC));
+    sp = request_span(a, w.i);
+    const int64_t j = w.unit - first_unit(a, w.i, seg * kC);
+    const int all = (sp.len + kC - 1) / kC;
+    if (j < 0 || (j * seg >= all && j > 0)) {
+      w.chunks = -1;
+      return w;
+    }
+    c0 = int(j) * seg;
+    w.chunks = all - c0 < seg ? all - c0 : seg;
+    w.last = c0 + w.chunks >= all;
+  }
+  c0 = uniform(c0);
+  w.chunks = uniform(w.chunks);
+  w.row0 = uniform(sp.begin + int64_t(c0) * kC);
+  w.len = uniform(sp.len - c0 * kC);
+  w.pk0 = DELTA ? uniform(((first_unit(a, w.i, kC) + c0 - p.u0) * a.H + w.h) * int64_t(kPacket<PLANES>)) : 0;
+  w.pk_step = int64_t(a.H) * kPacket<PLANES>;
+  return w;
+}
+
+constexpr int kOutside = int(0x80000000u);  // an offset past the end of any resource
+
+// LDS of a block of CT NG column tiles.  Delta: keys and decays twice, S, Y, e^{G_C - G} U in three
+// planes, U in two.  Plain: S in two planes, V, e^{G_C - G} V in three.
+template <int DK, int TILES, bool DELTA, bool OUT>
 struct Layout {
-  static constexpr int kRow = kC * DK * 2;
+  static constexpr int kK = kRowsBytes<DK / 8>;
+  static constexpr int kKeys = DELTA ? 2 : 1;
+  static constexpr int kSPlanes = DELTA ? 3 : OUT ? 2 : 0;
+  static constexpr int kVPlanes = OUT ? (DELTA ? 2 : 1) : 0;
+  static constexpr int kDecays = DELTA ? 2 : 3;
+  static constexpr int kSBytes = DK / 32 * kSPlanes * 1024;
+  static constexpr int kS = kKeys * kK;
+  static constexpr int kY = kS + TILES * kSBytes;
+  static constexpr int kU = kY + TILES * (DELTA ? 6 * 1024 : 0);
+  static constexpr int kW = kU + TILES * 6 * 1024;
+  static constexpr int kD = kW + TILES * kVPlanes * 2 * 1024;
+  static constexpr int kBytes = kD + kDecays * int(sizeof(Decays));
+};
+
+// One block walks one request of a head over 16 CT NG columns.
+// Its waves are NG groups of four; a group has CT column tiles, and wave m of it has tokens sigma(m, .)
+// of every product over channels and DK / 4 channels of the state.  What the others need of a wave's
+// part goes through LDS in operand order.
+template <int DK, int CT, int NG, bool DELTA, bool OUT>
+__global__ __launch_bounds__(256 * NG) void linear_split_kernel(ChunkArgs p) {
+  constexpr int NT = 256 * NG, U = DK / 8, SK = DK / 32, TW = DK / 64, TILES = CT * NG;
+  using L = Layout<DK, TILES, DELTA, OUT>;
+  __shared__ __attribute__((aligned(16))) char lds[L::kBytes];
+  Decays* const dec = reinterpret_cast<Decays*>(lds + L::kD);
+
+  const LinearArgs& a = p.a;
+  const int tid = threadIdx.x, wave = uniform(tid / 64), lane = tid % 64, q = lane / 16, n = lane % 16;
+  const int m = wave % 4, grp = wave / 4;
+  const Walk w = walk_of<DELTA, true>(p);
+  if (w.chunks < 0) return;
+  const int k_col = key_column<U>(lane);
+  const int h = w.h, hk = h / a.rep, dv = a.dv, chunks = w.chunks;
+
+  // the state: lane (q, n) holds channels sigma(TW m + t, 4 q + e) of column n of each column tile
+  const int tile0 = grp * CT;               // this group's first column tile in the block
+  const int col0 = 16 * (w.cb * TILES + tile0) + n;
+  f32x4 S[CT][TW];
+  {
+    const float* from = w.start<DELTA, false>(p, DK);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int t = 0; t < TW; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          S[ct][t][e] = from && col0 + 16 * ct < dv
+                            ? from[int64_t(sigma(TW * m + t, 4 * q + e)) * dv + col0 + 16 * ct] : 0.0f;
+  }
+
+  // What a chunk takes from memory is asked for a chunk ahead: keys (staged by all waves), and this
+  // wave's queries, values, blocks of T and of P.  Rows come through buffer resources that end with the
+  // request's last row of the chunk: what lies past it reads as zero, and stores there are dropped.
+  // Every load is issued on every path, so that a wait for one never waits for those behind it.
+  constexpr int kRows = NT / U, kPasses = kC / kRows;
+  u32x4 rk[kPasses], rd;
+  bf16x8 rq[OUT ? SK : 1], rt[DELTA ? 2 : 1][3], rp[2][2];
+  uint16_t rv[CT][4];
+  float rg = 0;
+  const bool deep = m >= 2;                 // a wave of the later tokens has two blocks, (m, 0) and (m, 1)
+  const uint16_t* const kb = a.io.k + hk * a.io.k_head;
+  const uint16_t* const qb = a.io.q + (OUT ? hk * a.io.q_head : 0);
+  const uint16_t* const vb = a.io.v + h * a.io.v_head;
+  uint16_t* const ob = a.io.o + (OUT ? h * a.io.o_head : 0);
+  const int k_off = (tid / U * p.k_tok + 8 * (tid % U)) * 2;
+  const int q_off = (sigma(m, n) * p.q_tok + 8 * q) * 2;
+  int v_off[CT], o_off[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const bool in = col0 + 16 * ct < dv;
+    v_off[ct] = in ? (sigma(m, 4 * q) * p.v_tok + col0 + 16 * ct) * 2 : kOutside;
+    o_off[ct] = in ? (sigma(m, 4 * q) * p.o_tok + col0 + 16 * ct) * 2 : kOutside;
+  }
+  const auto load_k = [&](int c) {
+    const __amdgpu_buffer_rsrc_t r = w.rows(kb, p.k_tok, DK, c);
+#pragma unroll
+    for (int j = 0; j < kPasses; ++j)
+      rk[j] = __builtin_bit_cast(u32x4, dasc_wy::ldf4(r, k_off, j * kRows * p.k_tok * 2));
+    if constexpr (DELTA) {
+      constexpr int kLast = int(sizeof(Decays)) / 16 - 1;
+      rd = reinterpret_cast<const u32x4*>(w.packet(p, c))[tid < kLast ? tid : kLast];
+    }
+  };
+  const auto put_k = [&](int c) {
+    char* K = lds + (DELTA ? (c & 1) * L::kK : 0);
+#pragma unroll
+    for (int j = 0; j < kPasses; ++j) {
+      const int r = j * kRows + tid / U;
+      *reinterpret_cast<u32x4*>(K + row_at<U>(r) + tid % U * 16) = rk[j];
+    }
+    if constexpr (DELTA) {
+      if (tid < int(sizeof(Decays)) / 16) reinterpret_cast<u32x4*>(dec + (c & 1))[tid] = rd;
+    }
+  };
+  const auto load_q = [&](int c) {
+    if constexpr (OUT) {
+      const __amdgpu_buffer_rsrc_t r = w.rows(qb, p.q_tok, DK, c);
+#pragma unroll
+      for (int s = 0; s < SK; ++s) rq[s] = __builtin_bit_cast(bf16x8, dasc_wy::ldf4(r, q_off, 64 * s));
+    }
+  };
+  const auto load_v = [&](int c) {
+    const __amdgpu_buffer_rsrc_t r = w.rows(vb, p.v_tok, dv, c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+        rv[ct][e] = uint16_t(__builtin_amdgcn_raw_buffer_load_b16(r, v_off[ct], e * p.v_tok * 2, 0));
+  };
+  const auto load_t = [&](int c) {
+    if constexpr (DELTA) {
+      const char* pk = w.packet(p, c) + kPacketT;
+#pragma unroll
+      for (int j = 0; j < 3; ++j) {
+        rt[0][j] = get(pk, j * kBlocks + block_of(m, 0), lane);
+        rt[1][j] = get(pk, j * kBlocks + block_of(m, 1), lane);
+      }
+    }
+  };
+  const auto load_p = [&](int c) {
+    if constexpr (DELTA && OUT) {
+      const char* pk = w.packet(p, c) + kPacketP;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        rp[0][j] = get(pk, j * kBlocks + block_of(m, 0), lane);
+        rp[1][j] = get(pk, j * kBlocks + block_of(m, 1), lane);
+      }
+    }
+  };
+  const auto put_s = [&]() {                // the state's planes, for all waves of the column tile
+    if constexpr (L::kSPlanes > 0) {
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int t = 0; t < TW; ++t) {
+          uint2 h2[L::kSPlanes];
+          half_planes(S[ct][t], h2);
+          put_half(lds + L::kS + (tile0 + ct) * L::kSBytes, TW * m + t, lane, h2);
+        }
+    }
+  };
+  const auto put_v = [&](const Decays& d) { // plain: the values, and what they add to the state
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      if constexpr (OUT) {
+        const uint2 raw[1] = {uint2{rv[ct][0] | uint32_t(rv[ct][1]) << 16, rv[ct][2] | uint32_t(rv[ct][3]) << 16}};
+        put_half(lds + L::kW + (tile0 + ct) * 2048, m, lane, raw);
+      }
+      f32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(uint32_t(rv[ct][e]) << 16) * d.er[sigma(m, 4 * q + e)];
+      uint2 h3[3];
+      half_planes(x, h3);
+      put_half(lds + L::kU + (tile0 + ct) * 6144, m, lane, h3);
+    }
+  };
+
+  if (chunks > 0) {
+    load_k(0);
+    load_q(0);
+    load_v(0);
+    load_t(0);
+    load_p(0);
+    if constexpr (!DELTA) {
+      if (wave == 0) {
+        make_decays(dec[0], w.gate(a, 0), a.scale, lane);
+        make_decays(dec[1], w.gate(a, 1), a.scale, lane);
+      }
+      rg = w.gate(a, 2);
+      lds_barrier();
+      put_v(dec[0]);
+    }
+    put_k(0);
+    put_s();
+    load_k(1);
+    lds_barrier();
+  }
+
+  for (int c = 0; c < chunks; ++c) {
+    const char* const K = lds + (DELTA ? (c & 1) * L::kK : 0);
+    const Decays& d = DELTA ? dec[c & 1] : dec[c % 3];
+    const bool more = c + 1 < chunks;
+    if constexpr (!DELTA) load_v(c + 1);
+    f32x4 O[CT], X[CT];
+    // products with the state: Q S, K S
+    if constexpr (OUT || DELTA) {
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) O[ct] = X[ct] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < SK; ++s) {
+        bf16x8 k;
+        if constexpr (DELTA) k = sigma_unit<U>(K, m, n, 4 * s + q);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          const char* sb = lds + L::kS + (tile0 + ct) * L::kSBytes;
+          bf16x8 x[L::kSPlanes];
+#pragma unroll
+          for (int j = 0; j < L::kSPlanes; ++j) x[j] = get(sb, s * L::kSPlanes + j, lane);
+          if constexpr (DELTA) {
+            X[ct] = mma(k, x[2], X[ct]);
+            if constexpr (OUT) O[ct] = mma(rq[s], x[1], O[ct]);
+            X[ct] = mma(k, x[1], X[ct]);
+            if constexpr (OUT) O[ct] = mma(rq[s], x[0], O[ct]);
+            X[ct] = mma(k, x[0], X[ct]);
+          } else {
+            O[ct] = mma(rq[s], x[1], O[ct]);
+            O[ct] = mma(rq[s], x[0], O[ct]);
+          }
+        }
+      }
+      if constexpr (OUT) {
+        const f32x4 eo = *reinterpret_cast<const f32x4*>(d.eo + sigma(m, 4 * q));
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) O[ct] *= eo;
+      }
+    }
+    if constexpr (DELTA) {
+      load_q(c + 1);
+      const f32x4 ex = *reinterpret_cast<const f32x4*>(d.e + sigma(m, 4 * q));
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        f32x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = fmaf(-ex[e], X[ct][e], __uint_as_float(uint32_t(rv[ct][e]) << 16));
+        uint2 h3[3];
+        half_planes(y, h3);
+        put_half(lds + L::kY + (tile0 + ct) * 6144, m, lane, h3);
+      }
+      load_v(c + 1);
+      lds_barrier();                        // Y is whole
+      const f32x4 er = *reinterpret_cast<const f32x4*>(d.er + sigma(m, 4 * q));
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        f32x4 u = {0, 0, 0, 0};
+        const char* yb = lds + L::kY + (tile0 + ct) * 6144;
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          if (s == 0 || deep) {
+            const bf16x8 y0 = get(yb, 3 * s, lane), y1 = get(yb, 3 * s + 1, lane), y2 = get(yb, 3 * s + 2, lane);
+            u = mma(rt[s][2], y0, u);
+            u = mma(rt[s][0], y2, u);
+            u = mma(rt[s][1], y1, u);
+            u = mma(rt[s][1], y0, u);
+            u = mma(rt[s][0], y1, u);
+            u = mma(rt[s][0], y0, u);
+          }
+        if constexpr (OUT) {
+          uint2 h2[2];
+          half_planes(u, h2);
+          put_half(lds + L::kW + (tile0 + ct) * 4096, m, lane, h2);
+        }
+        uint2 h3[3];
+        half_planes(u * er, h3);
+        put_half(lds + L::kU + (tile0 + ct) * 6144, m, lane, h3);
+      }
+      load_t(c + 1);
+      lds_barrier();                        // U is whole
+    } else if constexpr (OUT) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+        if (s == 0 || deep)
+          make_p<DK>(d.G, a.scale, m, s, lane, [&](int x, int u) { return sigma_unit<U>(K, x, n, u); },
+                     [&](int kk) { return rq[kk]; }, rp[s][0], rp[s][1]);
+      load_q(c + 1);
+    }
+
+    if constexpr (OUT) {
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        const char* wb = lds + L::kW + (tile0 + ct) * (DELTA ? 4096 : 2048);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          if (s == 0 || deep) {
+            if constexpr (DELTA) {
+              const bf16x8 u0 = get(wb, 2 * s, lane), u1 = get(wb, 2 * s + 1, lane);
+              O[ct] = mma(rp[s][0], u1, O[ct]);
+              O[ct] = mma(rp[s][1], u0, O[ct]);
+              O[ct] = mma(rp[s][0], u0, O[ct]);
+            } else {
+              const bf16x8 v = get(wb, s, lane);
+              O[ct] = mma(rp[s][1], v, O[ct]);
+              O[ct] = mma(rp[s][0], v, O[ct]);
+            }
+          }
+      }
+      load_p(c + 1);
+      const __amdgpu_buffer_rsrc_t ro = w.rows(ob, p.o_tok, dv, c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+          __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(short, __bf16(O[ct][e])), ro, o_off[ct],
+                                                e * p.o_tok * 2, 0);
+    }
+
+    // the state
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) decay_state<TW>(S[ct], d);
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int t = 0; t < TW; ++t) {
+        const int tt = TW * m + t;
+        const bf16x8 k = columns<kStride<U> * 16>(K + k_col, 32 * s, 64 * (tt / 2) + 8 * (tt % 2));
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          const char* ub = lds + L::kU + (tile0 + ct) * 6144;
+          S[ct][t] = mma(k, get(ub, 3 * s + 2, lane), S[ct][t]);
+          S[ct][t] = mma(k, get(ub, 3 * s + 1, lane), S[ct][t]);
+          S[ct][t] = mma(k, get(ub, 3 * s, lane), S[ct][t]);
+        }
+      }
+    if (more) {
+      if constexpr (!DELTA) {
+        lds_barrier();                      // everybody is done with this chunk
+        put_v(dec[(c + 1) % 3]);
+        if (wave == 0) make_decays(dec[(c + 2) % 3], rg, a.scale, lane);
+        rg = w.gate(a, c + 3);
+      }
+      put_k(c + 1);
+      put_s();
+      load_k(c + 2);
+      lds_barrier();
+    }
+  }
+
+  float* to = w.end<DELTA, false>(p, DK);
+  if (to) {
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+      if (col0 + 16 * ct < dv) {
+#pragma unroll
+        for (int t = 0; t < TW; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            to[int64_t(sigma(TW * m + t, 4 * q + e)) * dv + col0 + 16 * ct] = S[ct][t][e];
+      }
+  }
+}
+
+// ---- a wave per 16 columns ------------------------------------------------------------------------
+
+template <int DK, int TILES, bool DELTA, bool OUT>
+struct ColumnLayout {
+  static constexpr int kRow = kRowsBytes<DK / 8>;
   static constexpr int kV = kRow * (OUT ? 2 : 1);
-  static constexpr int kP = kV + kC * NW * 32;
+  static constexpr int kP = kV + kC * kVStride<2 * TILES> * 16;
   static constexpr int kT = kP + (OUT ? kPBytes : 0);
   static constexpr int kD = kT + (DELTA ? kTBytes : 0);
   static constexpr int kBytes = kD + int(sizeof(Decays)) * (DELTA ? 1 : 2);
 };
 
-// One block walks one request (delta) or one segment of one (plain) of a head, 16 NW columns.
+// waves of a SIMD that the registers are to leave room for
+template <int CT, bool DELTA, bool OUT>
+constexpr int kWavesPerSimd = CT == 1 && !DELTA && !OUT ? 4 : 2;
+
+// One block walks one request (delta) or one segment of one (plain) of a head over 16 CT NW columns, a wave
+// on 16 CT.  A wave has the whole state of its columns and needs nothing of another's: K, Q, V, P and T lie
+// in LDS for all of them.
 // LOCAL: only what the segment adds to a state of zero, left in seg_state for the join.
-template <int DK, int NW, bool DELTA, bool OUT, bool LOCAL>
-__global__ __launch_bounds__(64 * NW) void linear_chunk_kernel(ChunkArgs p) {
-  constexpr int NT = 64 * NW, KT = DK / 16, U = DK / 8, UV = 2 * NW;
-  using L = Layout<DK, NW, DELTA, OUT>;
+template <int DK, int CT, int NW, bool DELTA, bool OUT, bool LOCAL>
+__global__ __launch_bounds__(64 * NW, (kWavesPerSimd<CT, DELTA, OUT>)) void linear_columns_kernel(ChunkArgs p) {
+  constexpr int NT = 64 * NW, KT = DK / 16, U = DK / 8, UV = 2 * CT * NW;
+  using L = ColumnLayout<DK, CT * NW, DELTA, OUT>;
   __shared__ __attribute__((aligned(16))) char lds[L::kBytes];
   char* const K = lds;
   char* const Q = lds + L::kRow;
@@ -270,120 +781,103 @@ __global__ __launch_bounds__(64 * NW) void linear_chunk_kernel(ChunkArgs p) {
   Decays* const dec = reinterpret_cast<Decays*>(lds + L::kD);
 
   const LinearArgs& a = p.a;
-  const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, q = lane / 16, n = lane % 16;
-  const int cb = blockIdx.x % p.col_blocks;
-  const int h = blockIdx.x / p.col_blocks % a.H;
-  const int64_t unit = blockIdx.x / p.col_blocks / a.H;
-  const int hk = h / a.rep, dv = a.dv;
+  const int tid = threadIdx.x, wave = uniform(tid / 64), lane = tid % 64, q = lane / 16, n = lane % 16;
+  const Walk w = walk_of<DELTA, false>(p);
+  if (w.chunks < 0) return;
+  const int k_col = key_column<U>(lane), v_col = value_column<UV>(lane);
+  const int h = w.h, hk = h / a.rep, dv = a.dv, chunks = w.chunks;
 
-  // the tokens of this block
-  int i, c0, chunks;
-  bool first = true, last = true;
-  Span sp;
-  if constexpr (DELTA) {
-    i = int(unit);
-    sp = request_span(a, i);
-    c0 = 0;
-    chunks = (sp.len + kC - 1) / kC;
-  } else {
-    const int seg = p.seg_chunks;
-    if (seg == 0) {
-      i = int(unit);
-      sp = request_span(a, i);
-      c0 = 0;
-      chunks = (sp.len + kC - 1) / kC;
-    } else {
-      i = unit_request(a, unit, seg * kC);
-      sp = request_span(a, i);
-      const int64_t j = unit - first_unit(a, i, seg * kC);
-      const int all = (sp.len + kC - 1) / kC;
-      if (j < 0 || (j * seg >= all && j > 0)) return;
-      c0 = int(j) * seg;
-      chunks = all - c0 < seg ? all - c0 : seg;
-      first = false;                        // the join has left every segment's start
-      last = c0 + chunks >= all;
-    }
-  }
-  const int64_t row0 = sp.begin + int64_t(c0) * kC;
-  const int len = sp.len - c0 * kC;         // tokens from row0 to the request's end
-
-  // the state: lane (q, n) holds channels sigma(t, 4 q + i) of column n
-  const int col = 16 * (cb * NW + wave) + n;
-  const bool in = col < dv;
-  f32x4 S[KT];
+  // the state: lane (q, n) holds channels sigma(t, 4 q + i) of column n of each tile
+  const int col = 16 * CT * (w.cb * NW + wave) + n;
+  f32x4 S[CT][KT];
   {
-    const float* from = LOCAL ? nullptr
-                       : first ? slot_state(a, a.src, i, h, DK)
-                               : p.seg_state + (unit * a.H + h) * int64_t(DK) * dv;
+    const float* from = w.start<DELTA, LOCAL>(p, DK);
 #pragma unroll
-    for (int t = 0; t < KT; ++t)
+    for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        S[t][e] = from && in ? from[int64_t(sigma(t, 4 * q + e)) * dv + col] : 0.0f;
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          S[ct][t][e] = from && col + 16 * ct < dv
+                            ? from[int64_t(sigma(t, 4 * q + e)) * dv + col + 16 * ct] : 0.0f;
   }
 
-  // staging: 16-byte units of K, Q and V rows, and the packet, through registers
+  // What a chunk takes from memory goes through registers a chunk ahead: 16-byte units of K, Q and V
+  // rows and of the packet.  Rows come through buffer resources that end with the request's last row of
+  // the chunk; what lies past it reads as zero.
   constexpr int kRowsPass = NT / U, kPasses = kC / kRowsPass;
   constexpr int kVRows = NT / UV, kVPasses = kC / kVRows;
-  constexpr int kPk = DELTA ? ((OUT ? kPacket : kPacket - kPBytes) / 16 + NT - 1) / NT : 0;
-  u32x4 rk[kPasses], rq[OUT ? kPasses : 1], rv[kVPasses], rp[kPk ? kPk : 1];
-  float g_next = 0;
-  const uint16_t* const kb = a.io.k + row0 * p.k_tok + hk * a.io.k_head + 8 * (tid % U);
-  const uint16_t* const qb = OUT ? a.io.q + row0 * p.q_tok + hk * a.io.q_head + 8 * (tid % U) : nullptr;
-  const int vcol = 16 * NW * cb + 8 * (tid % UV);
-  const uint16_t* const vb = a.io.v + row0 * p.v_tok + h * a.io.v_head + vcol;
-  const int64_t slot0 = DELTA ? first_unit(a, i, kC) + c0 : 0;
-
+  constexpr int kT = DELTA ? (kBlocks * 64 + NT - 1) / NT : 0;   // a lane's eight values of a block of T each
+  u32x4 rk[kPasses], rq[OUT ? kPasses : 1], rv[kVPasses], rd;
+  float rt[kT ? kT : 1][8];
+  float rg = 0;
+  const uint16_t* const kb = a.io.k + hk * a.io.k_head;
+  const uint16_t* const qb = a.io.q + (OUT ? hk * a.io.q_head : 0);
+  const uint16_t* const vb = a.io.v + h * a.io.v_head;
+  uint16_t* const ob = a.io.o + (OUT ? h * a.io.o_head : 0);
+  const int vcol = 16 * CT * NW * w.cb + 8 * (tid % UV);
+  const int k_off = (tid / U * p.k_tok + 8 * (tid % U)) * 2;
+  const int q_off = (tid / U * p.q_tok + 8 * (tid % U)) * 2;
+  const int v_off = vcol < dv ? (tid / UV * p.v_tok + vcol) * 2 : kOutside;
+  int o_off[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+    o_off[ct] = col + 16 * ct < dv ? (8 * q * p.o_tok + col + 16 * ct) * 2 : kOutside;
   const auto load = [&](int c) {
-    const int at = c * kC, end = len - 1;   // rows past the end repeat the last one
+    const __amdgpu_buffer_rsrc_t k = w.rows(kb, p.k_tok, DK, c), v = w.rows(vb, p.v_tok, dv, c);
 #pragma unroll
-    for (int j = 0; j < kPasses; ++j) {
-      int r = at + j * kRowsPass + tid / U;
-      r = r < end ? r : end;
-      rk[j] = *reinterpret_cast<const u32x4*>(kb + int64_t(r) * p.k_tok);
-      if (OUT) rq[j] = *reinterpret_cast<const u32x4*>(qb + int64_t(r) * p.q_tok);
+    for (int j = 0; j < kPasses; ++j)
+      rk[j] = __builtin_bit_cast(u32x4, dasc_wy::ldf4(k, k_off, j * kRowsPass * p.k_tok * 2));
+    if constexpr (OUT) {
+      const __amdgpu_buffer_rsrc_t x = w.rows(qb, p.q_tok, DK, c);
+#pragma unroll
+      for (int j = 0; j < kPasses; ++j)
+        rq[j] = __builtin_bit_cast(u32x4, dasc_wy::ldf4(x, q_off, j * kRowsPass * p.q_tok * 2));
     }
 #pragma unroll
-    for (int j = 0; j < kVPasses; ++j) {    // values past the end are zero, and so is what they add
-      const int r = at + j * kVRows + tid / UV;
-      rv[j] = r <= end && vcol < dv ? *reinterpret_cast<const u32x4*>(vb + int64_t(r) * p.v_tok) : u32x4{0, 0, 0, 0};
-    }
+    for (int j = 0; j < kVPasses; ++j)
+      rv[j] = __builtin_bit_cast(u32x4, dasc_wy::ldf4(v, v_off, j * kVRows * p.v_tok * 2));
     if constexpr (DELTA) {
-      const char* pk = p.packets + ((slot0 + c) * a.H + h) * kPacket;
+      const char* pk = w.packet(p, c);
+      constexpr int kLast = int(sizeof(Decays)) / 16 - 1;
+      rd = reinterpret_cast<const u32x4*>(pk)[tid < kLast ? tid : kLast];
 #pragma unroll
-      for (int j = 0; j < kPk; ++j) {
-        int off = (j * NT + tid) * 16;
-        if (!OUT && off >= kTBytes) off += kPBytes;
-        if (off < kPacket) rp[j] = *reinterpret_cast<const u32x4*>(pk + off);
+      for (int j = 0; j < kT; ++j) {
+        const int x = j * NT + tid;
+        const f32x4* f = reinterpret_cast<const f32x4*>(pk + kPacketT) + (x < kBlocks * 64 ? x : 0);
+        const f32x4 lo = f[0], hi = f[kBlocks * 64];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          rt[j][e] = lo[e];
+          rt[j][4 + e] = hi[e];
+        }
       }
+    } else {
+      rg = w.gate(a, c + 1);
     }
-  };
-  const auto load_g = [&](int c) {
-    const int r = c * kC + lane;
-    return r < len ? a.io.g[(row0 + r) * a.io.g_tok + h * a.io.g_head] : 0.0f;
   };
   const auto stage = [&]() {
 #pragma unroll
     for (int j = 0; j < kPasses; ++j) {
-      const int r = j * kRowsPass + tid / U, at = (r * U + swizzle<U>(r, tid % U)) * 16;
+      const int r = j * kRowsPass + tid / U, at = row_at<U>(r) + tid % U * 16;
       *reinterpret_cast<u32x4*>(K + at) = rk[j];
       if (OUT) *reinterpret_cast<u32x4*>(Q + at) = rq[j];
     }
 #pragma unroll
     for (int j = 0; j < kVPasses; ++j) {
       const int r = j * kVRows + tid / UV;
-      *reinterpret_cast<u32x4*>(V + (r * UV + swizzle<UV>(r, tid % UV)) * 16) = rv[j];
+      *reinterpret_cast<u32x4*>(V + (r * kVStride<UV> + tid % UV) * 16) = rv[j];
     }
     if constexpr (DELTA) {
+      if (tid < int(sizeof(Decays)) / 16) reinterpret_cast<u32x4*>(dec)[tid] = rd;
 #pragma unroll
-      for (int j = 0; j < kPk; ++j) {
-        int off = (j * NT + tid) * 16;
-        if (!OUT && off >= kTBytes) off += kPBytes;
-        if (off < kPacket) {
-          char* to = off < kTBytes ? T + off
-                     : off < kTBytes + kPBytes ? P + (off - kTBytes)
-                                               : reinterpret_cast<char*>(dec) + (off - kTBytes - kPBytes);
-          *reinterpret_cast<u32x4*>(to) = rp[j];
+      for (int j = 0; j < kT; ++j) {
+        const int x = j * NT + tid;
+        bf16x8 t[3];
+        planes<3>(rt[j], t);
+        if (x < kBlocks * 64) {
+#pragma unroll
+          for (int y = 0; y < 3; ++y) *reinterpret_cast<bf16x8*>(T + y * kBlocks * 1024 + x * 16) = t[y];
         }
       }
     }
@@ -393,157 +887,172 @@ __global__ __launch_bounds__(64 * NW) void linear_chunk_kernel(ChunkArgs p) {
   if (chunks > 0) {
     load(0);
     if constexpr (!DELTA) {
-      if (wave == NW - 1) {
-        make_decays(dec[0], load_g(0), a.scale, lane);
-        g_next = load_g(1);
-      }
+      if (wave == NW - 1) make_decays(dec[0], w.gate(a, 0), a.scale, lane);
     }
     stage();
   }
-  __syncthreads();
+  lds_barrier();
 
   for (int c = 0; c < chunks; ++c) {
     const Decays& d = DELTA ? dec[0] : dec[c & 1];
-    if (c + 1 < chunks) load(c + 1);
-    f32x4 O[4], X[4];
-    bf16x8 v[2];
-    // what needs the state: Q S, K S
-    if constexpr (OUT || DELTA) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t) O[t] = X[t] = f32x4{0, 0, 0, 0};
-#pragma unroll
-      for (int s = 0; s < DK / 32; ++s) {
-        bf16x8 sp_[3];
-        planes<3>(S[2 * s], S[2 * s + 1], sp_);
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const int r = sigma(t, n);
-          if constexpr (DELTA) {
-            const bf16x8 k = row_unit<U>(K, r, 4 * s + q);
-            X[t] = mma(k, sp_[2], X[t]);
-            X[t] = mma(k, sp_[1], X[t]);
-            X[t] = mma(k, sp_[0], X[t]);
-          }
-          if constexpr (OUT) {
-            const bf16x8 x = row_unit<U>(Q, r, 4 * s + q);
-            O[t] = mma(x, sp_[1], O[t]);
-            O[t] = mma(x, sp_[0], O[t]);
-          }
-        }
+    const float g_next = rg;
+    load(c + 1);
+    if constexpr (OUT) {
+      for (int b = wave; b < kBlocks; b += NW) {
+        const int t = b < 2 ? b : 2 + (b - 2) / 2, s = b < 2 ? 0 : (b - 2) % 2;
+        bf16x8 hi, lo;
+        make_p<DK>(d.G, a.scale, t, s, lane, [&](int x, int u) { return sigma_unit<U>(K, x, n, u); },
+                   [&](int kk) { return sigma_unit<U>(Q, t, n, 4 * kk + q); }, hi, lo);
+        char* at = P + b * 1024 + lane * 16;
+        *reinterpret_cast<bf16x8*>(at) = hi;
+        *reinterpret_cast<bf16x8*>(at + kBlocks * 1024) = lo;
       }
     }
     if constexpr (!DELTA) {
-      if constexpr (OUT) {
-        for (int w = wave; w < kBlocks; w += NW) {
-          const int qt = w < 2 ? w : 2 + (w - 2) / 2, s = w < 2 ? 0 : (w - 2) % 2;
-          make_p<DK>(P, d.G, a.scale, qt, s, lane,
-                     [&](int r, int u) { return row_unit<U>(K, r, u); },
-                     [&](int r, int u) { return row_unit<U>(Q, r, u); });
+      if (wave == NW - 1) make_decays(dec[(c + 1) & 1], g_next, a.scale, lane);
+    }
+    f32x4 O[CT][4], X[CT][4];
+    bf16x8 v[CT][2];
+    // what needs the state: Q S, K S
+    if constexpr (OUT || DELTA) {
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) O[ct][t] = X[ct][t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < DK / 32; ++s) {
+        bf16x8 b[CT][3];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) planes<3>(S[ct][2 * s], S[ct][2 * s + 1], b[ct]);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          if constexpr (DELTA) {
+            const bf16x8 k = sigma_unit<U>(K, t, n, 4 * s + q);
+#pragma unroll
+            for (int j = 2; j >= 0; --j)
+#pragma unroll
+              for (int ct = 0; ct < CT; ++ct) X[ct][t] = mma(k, b[ct][j], X[ct][t]);
+          }
+          if constexpr (OUT) {
+            const bf16x8 x = sigma_unit<U>(Q, t, n, 4 * s + q);
+#pragma unroll
+            for (int j = 1; j >= 0; --j)
+#pragma unroll
+              for (int ct = 0; ct < CT; ++ct) O[ct][t] = mma(x, b[ct][j], O[ct][t]);
+          }
         }
       }
-      if (wave == NW - 1 && c + 1 < chunks) {
-        make_decays(dec[(c + 1) & 1], g_next, a.scale, lane);
-        g_next = load_g(c + 2);
-      }
-      if constexpr (OUT) lds_barrier();     // P is whole
     }
+    if constexpr (OUT) lds_barrier();       // P is whole
 #pragma unroll
-    for (int s = 0; s < 2; ++s) v[s] = columns<UV>(V, 32 * s, 4 * wave, 1, lane);
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) v[ct][s] = columns<kVStride<UV> * 16>(V + v_col, 32 * s, 32 * (wave * CT + ct));
 
-    f32x4 Uf[4];                            // U in fp32
+    f32x4 Uf[CT][4];                        // U in fp32
     if constexpr (DELTA) {
-      bf16x8 y[2][3];
+      bf16x8 y[CT][2][3];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        float x[8];
-        widen8(v[s], x);
+      for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          x[e] = fmaf(-d.e[32 * s + 8 * q + e], X[2 * s + e / 4][e % 4], x[e]);
-        planes<3>(x, y[s]);
-      }
+        for (int s = 0; s < 2; ++s) {
+          float x[8];
+          widen8(v[ct][s], x);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            x[e] = fmaf(-d.e[32 * s + 8 * q + e], X[ct][2 * s + e / 4][e % 4], x[e]);
+          planes<3>(x, y[ct][s]);
+        }
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        Uf[t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) Uf[ct][t] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int s = 0; s <= t / 2; ++s) {
           const char* b = T + block_of(t, s) * 1024 + lane * 16;
           const bf16x8 t0 = *reinterpret_cast<const bf16x8*>(b);
           const bf16x8 t1 = *reinterpret_cast<const bf16x8*>(b + kBlocks * 1024);
           const bf16x8 t2 = *reinterpret_cast<const bf16x8*>(b + 2 * kBlocks * 1024);
-          Uf[t] = mma(t2, y[s][0], Uf[t]);
-          Uf[t] = mma(t0, y[s][2], Uf[t]);
-          Uf[t] = mma(t1, y[s][1], Uf[t]);
-          Uf[t] = mma(t1, y[s][0], Uf[t]);
-          Uf[t] = mma(t0, y[s][1], Uf[t]);
-          Uf[t] = mma(t0, y[s][0], Uf[t]);
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            f32x4 u = Uf[ct][t];
+            u = mma(t2, y[ct][s][0], u);
+            u = mma(t0, y[ct][s][2], u);
+            u = mma(t1, y[ct][s][1], u);
+            u = mma(t1, y[ct][s][0], u);
+            u = mma(t0, y[ct][s][1], u);
+            Uf[ct][t] = mma(t0, y[ct][s][0], u);
+          }
         }
-      }
-    } else {
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        float x[8];
-        widen8(v[s], x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) Uf[2 * s + e / 4][e % 4] = x[e];
       }
     }
 
     if constexpr (OUT) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+      for (int t = 0; t < 4; ++t) {
+        const f32x4 eo = *reinterpret_cast<const f32x4*>(d.eo + sigma(t, 4 * q));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) O[t][e] *= d.eo[32 * (t / 2) + 8 * q + 4 * (t % 2) + e];
+        for (int ct = 0; ct < CT; ++ct) O[ct][t] *= eo;
+      }
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        bf16x8 u[2];
-        if constexpr (DELTA) planes<2>(Uf[2 * s], Uf[2 * s + 1], u);
+        bf16x8 u[CT][2];
+        if constexpr (DELTA) {
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) planes<2>(Uf[ct][2 * s], Uf[ct][2 * s + 1], u[ct]);
+        }
 #pragma unroll
         for (int t = 2 * s; t < 4; ++t) {
           const char* b = P + block_of(t, s) * 1024 + lane * 16;
           const bf16x8 p0 = *reinterpret_cast<const bf16x8*>(b);
           const bf16x8 p1 = *reinterpret_cast<const bf16x8*>(b + kBlocks * 1024);
-          if constexpr (DELTA) {
-            O[t] = mma(p0, u[1], O[t]);
-            O[t] = mma(p1, u[0], O[t]);
-            O[t] = mma(p0, u[0], O[t]);
-          } else {
-            O[t] = mma(p1, v[s], O[t]);
-            O[t] = mma(p0, v[s], O[t]);
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            if constexpr (DELTA) {
+              O[ct][t] = mma(p0, u[ct][1], O[ct][t]);
+              O[ct][t] = mma(p1, u[ct][0], O[ct][t]);
+              O[ct][t] = mma(p0, u[ct][0], O[ct][t]);
+            } else {
+              O[ct][t] = mma(p1, v[ct][s], O[ct][t]);
+              O[ct][t] = mma(p0, v[ct][s], O[ct][t]);
+            }
           }
         }
       }
-      if (in) {
-        uint16_t* ob = a.io.o + (row0 + int64_t(c) * kC) * p.o_tok + h * a.io.o_head + col;
+      const __amdgpu_buffer_rsrc_t ro = w.rows(ob, p.o_tok, dv, c);
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+      for (int t = 0; t < 4; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = 32 * (t / 2) + 8 * q + 4 * (t % 2) + e;
-            if (c * kC + r < len) ob[int64_t(r) * p.o_tok] = __builtin_bit_cast(uint16_t, __bf16(O[t][e]));
-          }
-      }
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+            __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(short, __bf16(O[ct][t][e])), ro, o_off[ct],
+                                                  (32 * (t / 2) + 4 * (t % 2) + e) * p.o_tok * 2, 0);
     }
 
     // the state
-    decay_state<KT>(S, d);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) decay_state<KT>(S[ct], d);
     if constexpr (LOCAL) log2_sum += d.G[kC - 1];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      bf16x8 u[3];
-      f32x4 x0, x1;
+      bf16x8 u[CT][3];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x0[e] = Uf[2 * s][e] * d.er[32 * s + 8 * q + e];
-        x1[e] = Uf[2 * s + 1][e] * d.er[32 * s + 8 * q + 4 + e];
+      for (int ct = 0; ct < CT; ++ct) {
+        float x[8];
+        if constexpr (!DELTA) widen8(v[ct][s], x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          x[e] = (DELTA ? Uf[ct][2 * s + e / 4][e % 4] : x[e]) * d.er[32 * s + 8 * q + e];
+        planes<3>(x, u[ct]);
       }
-      planes<3>(x0, x1, u);
 #pragma unroll
       for (int t = 0; t < KT; ++t) {
-        const bf16x8 k = columns<U>(K, 32 * s, 8 * (t / 2) + t % 2, 2, lane);
-        S[t] = mma(k, u[2], S[t]);
-        S[t] = mma(k, u[1], S[t]);
-        S[t] = mma(k, u[0], S[t]);
+        const bf16x8 k = columns<kStride<U> * 16>(K + k_col, 32 * s, 64 * (t / 2) + 8 * (t % 2));
+#pragma unroll
+        for (int j = 2; j >= 0; --j)
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) S[ct][t] = mma(k, u[ct][j], S[ct][t]);
       }
     }
     lds_barrier();                          // everybody is done with this chunk
@@ -553,18 +1062,17 @@ __global__ __launch_bounds__(64 * NW) void linear_chunk_kernel(ChunkArgs p) {
     }
   }
 
-  float* to = nullptr;
-  if constexpr (LOCAL) {
-    to = p.seg_state + (unit * a.H + h) * int64_t(DK) * dv;
-    if (tid == 0 && cb == 0) p.seg_log2[unit * a.H + h] = log2_sum;
-  } else if (last) {
-    to = slot_state(a, a.dst, i, h, DK);
-  }
-  if (to && in) {
+  float* to = w.end<DELTA, LOCAL>(p, DK);
+  if (LOCAL && tid == 0 && w.cb == 0) p.seg_log2[w.unit * a.H + h] = log2_sum;
+  if (to) {
 #pragma unroll
-    for (int t = 0; t < KT; ++t)
+    for (int ct = 0; ct < CT; ++ct)
+      if (col + 16 * ct < dv) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) to[int64_t(sigma(t, 4 * q + e)) * dv + col] = S[t][e];
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) to[int64_t(sigma(t, 4 * q + e)) * dv + col + 16 * ct] = S[ct][t][e];
+      }
   }
 }
 
@@ -572,6 +1080,8 @@ __global__ __launch_bounds__(64 * NW) void linear_chunk_kernel(ChunkArgs p) {
 
 // Segment j's start: its own from the request's first state, and what the segments before it add.
 // Replaces the segments' sums by their starts; with no output to come, writes the last state.
+constexpr int kAhead = 8;
+
 __global__ __launch_bounds__(256) void linear_join_kernel(ChunkArgs p, int dk, bool finish) {
   const LinearArgs& a = p.a;
   const int64_t per = int64_t(dk) * a.dv;
@@ -584,20 +1094,29 @@ __global__ __launch_bounds__(256) void linear_join_kernel(ChunkArgs p, int dk, b
   const int64_t u0 = first_unit(a, i, len);
   const float* from = slot_state(a, a.src, i, h, dk);
   f32x4 S = from ? *reinterpret_cast<const f32x4*>(from + x) : f32x4{0, 0, 0, 0};
-  for (int j = 0; j < segs; ++j) {
-    const int64_t u = u0 + j;
-    f32x4* at = reinterpret_cast<f32x4*>(p.seg_state + (u * a.H + h) * per + x);
-    const f32x4 add = *at;
-    *at = S;
-    if (j + 1 < segs || finish) {
-      const double end = p.seg_log2[u * a.H + h];
-      const double f = exp2(end);
-      if (end > -0.72) {
-        const float m = float(f - 1.0);
+  const auto at = [&](int j) { return reinterpret_cast<f32x4*>(p.seg_state + ((u0 + j) * a.H + h) * per + x); };
+  for (int j0 = 0; j0 < segs; j0 += kAhead) {       // what kAhead segments add, asked for together
+    f32x4 add[kAhead];
+    double end[kAhead];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) S[e] = fmaf(S[e], m, S[e]) + add[e];
-      } else {
-        S = S * float(f) + add;
+    for (int e = 0; e < kAhead; ++e) {
+      const int j = j0 + e < segs ? j0 + e : segs - 1;
+      add[e] = *at(j);
+      end[e] = p.seg_log2[(u0 + j) * a.H + h];
+    }
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) {
+      const int j = j0 + e;
+      if (j >= segs) break;
+      *at(j) = S;
+      if (j + 1 < segs || finish) {
+        if (end[e] > -0.72) {
+          const float m = expm1f(float(end[e] * 0.6931471805599453));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) S[i] = fmaf(S[i], m, S[i]) + add[e][i];
+        } else {
+          S = S * dasc_wy::ex2(float(end[e])) + add[e];
+        }
       }
     }
   }
@@ -611,124 +1130,190 @@ __global__ __launch_bounds__(256) void linear_join_kernel(ChunkArgs p, int dk, b
 
 constexpr int kTS = 68;                     // floats from row to row of a 64 x 64 matrix in LDS
 
-// 16 x 16 block product on fp32 matrix instructions: c + x y, x and y in LDS, y's rows `ys` apart
-__device__ inline f32x4 block_mul(const float* x, const float* y, int ys, f32x4 c, int lane) {
+// 16 x 16 blocks of a matrix in LDS on fp32 matrix instructions: c + x y
+__device__ inline f32x4 block_mul(const float* x, const float* y, f32x4 c, int lane) {
   const int q = lane / 16, r = lane % 16;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) c = mma32(x[r * kTS + 4 * k + q], y[(4 * k + q) * ys + r], c);
+  for (int k = 0; k < 4; ++k) c = mma32(x[r * kTS + 4 * k + q], y[(4 * k + q) * kTS + r], c);
   return c;
 }
+__device__ inline void block_put(float* x, f32x4 v, int lane) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[(4 * (lane / 16) + e) * kTS + lane % 16] = v[e];
+}
 
-template <int DK, bool OUT>
-__global__ __launch_bounds__(256) void linear_factor_kernel(ChunkArgs p) {
-  constexpr int NW = 4;
-  __shared__ __attribute__((aligned(16))) float A[kC * kTS], T[kC * kTS], W[NW][16 * 20];
-  __shared__ __attribute__((aligned(16))) Decays dec;
-  __shared__ float bt[kC];
+// A wave per chunk and head, four of a block's waves on heads side by side, none waiting for another.
+// A and P have the same decays: both are formed transposed, block (t, s) at a time, whose lane (q, n)
+// holds columns 32 s + 8 q .. + 7 of row sigma(t, n).  A is inverted in place in LDS, in fp32: the
+// diagonal 16 x 16 blocks by substitution, a column per lane, all four at once; then the blocks (1, 0)
+// and (3, 2); then the lower left 32 x 32.
+template <int DK, bool OUT, bool PLANES>
+__global__ __launch_bounds__(256) void linear_factor_kernel(ChunkArgs p, int64_t total) {
+  constexpr int NW = 4, SK = DK / 32;
+  constexpr bool kP = OUT && PLANES;
+  struct Own {
+    float A[kC * kTS];
+    Decays d;
+    float beta[kC];
+  };
+  __shared__ __attribute__((aligned(16))) Own own[NW];
   const LinearArgs& a = p.a;
-  const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, q = lane / 16, n = lane % 16;
-  const int h = blockIdx.x % a.H;
-  const int64_t unit = blockIdx.x / a.H;
-  const int hk = h / a.rep;
-  const int i = unit_request(a, unit, kC);
+  const int wave = uniform(int(threadIdx.x / 64)), lane = threadIdx.x % 64, q = lane / 16, n = lane % 16;
+  const int64_t job = int64_t(blockIdx.x) * NW + wave;
+  if (job >= total) return;
+  const int h = int(job % a.H), hk = h / a.rep;
+  const int64_t unit = p.u0 + job / a.H;
+  const int i = uniform(unit_request(a, unit, kC));
   const Span sp = request_span(a, i);
   const int64_t c = unit - first_unit(a, i, kC);
   if (c < 0 || c * kC >= sp.len) return;
-  const int64_t row0 = sp.begin + c * kC;
-  const int len = sp.len - int(c) * kC;     // tokens from row0 to the request's end
+  const int64_t row0 = uniform(sp.begin + c * kC);
+  const int len = uniform(sp.len - int(c) * kC);   // tokens from row0 to the request's end
+  float* const A = own[wave].A;
+  Decays& d = own[wave].d;
+  float* const beta = own[wave].beta;
+  char* const pk = p.packets + uniform(job * int64_t(kPacket<PLANES>));
 
-  const uint16_t* const kb = a.io.k + row0 * p.k_tok + hk * a.io.k_head;
-  const uint16_t* const qb = OUT ? a.io.q + row0 * p.q_tok + hk * a.io.q_head : nullptr;
-  const auto ku = [&](int r, int u) {
-    r = r < len ? r : len - 1;
-    return *reinterpret_cast<const bf16x8*>(kb + int64_t(r) * p.k_tok + 8 * u);
-  };
-  const auto qu = [&](int r, int u) {
-    r = r < len ? r : len - 1;
-    return *reinterpret_cast<const bf16x8*>(qb + int64_t(r) * p.q_tok + 8 * u);
-  };
-
-  // K K^T, rows 16 wave .., in registers until the decays are there
-  f32x4 kk[4];
-#pragma unroll
-  for (int t = 0; t < 4; ++t) kk[t] = f32x4{0, 0, 0, 0};
-#pragma unroll
-  for (int s = 0; s < DK / 32; ++s) {
-    const bf16x8 x = ku(16 * wave + n, 4 * s + q);
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-      if (t <= wave) kk[t] = mma(x, ku(16 * t + n, 4 * s + q), kk[t]);
-  }
-  if (wave == 0) {
-    const bool on = lane < len;
-    const int64_t r = row0 + lane;
-    bt[lane] = on ? a.io.beta[r * a.io.beta_tok + h * a.io.beta_head] : 0.0f;
-    make_decays(dec, on ? a.io.g[r * a.io.g_tok + h * a.io.g_head] : 0.0f, a.scale, lane);
-  }
-  __syncthreads();
+  const __amdgpu_buffer_rsrc_t rk = chunk_rows(a.io.k + hk * a.io.k_head, p.k_tok, DK, row0, len);
+  bf16x8 k[4][SK];
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int r = 16 * wave + 4 * q + e, s = 16 * t + n;
-      A[r * kTS + s] = s < r ? bt[r] * kk[t][e] * decay_of(dec.G[r], dec.G[s]) : 0.0f;
-      T[r * kTS + s] = 0.0f;
-    }
-  __syncthreads();
+    for (int s = 0; s < SK; ++s)
+      k[t][s] = __builtin_bit_cast(bf16x8, dasc_wy::ldf4(rk, (sigma(0, n) * p.k_tok + 8 * q) * 2,
+                                                         (sigma(t, 0) * p.k_tok + 32 * s) * 2));
+  {
+    const int64_t r = row0 + (lane < len ? lane : len - 1);
+    const float b = a.io.beta[r * a.io.beta_tok + h * a.io.beta_head];
+    const float g = a.io.g[r * a.io.g_tok + h * a.io.g_head];
+    beta[lane] = lane < len ? b : 0.0f;
+    make_decays(d, lane < len ? g : 0.0f, a.scale, lane);
+  }
+  dasc_wy::wave_lds_sync();
 
-  // T = (I + A)^-1: the diagonal blocks by substitution, a column per lane
-  if (lane < 16) {
-    const float* Ad = A + (16 * wave) * kTS + 16 * wave;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    bf16x8 x[SK];
+    if constexpr (kP) {
+      const __amdgpu_buffer_rsrc_t rq = chunk_rows(a.io.q + hk * a.io.q_head, p.q_tok, DK, row0, len);
+#pragma unroll
+      for (int s = 0; s < SK; ++s)
+        x[s] = __builtin_bit_cast(bf16x8, dasc_wy::ldf4(rq, (sigma(0, n) * p.q_tok + 8 * q) * 2,
+                                                        (sigma(t, 0) * p.q_tok + 32 * s) * 2));
+    }
+    const int r = sigma(t, n);
+    const double gr = d.G[r];
+    const float br = beta[r];
+#pragma unroll
+    for (int s = 0; s <= t / 2; ++s) {
+      f32x4 y[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}}, z[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+      for (int kk = 0; kk < SK; ++kk)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          y[j] = mma(k[2 * s + j][kk], k[t][kk], y[j]);
+          if constexpr (kP) z[j] = mma(k[2 * s + j][kk], x[kk], z[j]);
+        }
+      const int c0 = 32 * s + 8 * q;
+      float Pf[8];
+      f32x4 Af[2];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float D = decay_of(gr, d.G[c0 + e]);
+        Af[e / 4][e % 4] = c0 + e < r ? br * D * y[e / 4][e % 4] : 0.0f;
+        if constexpr (kP) Pf[e] = c0 + e <= r ? a.scale * D * z[e / 4][e % 4] : 0.0f;
+      }
+      *reinterpret_cast<f32x4*>(A + r * kTS + c0) = Af[0];
+      *reinterpret_cast<f32x4*>(A + r * kTS + c0 + 4) = Af[1];
+      if constexpr (kP) {
+        bf16x8 hi, lo;
+        dasc_wy::split8(Pf, hi, lo);
+        char* at = pk + kPacketP + block_of(t, s) * 1024 + lane * 16;
+        *reinterpret_cast<bf16x8*>(at) = hi;
+        *reinterpret_cast<bf16x8*>(at + kBlocks * 1024) = lo;
+      }
+    }
+  }
+  dasc_wy::wave_lds_sync();
+
+  const auto block = [&](int x, int y) { return A + 16 * x * kTS + 16 * y; };
+  const f32x4 zero = {0, 0, 0, 0};
+  {
+    float* const D = block(q, q);           // this lane: column n of diagonal block q
     float x[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      float s = r == lane ? 1.0f : 0.0f;
+      float s[4] = {r == n ? 1.0f : 0.0f, 0, 0, 0};
 #pragma unroll
-      for (int j = 0; j < r; ++j) s = fmaf(-Ad[r * kTS + j], x[j], s);
-      x[r] = s;
+      for (int j = 0; j < r; ++j) s[j % 4] = fmaf(-D[r * kTS + j], x[j], s[j % 4]);
+      x[r] = (s[0] + s[1]) + (s[2] + s[3]);
     }
+    dasc_wy::wave_lds_sync();
 #pragma unroll
-    for (int r = 0; r < 16; ++r) T[(16 * wave + r) * kTS + 16 * wave + lane] = x[r];
+    for (int r = 0; r < 16; ++r) D[r * kTS + n] = x[r];
   }
-  __syncthreads();
-  // the blocks below, one diagonal after another: T_ij = -T_ii sum_k A_ik T_kj
+  dasc_wy::wave_lds_sync();
+  {
+    const f32x4 x = block_mul(block(1, 0), block(0, 0), zero, lane), y = block_mul(block(3, 2), block(2, 2), zero, lane);
+    dasc_wy::wave_lds_sync();
+    block_put(block(1, 0), -x, lane);
+    block_put(block(3, 2), -y, lane);
+    dasc_wy::wave_lds_sync();
+    const f32x4 u = block_mul(block(1, 1), block(1, 0), zero, lane), v = block_mul(block(3, 3), block(3, 2), zero, lane);
+    dasc_wy::wave_lds_sync();
+    block_put(block(1, 0), u, lane);
+    block_put(block(3, 2), v, lane);
+    dasc_wy::wave_lds_sync();
+  }
+  {
+    f32x4 x[2][2], y[2][2];
 #pragma unroll
-  for (int d = 1; d < 4; ++d) {
-    if (wave < 4 - d) {
-      const int bi = wave + d, bj = wave;
-      f32x4 x = {0, 0, 0, 0};
-      for (int k = bj; k < bi; ++k) x = block_mul(A + 16 * bi * kTS + 16 * k, T + 16 * k * kTS + 16 * bj, kTS, x, lane);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) W[wave][(4 * q + e) * 20 + n] = -x[e];
-      dasc_wy::wave_lds_sync();
-      x = block_mul(T + 16 * bi * kTS + 16 * bi, W[wave], 20, f32x4{0, 0, 0, 0}, lane);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) T[(16 * bi + 4 * q + e) * kTS + 16 * bj + n] = x[e];
+    for (int r = 0; r < 2; ++r) {
+      x[r][0] = block_mul(block(2 + r, 1), block(1, 0), block_mul(block(2 + r, 0), block(0, 0), zero, lane), lane);
+      x[r][1] = block_mul(block(2 + r, 1), block(1, 1), zero, lane);
     }
-    __syncthreads();
+    dasc_wy::wave_lds_sync();
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) block_put(block(2 + r, j), -x[r][j], lane);
+    dasc_wy::wave_lds_sync();
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      y[0][j] = block_mul(block(2, 2), block(2, j), zero, lane);
+      y[1][j] = block_mul(block(3, 3), block(3, j), block_mul(block(3, 2), block(2, j), zero, lane), lane);
+    }
+    dasc_wy::wave_lds_sync();
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) block_put(block(2 + r, j), y[r][j], lane);
+    dasc_wy::wave_lds_sync();
   }
 
-  char* const pk = p.packets + (unit * a.H + h) * kPacket;
-  for (int b = wave; b < kBlocks; b += NW) {
-    const int t = b < 2 ? b : 2 + (b - 2) / 2, s = b < 2 ? 0 : (b - 2) % 2;
-    const float* row = T + sigma(t, n) * kTS + 32 * s + 8 * q;
-    float x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = row[e] * bt[32 * s + 8 * q + e];
-    bf16x8 pl[3];
-    planes<3>(x, pl);
+  for (int t = 0; t < 4; ++t)
 #pragma unroll
-    for (int j = 0; j < 3; ++j)
-      *reinterpret_cast<bf16x8*>(pk + (j * kBlocks + b) * 1024 + lane * 16) = pl[j];
-  }
-  if constexpr (OUT) {
-    for (int b = wave; b < kBlocks; b += NW) {
-      const int qt = b < 2 ? b : 2 + (b - 2) / 2, s = b < 2 ? 0 : (b - 2) % 2;
-      make_p<DK>(pk + kTBytes, dec.G, a.scale, qt, s, lane, ku, qu);
+    for (int s = 0; s <= t / 2; ++s) {
+      const int c0 = 32 * s + 8 * q;
+      const float* row = A + sigma(t, n) * kTS + c0;
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = row[e] * beta[c0 + e];
+      if constexpr (PLANES) {
+        bf16x8 pl[3];
+        planes<3>(x, pl);
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+          *reinterpret_cast<bf16x8*>(pk + kPacketT + (j * kBlocks + block_of(t, s)) * 1024 + lane * 16) = pl[j];
+      } else {
+        f32x4* f = reinterpret_cast<f32x4*>(pk + kPacketT) + block_of(t, s) * 64 + lane;
+        f[0] = f32x4{x[0], x[1], x[2], x[3]};
+        f[kBlocks * 64] = f32x4{x[4], x[5], x[6], x[7]};
+      }
     }
-  }
-  for (int b = tid; b < int(sizeof(Decays)) / 16; b += 256)
-    reinterpret_cast<u32x4*>(pk + kTBytes + kPBytes)[b] = reinterpret_cast<const u32x4*>(&dec)[b];
+  for (int b = lane; b < int(sizeof(Decays)) / 16; b += 64)
+    reinterpret_cast<u32x4*>(pk)[b] = reinterpret_cast<const u32x4*>(&d)[b];
 }
 
 // ---- launches --------------------------------------------------------------------------------------------
@@ -736,8 +1321,6 @@ __global__ __launch_bounds__(256) void linear_factor_kernel(ChunkArgs p) {
 // Blocks that fill the chip: two on each of 256 CUs
 constexpr int64_t kFill = 512;
 constexpr int kMinSegment = 8;              // chunks of a segment at least: its state costs what 4 chunks do
-
-int waves_of(int dv) { return dv <= 32 ? 2 : dv <= 64 ? 4 : 8; }
 
 // chunks of a segment of the plain rule, 0: requests are not split
 int segment_chunks(const ChunkPlan& c) {
@@ -752,49 +1335,105 @@ int segment_chunks(const ChunkPlan& c) {
 
 int64_t units_of(const ChunkPlan& c, int64_t tokens) { return c.n_tokens / tokens + c.n_req; }
 
-template <int DK, int NW, bool DELTA, bool OUT, bool LOCAL>
-void launch_walk(const ChunkArgs& p, int64_t units, hipStream_t st) {
-  linear_chunk_kernel<DK, NW, DELTA, OUT, LOCAL><<<uint32_t(units * p.a.H * p.col_blocks), 64 * NW, 0, st>>>(p);
+// Column tiles of 16 that a block takes: the fewest that keep the blocks at one per CU, because a chunk
+// takes a block the less time the fewer it has (four waves on one tile share a chunk's work; eight waves
+// of a tile each share its keys).  us per chunk of 64 tokens, dk = dv = 128, delta rule, by heads:
+//     heads              32     64    128    256
+//     1 tile (split)    2.1    3.2    6.6   12.5
+//     2 tiles (split)   2.7    3.1    6.2   11.7
+//     4 tiles (split)   3.9    4.1    4.6    9.1
+//     8 tiles           5.1    5.4    5.8    6.6
+// Segments of a plain rule's request are as many heads; they take whole heads once they fill the chip.
+int tiles_of(int64_t heads, int dv, int most) {
+  int t = 1;
+  while (t < most && heads * ((dv + 16 * t - 1) / (16 * t)) > 256) t *= 2;
+  return t;
 }
 
-template <int DK, int NW>
-void launch_rule(const ChunkPlan& c, ChunkArgs& p, char* ws, hipStream_t st) {
-  const bool out = p.a.io.o;
-  p.col_blocks = (c.dv + 16 * NW - 1) / (16 * NW);
-  if (c.delta) {
-    p.packets = ws;
-    const uint32_t grid = uint32_t(units_of(c, kC) * c.H);
-    if (out) {
-      linear_factor_kernel<DK, true><<<grid, 256, 0, st>>>(p);
-      launch_walk<DK, NW, true, true, false>(p, c.n_req, st);
-    } else {
-      linear_factor_kernel<DK, false><<<grid, 256, 0, st>>>(p);
-      launch_walk<DK, NW, true, false, false>(p, c.n_req, st);
-    }
-    return;
-  }
-  p.seg_chunks = segment_chunks(c);
-  if (p.seg_chunks == 0) {
-    if (out) launch_walk<DK, NW, false, true, false>(p, c.n_req, st);
-    else launch_walk<DK, NW, false, false, false>(p, c.n_req, st);
-    return;
-  }
-  const int64_t units = units_of(c, int64_t(p.seg_chunks) * kC);
-  p.seg_state = reinterpret_cast<float*>(ws);
-  p.seg_log2 = reinterpret_cast<double*>(ws + units * c.H * int64_t(DK) * c.dv * 4);
-  launch_walk<DK, NW, false, false, true>(p, units, st);
-  linear_join_kernel<<<dim3((DK * c.dv + 1023) / 1024, c.H, c.n_req), 256, 0, st>>>(p, DK, !out);
-  if (out) launch_walk<DK, NW, false, true, false>(p, units, st);
+// Units of a window: packets of 1 GiB (270000 tokens of 8 heads) bound the workspace, whatever the
+// length; a longer call takes two launches for each window more.
+constexpr int64_t kWindowBytes = int64_t(1) << 30;
+
+int64_t window_units(const ChunkPlan& c) {
+  const int64_t all = units_of(c, kC), fit = kWindowBytes / (c.H * int64_t(kPacket<true>));
+  return all <= fit ? all : fit > 0 ? fit : 1;
 }
+
+struct Launch {
+  const ChunkPlan& c;
+  ChunkArgs p;
+  int64_t units;
+  hipStream_t st;
+
+  template <int DK, bool DELTA, bool OUT, bool LOCAL>
+  void walk(int tiles) {
+    p.col_blocks = (c.dv + 16 * tiles - 1) / (16 * tiles);
+    const uint32_t grid = uint32_t(units * c.H * p.col_blocks);
+    constexpr int kWhole = DK == 64 ? 4 : 8;
+    if (tiles == kWhole) {
+      linear_columns_kernel<DK, 1, kWhole, DELTA, OUT, LOCAL><<<grid, 64 * kWhole, 0, st>>>(p);
+    } else if constexpr (!LOCAL) {
+      if (tiles == 1) linear_split_kernel<DK, 1, 1, DELTA, OUT><<<grid, 256, 0, st>>>(p);
+      else if (tiles == 2) linear_split_kernel<DK, 1, 2, DELTA, OUT><<<grid, 512, 0, st>>>(p);
+      else if constexpr (DK == 128) linear_split_kernel<DK, 2, 2, DELTA, OUT><<<grid, 512, 0, st>>>(p);
+    }
+  }
+
+  template <int DK>
+  void run(char* ws) {
+    constexpr int kWhole = DK == 64 ? 4 : 8;
+    const bool out = p.a.io.o;
+    if (c.delta) {
+      units = c.n_req;
+      const int tiles = tiles_of(units * c.H, c.dv, kWhole);
+      const int64_t all = units_of(c, kC), step = window_units(c);
+      float* const carry = reinterpret_cast<float*>(ws + step * c.H * kPacket<true>);
+      const int64_t carried = int64_t(c.H) * DK * c.dv;
+      p.packets = ws;
+      for (int64_t u = 0, j = 0; u < all; u += step, ++j) {
+        p.u0 = u;
+        p.u1 = u + step < all ? u + step : all;
+        p.carry_in = carry + (j & 1) * carried;
+        p.carry_out = carry + (1 - (j & 1)) * carried;
+        const int64_t jobs = (p.u1 - p.u0) * c.H;
+        const uint32_t grid = uint32_t((jobs + 3) / 4);
+        if (tiles == kWhole) linear_factor_kernel<DK, false, false><<<grid, 256, 0, st>>>(p, jobs);
+        else if (out) linear_factor_kernel<DK, true, true><<<grid, 256, 0, st>>>(p, jobs);
+        else linear_factor_kernel<DK, false, true><<<grid, 256, 0, st>>>(p, jobs);
+        if (out) walk<DK, true, true, false>(tiles);
+        else walk<DK, true, false, false>(tiles);
+      }
+      return;
+    }
+    p.seg_chunks = segment_chunks(c);
+    if (p.seg_chunks == 0) {
+      units = c.n_req;
+      const int tiles = tiles_of(units * c.H, c.dv, kWhole);
+      if (out) walk<DK, false, true, false>(tiles);
+      else walk<DK, false, false, false>(tiles);
+      return;
+    }
+    units = units_of(c, int64_t(p.seg_chunks) * kC);
+    p.seg_state = reinterpret_cast<float*>(ws);
+    p.seg_log2 = reinterpret_cast<double*>(ws + units * c.H * int64_t(DK) * c.dv * 4);
+    walk<DK, false, false, true>(kWhole);
+    linear_join_kernel<<<dim3((DK * c.dv + 1023) / 1024, c.H, c.n_req), 256, 0, st>>>(p, DK, !out);
+    if (out) walk<DK, false, true, false>(kWhole);
+  }
+};
 
 }  // namespace
 
 bool linear_chunk_supported(const ChunkPlan& c) {
-  return (c.dk == 64 || c.dk == 128) && c.dv % 16 == 0 && c.n_tokens > 0;
+  // (a grid counts threads in 32 bits)
+  return (c.dk == 64 || c.dk == 128) && c.dv % 16 == 0 && c.n_tokens > 0 && int64_t(c.n_req) * c.H <= (1 << 21);
 }
 
 int64_t linear_chunk_workspace(const ChunkPlan& c) {
-  if (c.delta) return units_of(c, kC) * c.H * kPacket;
+  if (c.delta) {
+    const int64_t step = window_units(c), carry = step < units_of(c, kC) ? 2 * int64_t(c.H) * c.dk * c.dv * 4 : 0;
+    return step * c.H * kPacket<true> + carry;
+  }
   const int seg = segment_chunks(c);
   return seg ? units_of(c, int64_t(seg) * kC) * c.H * (int64_t(c.dk) * c.dv * 4 + 8) : 0;
 }
@@ -806,16 +1445,9 @@ void launch_linear_chunks(const ChunkPlan& c, const LinearArgs& a, void* ws, hip
   p.k_tok = int32_t(a.io.k_tok);
   p.v_tok = int32_t(a.io.v_tok);
   p.o_tok = int32_t(a.io.o_tok);
-  char* w = static_cast<char*>(ws);
-  switch (waves_of(c.dv)) {
-#define DASC_WAVES(N)                                        \
-  case N:                                                    \
-    if (c.dk == 64) launch_rule<64, N>(c, p, w, st);         \
-    else launch_rule<128, N>(c, p, w, st);                   \
-    break;
-    DASC_WAVES(2) DASC_WAVES(4) DASC_WAVES(8)
-#undef DASC_WAVES
-  }
+  Launch l{c, p, 0, st};
+  if (c.dk == 64) l.run<64>(static_cast<char*>(ws));
+  else l.run<128>(static_cast<char*>(ws));
 }
 
 }  // namespace dasc

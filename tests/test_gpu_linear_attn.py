@@ -309,3 +309,78 @@ def test_graph_replays():
         torch.cuda.synchronize()
         np.testing.assert_array_equal(o.float().cpu().numpy(), want_o[..., :dv])
         np.testing.assert_array_equal(pool.cpu().numpy()[2:4, 1], want_pool[2:4, 1])
+
+
+@pytest.mark.parametrize("delta", [False, True])
+def test_chunks_beyond_32_bits(delta):
+    """Rows of one prompt spread over more than 2^31 elements, each close enough for the chunked form."""
+    import torch
+
+    H, d, length, stride = 2, 64, 200, 12_000_000
+    sh = D.Shape("gdn", 1, H, H, d, d)
+    announce(f"linear_attn chunks with a token stride of {stride} delta={delta}")
+    flat = torch.empty(stride * length, dtype=torch.bfloat16, device="cuda")
+    part = lambda at: flat.as_strided((length, H, d), (stride, d, 1), at)  # noqa: E731
+    q, k, v, o = (part(j * H * d) for j in range(4))
+    m = make(21, [length], H, H, d, d, delta, L=1)
+    for x, y in zip((q, k, v), views(m, m["qkv"])):
+        x.copy_(y.cuda())
+    pool = m["pool"].cuda()
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    D.dasc_linear_attn(sh, 0, pool, i32(0), i32(1), q, k, v, m["g"].cuda(), o, i32(0, length), length,
+                       beta=None if m["beta"] is None else m["beta"].cuda(), scale=0.3)
+    torch.cuda.synchronize()
+    got = np.full((length, H, d + 4), 7.0, np.float32)
+    got[..., :d] = o.float().cpu().numpy()
+    check(m, [0], [1], (got, pool.cpu().numpy()), layer=0)
+
+
+def test_a_call_in_windows_equals_its_parts():
+    """A delta-rule call whose chunks need more than one window of workspace, a prompt across the
+    border, against two calls that meet in the middle of the prompt: the same chunks, the same bits."""
+    import torch
+
+    H, d, cut, rest = 8, 64, 64 * 2500, 64 * 2600 + 11
+    lens = [100, cut + rest, 0, 77]
+    N = sum(lens)
+    sh = D.Shape("gdn", 1, H, H // 2, d, d)
+    gen = torch.Generator(device="cuda").manual_seed(22)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=gen)  # noqa: E731
+    q = rnd(N, H // 2, d).bfloat16()
+    k = torch.nn.functional.normalize(rnd(N, H // 2, d), dim=-1).bfloat16()
+    v, g, beta = rnd(N, H, d).bfloat16(), -rnd(N, H).abs() * 0.05, torch.sigmoid(rnd(N, H))
+    pool = rnd(8, 1, H, d, d)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    announce(f"linear_attn in windows: {N} tokens x {H} heads")
+    one = D.dasc_linear_attn_workspace_bytes(sh, 4, N, cut + rest, True)
+    assert one < 1.1 * 2 ** 30 < N / 64 * H * 32000      # bounded, and more than one window
+    a, oa = pool.clone(), torch.zeros_like(v)
+    D.dasc_linear_attn(sh, 0, a, i32(0, 1, 2, 3), i32(4, 5, 6, 7), q, k, v, g, oa,
+                       i32(0, 100, 100 + cut + rest, 100 + cut + rest, N), cut + rest, beta=beta)
+    b, ob = pool.clone(), torch.zeros_like(v)
+    at = 100 + cut
+    D.dasc_linear_attn(sh, 0, b, i32(0, 1), i32(4, 5), q[:at], k[:at], v[:at], g[:at], ob[:at], i32(0, 100, at),
+                       cut, beta=beta[:at])
+    D.dasc_linear_attn(sh, 0, b, i32(5, 2, 3), i32(5, 6, 7), q[at:], k[at:], v[at:], g[at:], ob[at:],
+                       i32(0, rest, rest, rest + 77), rest, beta=beta[at:])
+    torch.cuda.synchronize()
+    assert torch.equal(oa, ob) and torch.equal(a, b)
+    assert torch.isfinite(oa.float()).all() and oa[-1].abs().max() > 0
+
+
+def test_rows_that_are_not_apart():
+    """A key repeated over the tokens (stride 0) takes the token-by-token form, with the same rule."""
+    import torch
+
+    m = make(23, [150], 2, 2, 128, 128, True)
+    H, Hqk, dk, dv = m["dims"]
+    q, k, v = (x.clone() for x in views(m, m["qkv"]))
+    m["qkv"][:, Hqk * dk:2 * Hqk * dk] = m["qkv"][0, Hqk * dk:2 * Hqk * dk]
+    pool = m["pool"].cuda()
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    o = torch.full((150, H, dv + 4), 7.0, dtype=torch.bfloat16, device="cuda")
+    D.dasc_linear_attn(D.Shape("gdn", m["L"], H, Hqk, dk, dv), 1, pool, i32(0), i32(1), q.cuda(),
+                       k[:1].cuda().expand(150, Hqk, dk), v.cuda(), m["g"].cuda(), o[..., :dv], i32(0, 150), 150,
+                       beta=m["beta"].cuda(), scale=0.3)
+    torch.cuda.synchronize()
+    check(m, [0], [1], (o.float().cpu().numpy(), pool.cpu().numpy()))
