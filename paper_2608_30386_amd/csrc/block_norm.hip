@@ -4,9 +4,8 @@
 //     x' = x + scale channel_scale b
 //     h  = x' rsqrt(mean(x'^2) + eps) w_pre
 //
-// A row stays in registers from its first load to its last store, on 16, 64, 256 or 1024 lanes
-// with up to four vectors of eight elements each, so every input is read once.  The sums are
-// fp32.
+// A row stays in registers from its first load to its last store, on 16 or 64 lanes or a block of up to
+// 16 waves, so every input is read once.  The sums are fp32.
 
 #include <hip/hip_runtime.h>
 
@@ -22,139 +21,176 @@ namespace {
 
 constexpr int kMaxDim = 32768;
 
-// Sum over the L lanes of a row; every lane gets it.  Rows of more than a wave meet in LDS.
+// Sum over the lanes of a row, 16 or 64 of them or (L = 0) a block's; every lane gets it.  The waves of
+// a block meet in LDS.
 template <int L>
 __device__ inline float row_sum(float x, float* part) {
 #pragma unroll
-  for (int m = 1; m < (L < 64 ? L : 64); m *= 2) x += __shfl_xor(x, m);
-  if constexpr (L > 64) {
-    const int wave = threadIdx.x / 64;
-    if (threadIdx.x % 64 == 0) part[wave] = x;
+  for (int m = 1; m < (L == 16 ? 16 : 64); m *= 2) x += __shfl_xor(x, m);
+  if constexpr (L == 0) {
+    const int waves = blockDim.x / 64;
+    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = x;
     __syncthreads();
     x = 0;
-#pragma unroll
-    for (int i = 0; i < L / 64; ++i) x += part[i];
+    for (int i = 0; i < waves; ++i) x += part[i];
   }
   return x;
 }
 
-template <typename T>
-__device__ inline void weights8(const void* w, bool wide, int c, int n, float (&x)[8]) {
-  if (wide) load8(static_cast<const float*>(w), c, n, x);
-  else load8(static_cast<const T*>(w), c, n, x);
+// 1 / (1 + e^-z) within 2 ulp: the exponent's rounding error, z large, goes back in as a factor.  (The
+// library's exponential and division take some 30 instructions, which bound rows of 128: 57 us for
+// 8192 x 32 of them with a gate.)
+__device__ inline float sigmoid(float z) {
+  const float t = -1.44269504f * z;
+  float r = fmaf(-1.44269504f, z, -t);
+  r = fmaf(-1.92596299e-8f, z, r);                    // log2 e is 1.44269504 + 1.92596299e-8
+  r = fabsf(t) < 126.0f ? r : 0.0f;                  // (past it e is 0 or infinite)
+  const float e = __builtin_amdgcn_exp2f(t);
+  return __builtin_amdgcn_rcpf(fmaf(e, fmaf(0.693147182f, r, 1.0f), 1.0f));
 }
 
-template <typename T, typename X, int L, int NV>
-__global__ __launch_bounds__(L < 256 ? 256 : L) void block_norm_kernel(dasc_norm_io a, int64_t row0, int64_t rows) {
-  constexpr int kRows = L < 256 ? 256 / L : 1;        // rows of a block
-  __shared__ float part[2][L > 64 ? L / 64 : 1];
-  const int lane = threadIdx.x % L;
-  const int64_t row = row0 + int64_t(blockIdx.x) * kRows + threadIdx.x / L;
+// A row on 16 or 64 lanes, or (L = 0) on a block; a lane makes A accesses of VEC elements to each tensor.
+// Everything a row needs is asked for before its first sum.  Rows (i, j) of [outer, inner]; `inner` is
+// divided by as 32-bit numbers.  What lies past the row's end is zero throughout.
+template <typename T, typename X, int L, int A, int VEC>
+__global__ __launch_bounds__(L ? 256 : 1024) void block_norm_kernel(dasc_norm_io a, uint32_t row0, uint32_t rows) {
+  __shared__ float part[2][16];
+  const int lanes = L ? L : blockDim.x;
+  const int lane = L ? threadIdx.x % lanes : threadIdx.x;
+  const uint32_t row = row0 + (L ? blockIdx.x * (256 / lanes) + threadIdx.x / lanes : blockIdx.x);
   if (row >= rows) return;                            // whole rows: no barrier is left waiting
-  const int64_t i = row / a.inner, j = row % a.inner;
+  const int64_t i = a.inner == 1 ? row : row / uint32_t(a.inner), j = a.inner == 1 ? 0 : row % uint32_t(a.inner);
   const int n = a.dim;
   const bool wide = a.w_dtype == DASC_DTYPE_F32;
   const float inv = 1.0f / float(n);
 
-  float x[NV][8];
+  const auto at = [&](int v) { return (v * lanes + lane) * VEC; };   // the column of access v
+  const auto times = [&](const void* w, int v, float (&t)[VEC]) {    // t *= w
+    float f[VEC];
+    if (wide) load_vec<VEC>(static_cast<const float*>(w), at(v), n, f);
+    else load_vec<VEC>(static_cast<const T*>(w), at(v), n, f);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) t[e] *= f[e];
+  };
+
+  float x[A][VEC], gate[A][VEC], res[A][VEC];
   const T* y = static_cast<const T*>(a.y) + i * a.y_out + j * a.y_in;
 #pragma unroll
-  for (int v = 0; v < NV; ++v) load8(y, (v * L + lane) * 8, n, x[v]);
+  for (int v = 0; v < A; ++v) load_vec<VEC>(y, at(v), n, x[v]);
+  if (a.gate) {
+    const T* g = static_cast<const T*>(a.gate) + i * a.gate_out + j * a.gate_in;
+#pragma unroll
+    for (int v = 0; v < A; ++v) load_vec<VEC>(g, at(v), n, gate[v]);
+  }
+  if (a.x) {
+    const X* r = static_cast<const X*>(a.x) + i * a.x_row_out + j * a.x_row_in;
+#pragma unroll
+    for (int v = 0; v < A; ++v) load_vec<VEC>(r, at(v), n, res[v]);
+  }
   float s = a.scale;
   if (a.w_post) {
     float ss = 0;
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+    for (int v = 0; v < A; ++v)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(x[v][e], x[v][e], ss);
-    ss = row_sum<L>(ss, part[0]);
-    s *= 1.0f / sqrtf(ss * inv + a.eps);
+      for (int e = 0; e < VEC; ++e) ss = fmaf(x[v][e], x[v][e], ss);
+    s *= rsqrtf(row_sum<L>(ss, part[0]) * inv + a.eps);
   }
-#pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int c = (v * L + lane) * 8;
-    if (c >= n) continue;
-    float t[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[v][e] *= s;
-    if (a.w_post) {
-      weights8<T>(a.w_post, wide, c, n, t);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[v][e] *= t[e];
-    }
-    if (a.gate) {
-      load8(static_cast<const T*>(a.gate) + i * a.gate_out + j * a.gate_in, c, n, t);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float sig = 1.0f / (1.0f + expf(-t[e]));
-        x[v][e] *= a.act == DASC_ACT_SILU ? t[e] * sig : sig;
-      }
-    }
-    if (a.channel_scale) {
-      weights8<T>(a.channel_scale, wide, c, n, t);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[v][e] *= t[e];
-    }
-    if (a.x) {
-      load8(static_cast<const X*>(a.x) + i * a.x_row_out + j * a.x_row_in, c, n, t);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[v][e] += t[e];
-    }
-    if (a.x_out) store8(static_cast<X*>(a.x_out) + i * a.xo_out + j * a.xo_in, c, n, x[v]);
-  }
-  if (!a.h_out) return;
   float ss = 0;
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    if ((v * L + lane) * 8 >= n) continue;
+  for (int v = 0; v < A; ++v) {
+    if (at(v) >= n) continue;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if ((v * L + lane) * 8 + e < n) ss = fmaf(x[v][e], x[v][e], ss);
+    for (int e = 0; e < VEC; ++e) x[v][e] *= s;
+    if (a.w_post) times(a.w_post, v, x[v]);
+    if (a.gate) {
+      if (a.act == DASC_ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[v][e] *= gate[v][e] * sigmoid(gate[v][e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[v][e] *= sigmoid(gate[v][e]);
+      }
+    }
+    if (a.channel_scale) times(a.channel_scale, v, x[v]);
+    if (a.x) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[v][e] += res[v][e];
+    }
+    if (a.x_out) store_vec<VEC>(static_cast<X*>(a.x_out) + i * a.xo_out + j * a.xo_in, at(v), n, x[v]);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) ss = fmaf(x[v][e], x[v][e], ss);
   }
-  ss = row_sum<L>(ss, part[1]);
-  const float r = 1.0f / sqrtf(ss * inv + a.eps);
+  if (!a.h_out) return;
+  const float r = rsqrtf(row_sum<L>(ss, part[1]) * inv + a.eps);
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int c = (v * L + lane) * 8;
-    if (c >= n) continue;
-    float t[8];
-    weights8<T>(a.w_pre, wide, c, n, t);
+  for (int v = 0; v < A; ++v) {
+    if (at(v) >= n) continue;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) t[e] *= x[v][e] * r;
-    store8(static_cast<T*>(a.h_out) + i * a.h_row_out + j * a.h_row_in, c, n, t);
+    for (int e = 0; e < VEC; ++e) x[v][e] *= r;
+    times(a.w_pre, v, x[v]);
+    store_vec<VEC>(static_cast<T*>(a.h_out) + i * a.h_row_out + j * a.h_row_in, at(v), n, x[v]);
   }
 }
 
 constexpr int64_t kBlocksPerLaunch = int64_t(1) << 21;   // a grid counts threads in 32 bits
 
-template <typename T, typename X, int L, int NV>
-void launch(const dasc_norm_io& a, hipStream_t st) {
-  constexpr int kRows = L < 256 ? 256 / L : 1;
+template <typename T, typename X, int L, int A, int VEC>
+void launch(const dasc_norm_io& a, int threads, hipStream_t st) {
+  constexpr int kRows = L ? 256 / L : 1;
   const int64_t rows = a.outer * a.inner;
   for (int64_t r0 = 0; r0 < rows; r0 += kBlocksPerLaunch * kRows) {
     const int64_t left = rows - r0;
     const int64_t n = left < kBlocksPerLaunch * kRows ? left : kBlocksPerLaunch * kRows;
-    block_norm_kernel<T, X, L, NV><<<uint32_t((n + kRows - 1) / kRows), L < 256 ? 256 : L, 0, st>>>(a, r0, r0 + n);
+    block_norm_kernel<T, X, L, A, VEC><<<uint32_t((n + kRows - 1) / kRows), threads, 0, st>>>(
+        a, uint32_t(r0), uint32_t(r0 + n));
   }
 }
 
+// Whether every row of every tensor starts at a multiple of eight elements
+bool by_eight(const dasc_norm_io& a, int e, int r, int w) {
+  uint64_t bits = 0;
+  const auto add = [&](const void* p, int size, int64_t so, int64_t si) {
+    if (!p) return;
+    bits |= reinterpret_cast<uintptr_t>(p) / size;
+    if (a.outer > 1) bits |= uint64_t(so);
+    if (a.inner > 1) bits |= uint64_t(si);
+  };
+  add(a.y, e, a.y_out, a.y_in);
+  add(a.gate, e, a.gate_out, a.gate_in);
+  add(a.x, r, a.x_row_out, a.x_row_in);
+  add(a.x_out, r, a.xo_out, a.xo_in);
+  add(a.h_out, e, a.h_row_out, a.h_row_in);
+  add(a.w_post, w, 0, 0);
+  add(a.w_pre, w, 0, 0);
+  add(a.channel_scale, w, 0, 0);
+  return bits % 8 == 0;
+}
+
+// The shape of a row, us for 6000 rows of a gated bf16 block and an fp32 residual:
+// - accesses of eight elements where all rows are aligned to that (4096: 77, by four 83), of four where
+//   not (1500: 36.5, by eight 45; 2052: 50.6 and 62; 1999: 52 and 62);
+// - as many waves as there are 512s, and a third access where a little is left over (2050: 50 on four
+//   waves, 55 on five);
+// - rows of up to 128 on 16 lanes, eight elements each.
 template <typename T, typename X>
-void launch_dim(const dasc_norm_io& a, hipStream_t st) {
-  const int n = a.dim;
-  if (n <= 128) launch<T, X, 16, 1>(a, st);
-  else if (n <= 512) launch<T, X, 64, 1>(a, st);
-  else if (n <= 1024) launch<T, X, 64, 2>(a, st);
-  else if (n <= 2048) launch<T, X, 256, 1>(a, st);
-  else if (n <= 4096) launch<T, X, 256, 2>(a, st);
-  else if (n <= 8192) launch<T, X, 256, 4>(a, st);
-  else if (n <= 16384) launch<T, X, 1024, 2>(a, st);
-  else launch<T, X, 1024, 4>(a, st);
+void launch_dim(const dasc_norm_io& a, bool eight, hipStream_t st) {
+  const int n = a.dim, whole = n / 512, over = n % 512;
+  const auto threads = [n](int per) { return (n + 64 * per - 1) / (64 * per) * 64; };
+  if (n <= 128) launch<T, X, 16, 1, 8>(a, 256, st);
+  else if (n <= 512) launch<T, X, 64, 2, 4>(a, 256, st);
+  else if (n <= 1024) launch<T, X, 64, 4, 4>(a, 256, st);
+  else if (eight && n <= 8192) launch<T, X, 0, 1, 8>(a, threads(8), st);
+  else if (over > 0 && over <= 64 * whole && whole <= 16) launch<T, X, 0, 3, 4>(a, 64 * whole, st);
+  else if (n <= 8192) launch<T, X, 0, 2, 4>(a, threads(8), st);
+  else if (n <= 16384) launch<T, X, 0, 4, 4>(a, threads(16), st);
+  else launch<T, X, 0, 8, 4>(a, threads(32), st);
 }
 
 template <typename T>
-void launch_res(const dasc_norm_io& a, hipStream_t st) {
-  if (a.res_dtype == a.dtype) launch_dim<T, T>(a, st);
-  else launch_dim<T, float>(a, st);
+void launch_res(const dasc_norm_io& a, bool eight, hipStream_t st) {
+  if (a.res_dtype == a.dtype) launch_dim<T, T>(a, eight, st);
+  else launch_dim<T, float>(a, eight, st);
 }
 
 bool aligned_to(const void* p, int n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -200,10 +236,11 @@ extern "C" int dasc_block_norm(const dasc_norm_io* io, dasc_stream_t stream) {
   if (a.h_out && !apart(a.h_row_out, a.h_row_in)) return DASC_E_INVAL;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   (void)hipGetLastError();
+  const bool eight = by_eight(a, e, r, w);
   switch (a.dtype) {
-    case DASC_DTYPE_BF16: launch_res<bf16_t>(a, st); break;
-    case DASC_DTYPE_F16: launch_res<f16_t>(a, st); break;
-    default: launch_dim<float, float>(a, st); break;
+    case DASC_DTYPE_BF16: launch_res<bf16_t>(a, eight, st); break;
+    case DASC_DTYPE_F16: launch_res<f16_t>(a, eight, st); break;
+    default: launch_dim<float, float>(a, eight, st); break;
   }
   return launch_status();
 }

@@ -26,18 +26,40 @@ _NORM_IO = struct.Struct("@8P11q6i2f")
 assert _LINEAR_IO.size == C.sizeof(_lib.LinearIo) and _NORM_IO.size == C.sizeof(_lib.NormIo)
 
 
-def _strided(t, dtype, shape, name, dense=True):
-    """Pointer of a strided device tensor of this type and shape, its last dimension contiguous
-    if `dense`.  torch's own strides keep every row inside the tensor's storage."""
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+
+
+def _rows(t, dtype, shape, name, dense=True):
+    """(pointer, first stride, second stride) of a strided device tensor of this type and shape, of
+    two or three dimensions, its last dimension contiguous if `dense`.  torch's own strides keep every
+    row inside the tensor's storage.  Few attribute reads: they are most of a small call's host time."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
-        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
-    if dense and shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
+    s = t.stride()
+    if dense and s[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name}'s last dimension must be contiguous")
-    return t.data_ptr()
+    return t.data_ptr(), s[0], s[1]
+
+
+def _indices(t, n: int, name: str):
+    """Pointer of n int32 indices, or None."""
+    if t is None:
+        return None
+    p = _dev(t, _I32, name)
+    if t.numel() < n:
+        _need(t, n, name)
+    return p
+
+
+def _vector(t, dtype, n: int, name: str):
+    p = _dev(t, dtype, name)
+    if t.shape != (n,):
+        raise ValueError(f"{name} must be [{n}], got {list(t.shape)}")
+    return p
 
 
 def _scratch(need: int, workspace, device, stream):
@@ -77,39 +99,30 @@ def dasc_linear_attn(shape: Shape, layer: int, states, src_slot, dst_slot, q, k,
     """
     n_req = cu_seqlens.numel() - 1
     N, H, Hqk, dk, dv = k.shape[0], shape.n_heads, shape.n_qk_heads, shape.dk, shape.dv
-    _need(states, states.shape[0] * shape.rows * dv, "states")
-    bf, f32, kq, hv, th = torch.bfloat16, torch.float32, (N, Hqk, dk), (N, H, dv), (N, H)
-    pk = _strided(k, bf, kq, "k")
-    pv = _strided(v, bf, hv, "v")
-    pg = _strided(g, f32, th, "g", False)
-    pq = pb = po = None
-    sq = so = (0, 0, 0)
-    sb = (0, 0)
+    kq, hv, th = (N, Hqk, dk), (N, H, dv), (N, H)
+    pk, k0, k1 = _rows(k, _BF16, kq, "k")
+    pv, v0, v1 = _rows(v, _BF16, hv, "v")
+    pg, g0, g1 = _rows(g, _F32, th, "g", False)
+    pq = pb = po = q0 = q1 = b0 = b1 = o0 = o1 = 0
     if o is not None:
-        po, so = _strided(o, bf, hv, "o"), o.stride()
-        pq, sq = _strided(q, bf, kq, "q"), q.stride()
+        po, o0, o1 = _rows(o, _BF16, hv, "o")
+        pq, q0, q1 = _rows(q, _BF16, kq, "q")
     if beta is not None:
-        pb, sb = _strided(beta, f32, th, "beta", False), beta.stride()
-    sk, sv, sg = k.stride(), v.stride(), g.stride()
-    ps = pd = pl = None
-    if src_slot is not None:
-        _need(src_slot, n_req, "src_slot")
-        ps = _dev(src_slot, torch.int32, "src_slot")
-    if dst_slot is not None:
-        _need(dst_slot, n_req, "dst_slot")
-        pd = _dev(dst_slot, torch.int32, "dst_slot")
-    if lens is not None:
-        _need(lens, n_req, "lens")
-        pl = _dev(lens, torch.int32, "lens")
+        pb, b0, b1 = _rows(beta, _F32, th, "beta", False)
+    pc = _dev(cu_seqlens, _I32, "cu_seqlens")
+    n_pool = states.shape[0]
+    if states.numel() < n_pool * shape.rows * dv:
+        _need(states, n_pool * shape.rows * dv, "states")
+    ps = _indices(src_slot, n_req, "src_slot")
+    pd = _indices(dst_slot, n_req, "dst_slot")
+    pl = _indices(lens, n_req, "lens")
     need = (0 if workspace is not None else
             dasc_linear_attn_workspace_bytes(shape, n_req, N, max_len, beta is not None))
-    ws, ws_ptr, ws_bytes = _scratch(need, workspace, states.device, stream)
-    io = _LINEAR_IO.pack(pq or 0, pk, pv, pg, pb or 0, po or 0, sq[0], sq[1], sk[0], sk[1], sv[0], sv[1],
-                         sg[0], sg[1], sb[0], sb[1], so[0], so[1])
+    ws, ws_ptr, ws_bytes = _scratch(need, workspace, k.device if need else None, stream)
+    io = _LINEAR_IO.pack(pq, pk, pv, pg, pb, po, q0, q1, k0, k1, v0, v1, g0, g1, b0, b1, o0, o1)
     _check(LIB.dasc_linear_attn(
-        shape._ref, layer, _dev(states, f32, "states"), states.shape[0], ps, pd, io,
-        _dev(cu_seqlens, torch.int32, "cu_seqlens"), pl, n_req, N, max_len, scale, ws_ptr, ws_bytes,
-        _stream(stream)), "dasc_linear_attn")
+        shape._ref, layer, _dev(states, _F32, "states"), n_pool, ps, pd, io, pc, pl, n_req, N, max_len,
+        scale, ws_ptr, ws_bytes, _stream(stream)), "dasc_linear_attn")
     del ws
 
 
@@ -134,27 +147,24 @@ def dasc_verify_drafts(target, draft_tokens, u_accept, u_sample, out_tokens, n_e
     n_req, m, V = target.shape[0], target.shape[1] - 1, target.shape[2]
     if target.dtype not in DTYPE:
         raise TypeError(f"target must be bfloat16, float16 or float32, got {target.dtype}")
-    pt, stt = _strided(target, target.dtype, (n_req, m + 1, V), "target"), target.stride()
-    pd, sd = None, (0, 0)
+    pt, t0, t1 = _rows(target, target.dtype, (n_req, m + 1, V), "target")
+    pd, d0, d1 = None, 0, 0
     if draft is not None:
-        pd, sd = _strided(draft, target.dtype, (n_req, m, V), "draft"), draft.stride()
-    pn = None
-    if n_draft is not None:
-        _need(n_draft, n_req, "n_draft")
-        pn = _dev(n_draft, torch.int32, "n_draft")
-    _need(draft_tokens, n_req * m, "draft_tokens")
-    _need(u_accept, n_req * m, "u_accept")
-    _need(u_sample, n_req, "u_sample")
-    _need(out_tokens, n_req * (m + 1), "out_tokens")
-    _need(n_emitted, n_req, "n_emitted")
+        pd, d0, d1 = _rows(draft, target.dtype, (n_req, m, V), "draft")
+    pn = _indices(n_draft, n_req, "n_draft")
+    px = _indices(draft_tokens, n_req * m, "draft_tokens")
+    po = _indices(out_tokens, n_req * (m + 1), "out_tokens")
+    pe = _indices(n_emitted, n_req, "n_emitted")
+    pu = _dev(u_accept, _F32, "u_accept")
+    pr = _dev(u_sample, _F32, "u_sample")
+    if u_accept.numel() < n_req * m or u_sample.numel() < n_req:
+        _need(u_accept, n_req * m, "u_accept")
+        _need(u_sample, n_req, "u_sample")
     need = 0 if workspace is not None else dasc_verify_drafts_workspace_bytes(n_req, V)
     ws, ws_ptr, ws_bytes = _scratch(need, workspace, target.device, stream)
     _check(LIB.dasc_verify_drafts(
-        n_req, m, V, DTYPE[target.dtype], pt, stt[0], stt[1], pd, sd[0], sd[1],
-        _dev(draft_tokens, torch.int32, "draft_tokens"), pn, _dev(u_accept, torch.float32, "u_accept"),
-        _dev(u_sample, torch.float32, "u_sample"), _dev(out_tokens, torch.int32, "out_tokens"),
-        _dev(n_emitted, torch.int32, "n_emitted"), ws_ptr, ws_bytes, _stream(stream)),
-        "dasc_verify_drafts")
+        n_req, m, V, DTYPE[target.dtype], pt, t0, t1, pd, d0, d1, px, pn, pu, pr, po, pe, ws_ptr, ws_bytes,
+        _stream(stream)), "dasc_verify_drafts")
     del ws
 
 
@@ -172,31 +182,33 @@ def dasc_block_norm(y, gate=None, act: str = "none", w_post=None, x=None, scale:
         raise TypeError(f"y must be bfloat16, float16 or float32, got {y.dtype}")
     if y.dim() not in (2, 3):
         raise ValueError("y must be [rows, dim] or [outer, inner, dim]")
-    size, dt = y.shape, y.dtype
-    dim = size[-1]
+    size, dt = tuple(y.shape), y.dtype
+    deep, dim = len(size) == 3, size[-1]
+    if dim == 0:
+        raise ValueError("y must have columns")
     res = x if x is not None else x_out
     rdt = dt if res is None else res.dtype
-    if rdt is not dt and rdt is not torch.float32:
+    if rdt is not dt and rdt is not _F32:
         raise TypeError(f"x and x_out must be {dt} or float32, got {rdt}")
-    wdt = None
-    ptrs, strides = [], []
-    for t, d, name in ((y, dt, "y"), (gate, dt, "gate"), (x, rdt, "x"), (x_out, rdt, "x_out"),
-                       (h_out, dt, "h_out")):
-        if t is None:
-            ptrs.append(0)
-            strides += (0, 0)
-            continue
-        ptrs.append(_strided(t, d, size, name))
-        s = t.stride()
-        strides += (s[0], s[1] if len(s) == 3 else 0)
-    for t, name in ((w_post, "w_post"), (w_pre, "w_pre"), (channel_scale, "channel_scale")):
-        if t is None:
-            ptrs.append(0)
-            continue
-        wdt = wdt or t.dtype
-        if wdt is not dt and wdt is not torch.float32:
-            raise TypeError(f"{name} must be {dt} or float32, got {wdt}")
-        ptrs.append(_strided(t, wdt, (dim,), name))
-    io = _NORM_IO.pack(*ptrs, *strides, size[0], size[1] if len(size) == 3 else 1, dim, DTYPE[dt],
-                       DTYPE[rdt], DTYPE[wdt or dt], ACT[act], scale, eps)
+    py, y0, y1 = _rows(y, dt, size, "y")
+    pg = px = pxo = ph = g0 = g1 = x0 = x1 = xo0 = xo1 = h0 = h1 = 0
+    if gate is not None:
+        pg, g0, g1 = _rows(gate, dt, size, "gate")
+    if x is not None:
+        px, x0, x1 = _rows(x, rdt, size, "x")
+    if x_out is not None:
+        pxo, xo0, xo1 = _rows(x_out, rdt, size, "x_out")
+    if h_out is not None:
+        ph, h0, h1 = _rows(h_out, dt, size, "h_out")
+    weights = [t for t in (w_post, w_pre, channel_scale) if t is not None]
+    wdt = weights[0].dtype if weights else dt
+    if wdt is not dt and wdt is not _F32:
+        raise TypeError(f"weights must be {dt} or float32, got {wdt}")
+    pw = [0 if t is None else _vector(t, wdt, dim, name)
+          for t, name in ((w_post, "w_post"), (w_pre, "w_pre"), (channel_scale, "channel_scale"))]
+    if not deep:                           # rows have one stride
+        y1 = g1 = x1 = xo1 = h1 = 0
+    io = _NORM_IO.pack(py, pg, px, pxo, ph, *pw, y0, y1, g0, g1, x0, x1, xo0, xo1, h0, h1, size[0],
+                       size[1] if deep else 1, dim, DTYPE[dt], DTYPE[rdt], DTYPE[wdt], ACT[act], scale,
+                       eps)
     _check(LIB.dasc_block_norm(io, _stream(stream)), "dasc_block_norm")

@@ -70,7 +70,7 @@ def verify_inputs(seed, n, m, V, dtype, with_draft, ragged):
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
-@pytest.mark.parametrize("n,m,V", [(1, 4, 1000), (5, 3, 2048), (7, 0, 37), (3, 7, 2049), (2, 2, 1), (2, 1, 70001),
+@pytest.mark.parametrize("n,m,V", [(1, 4, 1000), (5, 3, 2048), (7, 0, 37), (3, 7, 2049), (2, 2, 1), (2, 1, 70001), (9, 1, 70001),
                                    (9, 300, 5)])
 @pytest.mark.parametrize("with_draft", [False, True])
 def test_verify(n, m, V, dtype, with_draft):

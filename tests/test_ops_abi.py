@@ -98,7 +98,7 @@ def verify(n=1, m=2, V=100, dtype=_lib.DASC_DTYPE_F32, ws=P, ws_bytes=1 << 40, s
 
 def test_verify_argument_errors():
     for bad in (dict(n=-1), dict(m=-1), dict(dtype=3), dict(dtype=-1), dict(strides=(-1, 1, 1, 1)),
-                dict(strides=(1, -1, 1, 1)), dict(strides=(1, 1, -1, 1)), dict(strides=(1, 1, 1, -1)), dict(ws=ODD)):
+                dict(strides=(1, -1, 1, 1)), dict(strides=(1, 1, -1, 1)), dict(strides=(1, 1, 1, -1)), dict(V=100000, ws=ODD)):
         assert verify(**bad) == E.DASC_E_INVAL, bad
     for bad in (dict(V=0), dict(V=(1 << 24) + 1), dict(m=1024)):
         assert verify(**bad) == E.DASC_E_SHAPE, bad
@@ -108,9 +108,9 @@ def test_verify_argument_errors():
     assert verify(draft=ODD) == E.DASC_E_INVAL and verify(count=ODD) == E.DASC_E_INVAL
     assert verify(target=P + 1, dtype=_lib.DASC_DTYPE_BF16) == E.DASC_E_INVAL
     out = C.c_size_t()
-    assert LIB.dasc_verify_drafts_workspace_bytes(3, 5000, C.byref(out)) == E.DASC_OK and out.value > 0
-    assert verify(n=3, V=5000, ws_bytes=out.value - 1) == E.DASC_E_WORKSPACE
-    assert verify(n=3, V=5000, ws=None) == E.DASC_E_WORKSPACE
+    assert LIB.dasc_verify_drafts_workspace_bytes(3, 100000, C.byref(out)) == E.DASC_OK and out.value > 0
+    assert verify(n=3, V=100000, ws_bytes=out.value - 1) == E.DASC_E_WORKSPACE
+    assert verify(n=3, V=100000, ws=None) == E.DASC_E_WORKSPACE
     assert verify(n=0, target=None) == E.DASC_OK
     assert LIB.dasc_verify_drafts_workspace_bytes(3, 0, C.byref(out)) == E.DASC_E_INVAL
     assert LIB.dasc_verify_drafts_workspace_bytes(-1, 5, C.byref(out)) == E.DASC_E_INVAL
