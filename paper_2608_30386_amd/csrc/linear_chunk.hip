@@ -221,17 +221,20 @@ __device__ inline void make_decays(Decays& d, float g, float scale, int lane) {
 // D_ts for s <= t from the running sums
 __device__ inline float decay_of(double gt, double gs) { return dasc_wy::ex2(float(gt - gs)); }
 
-template <int NT>
+// The state's decay.  BRANCH: on the chunk's kind, which is the same in all lanes; without, an
+// instruction more for each element.
+template <bool BRANCH, int NT>
 __device__ inline void decay_state(f32x4 (&S)[NT], const Decays& d) {
   const float m = d.m;
-  if (d.near) {
+  const bool near = d.near;
+  if (BRANCH && !near) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) S[t] *= m;
+  } else {
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) S[t][i] = fmaf(S[t][i], m, S[t][i]);
-  } else {
-#pragma unroll
-    for (int t = 0; t < NT; ++t) S[t] *= m;
+      for (int i = 0; i < 4; ++i) S[t][i] = fmaf(S[t][i], m, BRANCH || near ? S[t][i] : 0.0f);
   }
 }
 
@@ -313,6 +316,21 @@ __device__ inline __amdgpu_buffer_rsrc_t chunk_rows(const uint16_t* base, int to
   return dasc_wy::rsrc(base + row * tok, n ? ((n - 1) * tok + width) * 2 : 0);
 }
 
+// A tensor's chunks, or packets, one after another: a resource for each in turn, of `bytes` until the
+// last chunk's `tail`, then of nothing.  A pointer that moves on costs a chunk four scalar instructions
+// where an address formed anew cost fifteen.
+struct Stream {
+  const char* at;
+  int64_t step;
+  int bytes, tail;
+
+  __device__ inline __amdgpu_buffer_rsrc_t next(int c, int last) {
+    const __amdgpu_buffer_rsrc_t r = dasc_wy::rsrc(at, c < last ? bytes : c == last ? tail : 0);
+    at += step;
+    return r;
+  }
+};
+
 // What a block of either walk works on: a head's request (delta) or segment of one (plain), some columns
 struct Walk {
   int cb, h, i, chunks, len;                // chunks < 0: nothing; len: tokens from row0 to the request's end
@@ -335,12 +353,15 @@ struct Walk {
     return DELTA ? p.carry_out + h * head : nullptr;
   }
 
-  // rows of chunk c of a tensor, which end with the request
-  __device__ inline __amdgpu_buffer_rsrc_t rows(const uint16_t* base, int tok, int width, int c) const {
-    return chunk_rows(base, tok, width, row0 + int64_t(c) * kC, len - c * kC);
+  // the chunks of a tensor, the last of which ends with the request (or the segment), and the packets
+  __device__ inline Stream rows(const uint16_t* base, int tok, int width) const {
+    const int left = len - (chunks - 1) * kC, n = left < kC ? left : kC;
+    return {reinterpret_cast<const char*>(base + row0 * tok), int64_t(kC) * tok * 2, ((kC - 1) * tok + width) * 2,
+            ((n - 1) * tok + width) * 2};
   }
-  __device__ inline const char* packet(const ChunkArgs& p, int c) const {
-    return p.packets + pk0 + (c < chunks ? c : chunks - 1) * pk_step;
+  template <bool PLANES>
+  __device__ inline Stream packets(const ChunkArgs& p) const {
+    return {p.packets + pk0, pk_step, kPacket<PLANES>, kPacket<PLANES>};
   }
   // this lane's log-decay of chunk c, 0 past the request's end
   __device__ inline float gate(const LinearArgs& a, int c) const {
@@ -481,15 +502,21 @@ __global__ __launch_bounds__(256 * NG) void linear_split_kernel(ChunkArgs p) {
     v_off[ct] = in ? (sigma(m, 4 * q) * p.v_tok + col0 + 16 * ct) * 2 : kOutside;
     o_off[ct] = in ? (sigma(m, 4 * q) * p.o_tok + col0 + 16 * ct) * 2 : kOutside;
   }
+  // a packet: the decays by all waves, this wave's blocks (a wave of the earlier tokens has one, and the
+  // other lies outside)
+  constexpr int kLast = int(sizeof(Decays)) / 16 - 1;
+  const int d_off = (tid < kLast ? tid : kLast) * 16;
+  const int b_off[2] = {block_of(m, 0) * 1024 + lane * 16, deep ? block_of(m, 1) * 1024 + lane * 16 : kOutside};
+  const int last = chunks - 1;
+  Stream ks = w.rows(kb, p.k_tok, DK), qs = w.rows(qb, p.q_tok, DK), vs = w.rows(vb, p.v_tok, dv),
+         os = w.rows(ob, p.o_tok, dv), ds = w.packets<true>(p), ts = ds, ps = ds;
+
   const auto load_k = [&](int c) {
-    const __amdgpu_buffer_rsrc_t r = w.rows(kb, p.k_tok, DK, c);
+    const __amdgpu_buffer_rsrc_t r = ks.next(c, last);
 #pragma unroll
     for (int j = 0; j < kPasses; ++j)
       rk[j] = __builtin_bit_cast(u32x4, dasc_wy::ldf4(r, k_off, j * kRows * p.k_tok * 2));
-    if constexpr (DELTA) {
-      constexpr int kLast = int(sizeof(Decays)) / 16 - 1;
-      rd = reinterpret_cast<const u32x4*>(w.packet(p, c))[tid < kLast ? tid : kLast];
-    }
+    if constexpr (DELTA) rd = __builtin_bit_cast(u32x4, dasc_wy::ldf4(ds.next(c, last), d_off, 0));
   };
   const auto put_k = [&](int c) {
     char* K = lds + (DELTA ? (c & 1) * L::kK : 0);
@@ -504,13 +531,13 @@ __global__ __launch_bounds__(256 * NG) void linear_split_kernel(ChunkArgs p) {
   };
   const auto load_q = [&](int c) {
     if constexpr (OUT) {
-      const __amdgpu_buffer_rsrc_t r = w.rows(qb, p.q_tok, DK, c);
+      const __amdgpu_buffer_rsrc_t r = qs.next(c, last);
 #pragma unroll
       for (int s = 0; s < SK; ++s) rq[s] = __builtin_bit_cast(bf16x8, dasc_wy::ldf4(r, q_off, 64 * s));
     }
   };
   const auto load_v = [&](int c) {
-    const __amdgpu_buffer_rsrc_t r = w.rows(vb, p.v_tok, dv, c);
+    const __amdgpu_buffer_rsrc_t r = vs.next(c, last);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -519,22 +546,22 @@ __global__ __launch_bounds__(256 * NG) void linear_split_kernel(ChunkArgs p) {
   };
   const auto load_t = [&](int c) {
     if constexpr (DELTA) {
-      const char* pk = w.packet(p, c) + kPacketT;
+      const __amdgpu_buffer_rsrc_t r = ts.next(c, last);
 #pragma unroll
-      for (int j = 0; j < 3; ++j) {
-        rt[0][j] = get(pk, j * kBlocks + block_of(m, 0), lane);
-        rt[1][j] = get(pk, j * kBlocks + block_of(m, 1), lane);
-      }
+      for (int j = 0; j < 3; ++j)
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          rt[s][j] = __builtin_bit_cast(bf16x8, dasc_wy::ldf4(r, b_off[s], kPacketT + j * kBlocks * 1024));
     }
   };
   const auto load_p = [&](int c) {
     if constexpr (DELTA && OUT) {
-      const char* pk = w.packet(p, c) + kPacketP;
+      const __amdgpu_buffer_rsrc_t r = ps.next(c, last);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        rp[0][j] = get(pk, j * kBlocks + block_of(m, 0), lane);
-        rp[1][j] = get(pk, j * kBlocks + block_of(m, 1), lane);
-      }
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          rp[s][j] = __builtin_bit_cast(bf16x8, dasc_wy::ldf4(r, b_off[s], kPacketP + j * kBlocks * 1024));
     }
   };
   const auto put_s = [&]() {                // the state's planes, for all waves of the column tile
@@ -586,46 +613,51 @@ __global__ __launch_bounds__(256 * NG) void linear_split_kernel(ChunkArgs p) {
     lds_barrier();
   }
 
+  // What the next state does not need (Q S, P U, the output) stands behind what it does: a wave does it
+  // while it would wait for the others.
   for (int c = 0; c < chunks; ++c) {
     const char* const K = lds + (DELTA ? (c & 1) * L::kK : 0);
     const Decays& d = DELTA ? dec[c & 1] : dec[c % 3];
     const bool more = c + 1 < chunks;
     if constexpr (!DELTA) load_v(c + 1);
-    f32x4 O[CT], X[CT];
-    // products with the state: Q S, K S
-    if constexpr (OUT || DELTA) {
+    f32x4 O[CT];
+    bf16x8 sp[CT][SK][L::kSPlanes ? L::kSPlanes : 1];
+    if constexpr (L::kSPlanes > 0) {
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) O[ct] = X[ct] = f32x4{0, 0, 0, 0};
+      for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-      for (int s = 0; s < SK; ++s) {
-        bf16x8 k;
-        if constexpr (DELTA) k = sigma_unit<U>(K, m, n, 4 * s + q);
+        for (int s = 0; s < SK; ++s)
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          const char* sb = lds + L::kS + (tile0 + ct) * L::kSBytes;
-          bf16x8 x[L::kSPlanes];
-#pragma unroll
-          for (int j = 0; j < L::kSPlanes; ++j) x[j] = get(sb, s * L::kSPlanes + j, lane);
-          if constexpr (DELTA) {
-            X[ct] = mma(k, x[2], X[ct]);
-            if constexpr (OUT) O[ct] = mma(rq[s], x[1], O[ct]);
-            X[ct] = mma(k, x[1], X[ct]);
-            if constexpr (OUT) O[ct] = mma(rq[s], x[0], O[ct]);
-            X[ct] = mma(k, x[0], X[ct]);
-          } else {
-            O[ct] = mma(rq[s], x[1], O[ct]);
-            O[ct] = mma(rq[s], x[0], O[ct]);
-          }
-        }
-      }
+          for (int j = 0; j < L::kSPlanes; ++j)
+            sp[ct][s][j] = get(lds + L::kS + (tile0 + ct) * L::kSBytes, s * L::kSPlanes + j, lane);
+    }
+    const auto read_out = [&]() {           // Q S
       if constexpr (OUT) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) O[ct] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < SK; ++s)
+#pragma unroll
+          for (int j = 1; j >= 0; --j)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) O[ct] = mma(rq[s], sp[ct][s][j], O[ct]);
         const f32x4 eo = *reinterpret_cast<const f32x4*>(d.eo + sigma(m, 4 * q));
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) O[ct] *= eo;
       }
-    }
+    };
     if constexpr (DELTA) {
-      load_q(c + 1);
+      f32x4 X[CT];
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) X[ct] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < SK; ++s) {
+        const bf16x8 k = sigma_unit<U>(K, m, n, 4 * s + q);
+#pragma unroll
+        for (int j = 2; j >= 0; --j)
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) X[ct] = mma(k, sp[ct][s][j], X[ct]);
+      }
       const f32x4 ex = *reinterpret_cast<const f32x4*>(d.e + sigma(m, 4 * q));
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
@@ -637,6 +669,8 @@ __global__ __launch_bounds__(256 * NG) void linear_split_kernel(ChunkArgs p) {
         put_half(lds + L::kY + (tile0 + ct) * 6144, m, lane, h3);
       }
       load_v(c + 1);
+      read_out();
+      load_q(c + 1);
       lds_barrier();                        // Y is whole
       const f32x4 er = *reinterpret_cast<const f32x4*>(d.er + sigma(m, 4 * q));
 #pragma unroll
@@ -654,24 +688,50 @@ __global__ __launch_bounds__(256 * NG) void linear_split_kernel(ChunkArgs p) {
             u = mma(rt[s][0], y1, u);
             u = mma(rt[s][0], y0, u);
           }
+        uint2 h3[3];
+        half_planes(u * er, h3);
+        put_half(lds + L::kU + (tile0 + ct) * 6144, m, lane, h3);
         if constexpr (OUT) {
           uint2 h2[2];
           half_planes(u, h2);
           put_half(lds + L::kW + (tile0 + ct) * 4096, m, lane, h2);
         }
-        uint2 h3[3];
-        half_planes(u * er, h3);
-        put_half(lds + L::kU + (tile0 + ct) * 6144, m, lane, h3);
       }
       load_t(c + 1);
       lds_barrier();                        // U is whole
     } else if constexpr (OUT) {
+      read_out();
 #pragma unroll
       for (int s = 0; s < 2; ++s)
         if (s == 0 || deep)
           make_p<DK>(d.G, a.scale, m, s, lane, [&](int x, int u) { return sigma_unit<U>(K, x, n, u); },
                      [&](int kk) { return rq[kk]; }, rp[s][0], rp[s][1]);
       load_q(c + 1);
+    }
+
+    // the state
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) decay_state<false>(S[ct], d);
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int t = 0; t < TW; ++t) {
+        const int tt = TW * m + t;
+        const bf16x8 k = columns<kStride<U> * 16>(K + k_col, 32 * s, 64 * (tt / 2) + 8 * (tt % 2));
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          const char* ub = lds + L::kU + (tile0 + ct) * 6144;
+          S[ct][t] = mma(k, get(ub, 3 * s + 2, lane), S[ct][t]);
+          S[ct][t] = mma(k, get(ub, 3 * s + 1, lane), S[ct][t]);
+          S[ct][t] = mma(k, get(ub, 3 * s, lane), S[ct][t]);
+        }
+      }
+    if constexpr (DELTA) {
+      if (more) {
+        put_s();
+        put_k(c + 1);
+      }
+      load_k(c + 2);
     }
 
     if constexpr (OUT) {
@@ -694,7 +754,7 @@ __global__ __launch_bounds__(256 * NG) void linear_split_kernel(ChunkArgs p) {
           }
       }
       load_p(c + 1);
-      const __amdgpu_buffer_rsrc_t ro = w.rows(ob, p.o_tok, dv, c);
+      const __amdgpu_buffer_rsrc_t ro = os.next(c, last);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -702,36 +762,18 @@ __global__ __launch_bounds__(256 * NG) void linear_split_kernel(ChunkArgs p) {
           __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(short, __bf16(O[ct][e])), ro, o_off[ct],
                                                 e * p.o_tok * 2, 0);
     }
-
-    // the state
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) decay_state<TW>(S[ct], d);
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int t = 0; t < TW; ++t) {
-        const int tt = TW * m + t;
-        const bf16x8 k = columns<kStride<U> * 16>(K + k_col, 32 * s, 64 * (tt / 2) + 8 * (tt % 2));
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          const char* ub = lds + L::kU + (tile0 + ct) * 6144;
-          S[ct][t] = mma(k, get(ub, 3 * s + 2, lane), S[ct][t]);
-          S[ct][t] = mma(k, get(ub, 3 * s + 1, lane), S[ct][t]);
-          S[ct][t] = mma(k, get(ub, 3 * s, lane), S[ct][t]);
-        }
-      }
-    if (more) {
-      if constexpr (!DELTA) {
+    if constexpr (!DELTA) {
+      if (more) {
         lds_barrier();                      // everybody is done with this chunk
         put_v(dec[(c + 1) % 3]);
         if (wave == 0) make_decays(dec[(c + 2) % 3], rg, a.scale, lane);
         rg = w.gate(a, c + 3);
+        put_k(c + 1);
+        put_s();
+        load_k(c + 2);
       }
-      put_k(c + 1);
-      put_s();
-      load_k(c + 2);
-      lds_barrier();
     }
+    lds_barrier();                          // the next chunk's keys and state are whole
   }
 
   float* to = w.end<DELTA, false>(p, DK);
@@ -823,13 +865,16 @@ __global__ __launch_bounds__(64 * NW, (kWavesPerSimd<CT, DELTA, OUT>)) void line
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct)
     o_off[ct] = col + 16 * ct < dv ? (8 * q * p.o_tok + col + 16 * ct) * 2 : kOutside;
+  const int last = chunks - 1;
+  Stream ks = w.rows(kb, p.k_tok, DK), qs = w.rows(qb, p.q_tok, DK), vs = w.rows(vb, p.v_tok, dv),
+         os = w.rows(ob, p.o_tok, dv), ps = w.packets<false>(p);
   const auto load = [&](int c) {
-    const __amdgpu_buffer_rsrc_t k = w.rows(kb, p.k_tok, DK, c), v = w.rows(vb, p.v_tok, dv, c);
+    const __amdgpu_buffer_rsrc_t k = ks.next(c, last), v = vs.next(c, last);
 #pragma unroll
     for (int j = 0; j < kPasses; ++j)
       rk[j] = __builtin_bit_cast(u32x4, dasc_wy::ldf4(k, k_off, j * kRowsPass * p.k_tok * 2));
     if constexpr (OUT) {
-      const __amdgpu_buffer_rsrc_t x = w.rows(qb, p.q_tok, DK, c);
+      const __amdgpu_buffer_rsrc_t x = qs.next(c, last);
 #pragma unroll
       for (int j = 0; j < kPasses; ++j)
         rq[j] = __builtin_bit_cast(u32x4, dasc_wy::ldf4(x, q_off, j * kRowsPass * p.q_tok * 2));
@@ -838,14 +883,12 @@ __global__ __launch_bounds__(64 * NW, (kWavesPerSimd<CT, DELTA, OUT>)) void line
     for (int j = 0; j < kVPasses; ++j)
       rv[j] = __builtin_bit_cast(u32x4, dasc_wy::ldf4(v, v_off, j * kVRows * p.v_tok * 2));
     if constexpr (DELTA) {
-      const char* pk = w.packet(p, c);
-      constexpr int kLast = int(sizeof(Decays)) / 16 - 1;
-      rd = reinterpret_cast<const u32x4*>(pk)[tid < kLast ? tid : kLast];
+      const __amdgpu_buffer_rsrc_t r = ps.next(c, last);
+      rd = __builtin_bit_cast(u32x4, dasc_wy::ldf4(r, tid < int(sizeof(Decays)) / 16 ? tid * 16 : kOutside, 0));
 #pragma unroll
       for (int j = 0; j < kT; ++j) {
-        const int x = j * NT + tid;
-        const f32x4* f = reinterpret_cast<const f32x4*>(pk + kPacketT) + (x < kBlocks * 64 ? x : 0);
-        const f32x4 lo = f[0], hi = f[kBlocks * 64];
+        const int x = j * NT + tid, off = x < kBlocks * 64 ? x * 16 : kOutside;
+        const f32x4 lo = dasc_wy::ldf4(r, off, kPacketT), hi = dasc_wy::ldf4(r, off, kPacketT + kBlocks * 1024);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           rt[j][e] = lo[e];
@@ -1019,7 +1062,7 @@ __global__ __launch_bounds__(64 * NW, (kWavesPerSimd<CT, DELTA, OUT>)) void line
           }
         }
       }
-      const __amdgpu_buffer_rsrc_t ro = w.rows(ob, p.o_tok, dv, c);
+      const __amdgpu_buffer_rsrc_t ro = os.next(c, last);
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -1032,7 +1075,7 @@ __global__ __launch_bounds__(64 * NW, (kWavesPerSimd<CT, DELTA, OUT>)) void line
 
     // the state
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) decay_state<KT>(S[ct], d);
+    for (int ct = 0; ct < CT; ++ct) decay_state<true>(S[ct], d);
     if constexpr (LOCAL) log2_sum += d.G[kC - 1];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
