@@ -161,8 +161,14 @@ void launch_steps(const LinearArgs& a, hipStream_t st) {
   }
 }
 
-// Calls whose longest request has more tokens than this take the chunked form.
-constexpr int kStepTokens = 16;
+// Calls whose longest request has more tokens than this take the chunked form.  Token by token | in
+// chunks, us, dk = dv = 128, 32 heads:
+//     tokens                        4          8         16         32         64
+//     1 request, delta rule      - | -      15 | 16    25 | 16    46 | 17    87 | 19
+//     1 request, plain           - | -      13 |  7    22 |  7    39 |  7    74 |  7
+//     64 requests, delta rule    - | -      93 | 124  139 | 126  231 | 140  415 | 157
+//     64 requests, plain         - | -      89 |  91  129 |  94  208 |  99  364 | 107
+constexpr int kStepTokens = 8;
 
 bool takes_chunks(const ChunkPlan& c) { return c.max_len > kStepTokens && linear_chunk_supported(c); }
 

@@ -58,6 +58,7 @@ struct ChunkArgs {
   float* seg_state;                          // plain: [segments, H, dk, dv]
   double* seg_log2;                          // plain: [segments, H], the decay over a segment
   int32_t seg_chunks;                        // plain: chunks of a segment
+  int32_t seg_each;                          // plain: segments of every request, 0: as many as it has tokens for
   int32_t col_blocks;
 };
 
@@ -70,6 +71,16 @@ __device__ inline int64_t clamp_row(const LinearArgs& a, int i) {
 // cu[i] / len + i: numbers ascend, no two requests share one, and there are at most
 // n_tokens / len + n_req of them.
 __device__ inline int64_t first_unit(const LinearArgs& a, int i, int len) { return clamp_row(a, i) / len + i; }
+
+// A request's segments: numbered as units, or the same number for every request, where the last takes
+// what is left (of a request that is longer than the caller said).
+__device__ inline int64_t first_segment(const ChunkArgs& p, int i) {
+  return p.seg_each ? int64_t(i) * p.seg_each : first_unit(p.a, i, p.seg_chunks * kC);
+}
+__device__ inline int segments(const ChunkArgs& p, int len) {
+  const int seg = p.seg_chunks * kC, n = len > 0 ? (len - 1) / seg + 1 : 1;
+  return p.seg_each && n > p.seg_each ? p.seg_each : n;
+}
 
 // the request that unit u belongs to
 __device__ inline int unit_request(const LinearArgs& a, int64_t u, int len) {
@@ -403,16 +414,16 @@ __device__ inline Walk walk_of(const ChunkArgs& p) {
     }
   } else {
     const int seg = p.seg_chunks;
-    w.i = uniform(unit_request(a, w.unit, seg * kC));
+    w.i = uniform(p.seg_each ? int(w.unit / p.seg_each) : unit_request(a, w.unit, seg * kC));
     sp = request_span(a, w.i);
-    const int64_t j = w.unit - first_unit(a, w.i, seg * kC);
+    const int64_t j = w.unit - first_segment(p, w.i);
     const int all = (sp.len + kC - 1) / kC;
-    if (j < 0 || (j * seg >= all && j > 0)) {
+    if (j < 0 || j >= segments(p, sp.len)) {
       w.chunks = -1;
       return w;
     }
     c0 = int(j) * seg;
-    w.chunks = all - c0 < seg ? all - c0 : seg;
+    w.chunks = all - c0 < seg || j + 1 == p.seg_each ? all - c0 : seg;
     w.last = c0 + w.chunks >= all;
   }
   c0 = uniform(c0);
@@ -1131,10 +1142,8 @@ __global__ __launch_bounds__(256) void linear_join_kernel(ChunkArgs p, int dk, b
   const int64_t x = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;     // dv is a multiple of 4
   if (x >= per) return;
   const int h = blockIdx.y, i = blockIdx.z;
-  const int len = p.seg_chunks * kC;
-  const Span sp = request_span(a, i);
-  const int segs = sp.len > 0 ? (sp.len + len - 1) / len : 1;
-  const int64_t u0 = first_unit(a, i, len);
+  const int segs = segments(p, request_span(a, i).len);
+  const int64_t u0 = first_segment(p, i);
   const float* from = slot_state(a, a.src, i, h, dk);
   f32x4 S = from ? *reinterpret_cast<const f32x4*>(from + x) : f32x4{0, 0, 0, 0};
   const auto at = [&](int j) { return reinterpret_cast<f32x4*>(p.seg_state + ((u0 + j) * a.H + h) * per + x); };
@@ -1361,35 +1370,57 @@ __global__ __launch_bounds__(256) void linear_factor_kernel(ChunkArgs p, int64_t
 
 // ---- launches --------------------------------------------------------------------------------------------
 
-// Blocks that fill the chip: two on each of 256 CUs
-constexpr int64_t kFill = 512;
-constexpr int kMinSegment = 8;              // chunks of a segment at least: its state costs what 4 chunks do
-
-// chunks of a segment of the plain rule, 0: requests are not split
-int segment_chunks(const ChunkPlan& c) {
-  if (c.delta) return 0;
-  const int64_t blocks = int64_t(c.n_req) * c.H * ((c.dv + 127) / 128);
-  if (blocks >= kFill / 2) return 0;
-  const int64_t per = kFill / blocks;       // segments a request can use
-  int64_t chunks = (c.n_tokens / kC / c.n_req + per) / (per > 0 ? per : 1);
-  if (chunks < kMinSegment) chunks = kMinSegment;
-  return c.max_len > 2 * chunks * kC ? int(chunks) : 0;
-}
-
 int64_t units_of(const ChunkPlan& c, int64_t tokens) { return c.n_tokens / tokens + c.n_req; }
+
+constexpr int kCus = 256;                   // blocks that give every CU one
+
+// columns that the walk with a wave per 16 takes in a block
+constexpr int whole_tiles(int dk) { return dk == 64 ? 4 : 8; }
+
+struct Segments {
+  int chunks, each;                         // of a segment, 0: requests are not split; ChunkArgs::seg_each
+  int64_t units;
+};
+
+// Segments of the plain rule's requests, for a block per CU at most: a block more on some CUs makes all
+// wait (two share a CU's matrix units: 9.4 us per chunk against 4.7).  Equal numbers for every request
+// suit requests alike, numbers by length suit others; the shorter segments are taken.  A split request
+// costs 3.2 + 5.6 us per chunk of a segment and some 20 us for two launches more and the join, one that
+// is not 2.2 (32 heads or fewer) or 3.1 us (64) per chunk.  dk = dv = 128, us split | whole:
+//     16384 tokens x 32 heads  265 | 548     4096 x 32  80 | 145     1536 x 32  45 | 53    1024 x 32  40 | 38
+//     16384 x 4                 59 | 470     4096 x 4   40 | 121     1024 x 4   24 | 34     640 x 4   22 | 23
+//     2 of 2048 x 32            80 |  98     2 of 1024 x 32  - | 50
+// The states of 64 segments are joined one after another in 18 us, hence no more.
+constexpr int kMaxSegments = 64;
+
+Segments segments_of(const ChunkPlan& c) {
+  const int64_t cols = 16 * whole_tiles(c.dk), blocks = c.H * ((c.dv + cols - 1) / cols);
+  const int64_t room = kCus / blocks, tokens = c.max_len < c.n_tokens ? c.max_len : c.n_tokens;
+  const int64_t all = (tokens + kC - 1) / kC;
+  if (c.delta || room < 2) return {};
+  const int64_t each = room / c.n_req;      // segments of every request, or numbers by length
+  int64_t seg = each > 0 ? (all + each - 1) / each : all;
+  const int64_t by_length = room > c.n_req ? c.n_tokens / kC / (room - c.n_req) + 1 : all;
+  const bool alike = seg <= by_length;
+  if (!alike) seg = by_length;
+  if (seg < (all + kMaxSegments - 1) / kMaxSegments) seg = (all + kMaxSegments - 1) / kMaxSegments;
+  if (2 * all < 5 * seg + 23) return {};
+  const int64_t n = (all + seg - 1) / seg;
+  return {int(seg), alike ? int(n) : 0, alike ? n * c.n_req : units_of(c, seg * kC)};
+}
 
 // Column tiles of 16 that a block takes: the fewest that keep the blocks at one per CU, because a chunk
 // takes a block the less time the fewer it has (four waves on one tile share a chunk's work; eight waves
 // of a tile each share its keys).  us per chunk of 64 tokens, dk = dv = 128, delta rule, by heads:
 //     heads              32     64    128    256
-//     1 tile (split)    2.1    3.2    6.6   12.5
-//     2 tiles (split)   2.7    3.1    6.2   11.7
-//     4 tiles (split)   3.9    4.1    4.6    9.1
-//     8 tiles           5.1    5.4    5.8    6.6
-// Segments of a plain rule's request are as many heads; they take whole heads once they fill the chip.
+//     1 tile (split)    1.9    3.4    6.7   12.8
+//     2 tiles (split)   2.8    3.3    6.4   12.3
+//     4 tiles (split)   3.8    4.1    5.0    9.3
+//     8 tiles           5.7    5.8    6.0    7.2
+// The plain rule's segments, which fill the chip by themselves, take whole heads.
 int tiles_of(int64_t heads, int dv, int most) {
   int t = 1;
-  while (t < most && heads * ((dv + 16 * t - 1) / (16 * t)) > 256) t *= 2;
+  while (t < most && heads * ((dv + 16 * t - 1) / (16 * t)) > kCus) t *= 2;
   return t;
 }
 
@@ -1412,7 +1443,7 @@ struct Launch {
   void walk(int tiles) {
     p.col_blocks = (c.dv + 16 * tiles - 1) / (16 * tiles);
     const uint32_t grid = uint32_t(units * c.H * p.col_blocks);
-    constexpr int kWhole = DK == 64 ? 4 : 8;
+    constexpr int kWhole = whole_tiles(DK);
     if (tiles == kWhole) {
       linear_columns_kernel<DK, 1, kWhole, DELTA, OUT, LOCAL><<<grid, 64 * kWhole, 0, st>>>(p);
     } else if constexpr (!LOCAL) {
@@ -1424,7 +1455,7 @@ struct Launch {
 
   template <int DK>
   void run(char* ws) {
-    constexpr int kWhole = DK == 64 ? 4 : 8;
+    constexpr int kWhole = whole_tiles(DK);
     const bool out = p.a.io.o;
     if (c.delta) {
       units = c.n_req;
@@ -1448,7 +1479,9 @@ struct Launch {
       }
       return;
     }
-    p.seg_chunks = segment_chunks(c);
+    const Segments g = segments_of(c);
+    p.seg_chunks = g.chunks;
+    p.seg_each = g.each;
     if (p.seg_chunks == 0) {
       units = c.n_req;
       const int tiles = tiles_of(units * c.H, c.dv, kWhole);
@@ -1456,7 +1489,7 @@ struct Launch {
       else walk<DK, false, false, false>(tiles);
       return;
     }
-    units = units_of(c, int64_t(p.seg_chunks) * kC);
+    units = g.units;
     p.seg_state = reinterpret_cast<float*>(ws);
     p.seg_log2 = reinterpret_cast<double*>(ws + units * c.H * int64_t(DK) * c.dv * 4);
     walk<DK, false, false, true>(kWhole);
@@ -1477,8 +1510,7 @@ int64_t linear_chunk_workspace(const ChunkPlan& c) {
     const int64_t step = window_units(c), carry = step < units_of(c, kC) ? 2 * int64_t(c.H) * c.dk * c.dv * 4 : 0;
     return step * c.H * kPacket<true> + carry;
   }
-  const int seg = segment_chunks(c);
-  return seg ? units_of(c, int64_t(seg) * kC) * c.H * (int64_t(c.dk) * c.dv * 4 + 8) : 0;
+  return segments_of(c).units * c.H * (int64_t(c.dk) * c.dv * 4 + 8);
 }
 
 void launch_linear_chunks(const ChunkPlan& c, const LinearArgs& a, void* ws, hipStream_t st) {

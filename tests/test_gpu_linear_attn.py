@@ -202,6 +202,14 @@ def test_long_prompt_split_over_its_length(delta):
     check(m, [0, -1], [2, 3], call(m, [0, -1], [2, 3]))
 
 
+@pytest.mark.parametrize("lens,hint", [([1285, 1280], None), ([2500, 1, 0, 70], None), ([3000], 1300), ([40, 2900], 1300)])
+def test_segments_by_number_and_by_length(lens, hint):
+    """The plain rule's requests split evenly, by length, and where one is longer than the caller said."""
+    m = make(83, lens, 2, 1, 64, 64, False)
+    src, dst = list(range(len(lens))), list(range(len(lens)))
+    check(m, src, dst, call(m, src, dst, max_len=hint))
+
+
 def test_empty_calls():
     import torch
 
