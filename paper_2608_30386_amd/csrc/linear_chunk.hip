@@ -455,20 +455,31 @@ struct Layout {
   static constexpr int kBytes = kD + kDecays * int(sizeof(Decays));
 };
 
+// Whether what the next state does not need (Q S, P U, the output) and the staging of keys is done by
+// waves of their own, as many again, beside those that carry the state.  us per chunk of the delta rule,
+// dk = dv = 128, without | with: 1.94 | 1.70 on 32 heads, 3.37 | 3.00 on 64 (two tiles); dk = dv = 64,
+// 4 heads: 1.39 | 1.04.  With two column tiles a wave there are no registers for them.
+template <int CT, bool DELTA>
+constexpr bool kHelpers = DELTA && CT == 1;
+template <int CT, int NG, bool DELTA>
+constexpr int kSplitThreads = 256 * NG * (kHelpers<CT, DELTA> ? 2 : 1);
+
 // One block walks one request of a head over 16 CT NG columns.
 // Its waves are NG groups of four; a group has CT column tiles, and wave m of it has tokens sigma(m, .)
 // of every product over channels and DK / 4 channels of the state.  What the others need of a wave's
 // part goes through LDS in operand order.
 template <int DK, int CT, int NG, bool DELTA, bool OUT>
-__global__ __launch_bounds__(256 * NG) void linear_split_kernel(ChunkArgs p) {
+__global__ __launch_bounds__((kSplitThreads<CT, NG, DELTA>)) void linear_split_kernel(ChunkArgs p) {
+  constexpr bool HELP = kHelpers<CT, DELTA>;
   constexpr int NT = 256 * NG, U = DK / 8, SK = DK / 32, TW = DK / 64, TILES = CT * NG;
   using L = Layout<DK, TILES, DELTA, OUT>;
   __shared__ __attribute__((aligned(16))) char lds[L::kBytes];
   Decays* const dec = reinterpret_cast<Decays*>(lds + L::kD);
 
   const LinearArgs& a = p.a;
-  const int tid = threadIdx.x, wave = uniform(tid / 64), lane = tid % 64, q = lane / 16, n = lane % 16;
+  const int tid = threadIdx.x % NT, wave = uniform(tid / 64), lane = tid % 64, q = lane / 16, n = lane % 16;
   const int m = wave % 4, grp = wave / 4;
+  const bool helper = HELP && uniform(int(threadIdx.x / NT)) != 0;
   const Walk w = walk_of<DELTA, true>(p);
   if (w.chunks < 0) return;
   const int k_col = key_column<U>(lane);
@@ -479,7 +490,7 @@ __global__ __launch_bounds__(256 * NG) void linear_split_kernel(ChunkArgs p) {
   const int col0 = 16 * (w.cb * TILES + tile0) + n;
   f32x4 S[CT][TW];
   {
-    const float* from = w.start<DELTA, false>(p, DK);
+    const float* from = helper ? nullptr : w.start<DELTA, false>(p, DK);
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
@@ -603,60 +614,126 @@ __global__ __launch_bounds__(256 * NG) void linear_split_kernel(ChunkArgs p) {
     }
   };
 
-  if (chunks > 0) {
-    load_k(0);
-    load_q(0);
-    load_v(0);
-    load_t(0);
-    load_p(0);
-    if constexpr (!DELTA) {
-      if (wave == 0) {
-        make_decays(dec[0], w.gate(a, 0), a.scale, lane);
-        make_decays(dec[1], w.gate(a, 1), a.scale, lane);
-      }
-      rg = w.gate(a, 2);
-      lds_barrier();
-      put_v(dec[0]);
-    }
-    put_k(0);
-    put_s();
-    load_k(1);
-    lds_barrier();
-  }
-
-  // What the next state does not need (Q S, P U, the output) stands behind what it does: a wave does it
-  // while it would wait for the others.
-  for (int c = 0; c < chunks; ++c) {
-    const char* const K = lds + (DELTA ? (c & 1) * L::kK : 0);
-    const Decays& d = DELTA ? dec[c & 1] : dec[c % 3];
-    const bool more = c + 1 < chunks;
-    if constexpr (!DELTA) load_v(c + 1);
-    f32x4 O[CT];
-    bf16x8 sp[CT][SK][L::kSPlanes ? L::kSPlanes : 1];
+  constexpr int SP = L::kSPlanes ? L::kSPlanes : 1;
+  const auto get_s = [&](bf16x8 (&sp)[CT][SK][SP]) {
     if constexpr (L::kSPlanes > 0) {
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
         for (int s = 0; s < SK; ++s)
 #pragma unroll
-          for (int j = 0; j < L::kSPlanes; ++j)
-            sp[ct][s][j] = get(lds + L::kS + (tile0 + ct) * L::kSBytes, s * L::kSPlanes + j, lane);
+          for (int j = 0; j < SP; ++j)
+            sp[ct][s][j] = get(lds + L::kS + (tile0 + ct) * L::kSBytes, s * SP + j, lane);
     }
-    const auto read_out = [&]() {           // Q S
-      if constexpr (OUT) {
+  };
+  f32x4 O[CT];
+  const auto read_out = [&](const bf16x8 (&sp)[CT][SK][SP], const Decays& d) {      // Q S
+    if constexpr (OUT) {
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) O[ct] = f32x4{0, 0, 0, 0};
+      for (int ct = 0; ct < CT; ++ct) O[ct] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int s = 0; s < SK; ++s)
+      for (int s = 0; s < SK; ++s)
 #pragma unroll
-          for (int j = 1; j >= 0; --j)
+        for (int j = 1; j >= 0; --j)
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) O[ct] = mma(rq[s], sp[ct][s][j], O[ct]);
-        const f32x4 eo = *reinterpret_cast<const f32x4*>(d.eo + sigma(m, 4 * q));
+          for (int ct = 0; ct < CT; ++ct) O[ct] = mma(rq[s], sp[ct][s][j], O[ct]);
+      const f32x4 eo = *reinterpret_cast<const f32x4*>(d.eo + sigma(m, 4 * q));
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) O[ct] *= eo;
+      for (int ct = 0; ct < CT; ++ct) O[ct] *= eo;
+    }
+  };
+  const auto write_out = [&](int c) {       // P U, and the output
+    if constexpr (OUT) {
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        const char* wb = lds + L::kW + (tile0 + ct) * (DELTA ? 4096 : 2048);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          if (s == 0 || deep) {
+            if constexpr (DELTA) {
+              const bf16x8 u0 = get(wb, 2 * s, lane), u1 = get(wb, 2 * s + 1, lane);
+              O[ct] = mma(rp[s][0], u1, O[ct]);
+              O[ct] = mma(rp[s][1], u0, O[ct]);
+              O[ct] = mma(rp[s][0], u0, O[ct]);
+            } else {
+              const bf16x8 v = get(wb, s, lane);
+              O[ct] = mma(rp[s][1], v, O[ct]);
+              O[ct] = mma(rp[s][0], v, O[ct]);
+            }
+          }
       }
-    };
+      load_p(c + 1);
+      const __amdgpu_buffer_rsrc_t ro = os.next(c, last);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+          __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(short, __bf16(O[ct][e])), ro, o_off[ct],
+                                                e * p.o_tok * 2, 0);
+    }
+  };
+
+  if constexpr (HELP) {
+    if (helper) {                           // the same three barriers as the state's waves, below
+      if (chunks > 0) {
+        load_k(0);
+        load_q(0);
+        load_p(0);
+        put_k(0);
+        load_k(1);
+        lds_barrier();
+      }
+      for (int c = 0; c < chunks; ++c) {
+        if constexpr (OUT) {
+          bf16x8 sp[CT][SK][SP];
+          get_s(sp);
+          read_out(sp, dec[c & 1]);
+          load_q(c + 1);
+        }
+        lds_barrier();
+        put_k(c + 1);                       // (of nothing after the last chunk)
+        load_k(c + 2);
+        lds_barrier();
+        write_out(c);
+        lds_barrier();
+      }
+      return;
+    }
+  }
+
+  if (chunks > 0) {
+    if constexpr (!HELP) {
+      load_k(0);
+      load_q(0);
+    }
+    load_v(0);
+    load_t(0);
+    if constexpr (!HELP) load_p(0);
+    if constexpr (!DELTA) {
+      if (wave < 2) make_decays(dec[wave], w.gate(a, wave), a.scale, lane);
+      rg = w.gate(a, 2);
+      lds_barrier();
+      put_v(dec[0]);
+    }
+    if constexpr (!HELP) put_k(0);
+    put_s();
+    if constexpr (!HELP) load_k(1);
+    lds_barrier();
+  }
+
+  // Without helpers, what the next state does not need stands behind what it does: a wave does it while
+  // it would wait for the others.
+  for (int c = 0; c < chunks; ++c) {
+    const char* const K = lds + (DELTA ? (c & 1) * L::kK : 0);
+    const Decays& d = DELTA ? dec[c & 1] : dec[c % 3];
+    const bool more = c + 1 < chunks;
+    if constexpr (!DELTA) {
+      load_v(c + 1);
+      if (wave == 0) make_decays(dec[(c + 2) % 3], rg, a.scale, lane);    // (it has one block of P, others two)
+      rg = w.gate(a, c + 3);
+    }
+    bf16x8 sp[CT][SK][SP];
+    get_s(sp);
     if constexpr (DELTA) {
       f32x4 X[CT];
 #pragma unroll
@@ -680,8 +757,10 @@ __global__ __launch_bounds__(256 * NG) void linear_split_kernel(ChunkArgs p) {
         put_half(lds + L::kY + (tile0 + ct) * 6144, m, lane, h3);
       }
       load_v(c + 1);
-      read_out();
-      load_q(c + 1);
+      if constexpr (!HELP) {
+        read_out(sp, d);
+        load_q(c + 1);
+      }
       lds_barrier();                        // Y is whole
       const f32x4 er = *reinterpret_cast<const f32x4*>(d.er + sigma(m, 4 * q));
 #pragma unroll
@@ -711,7 +790,7 @@ __global__ __launch_bounds__(256 * NG) void linear_split_kernel(ChunkArgs p) {
       load_t(c + 1);
       lds_barrier();                        // U is whole
     } else if constexpr (OUT) {
-      read_out();
+      read_out(sp, d);
 #pragma unroll
       for (int s = 0; s < 2; ++s)
         if (s == 0 || deep)
@@ -737,48 +816,20 @@ __global__ __launch_bounds__(256 * NG) void linear_split_kernel(ChunkArgs p) {
           S[ct][t] = mma(k, get(ub, 3 * s, lane), S[ct][t]);
         }
       }
-    if constexpr (DELTA) {
+    if constexpr (HELP) {
+      put_s();                              // (for nobody after the last chunk)
+    } else if constexpr (DELTA) {
       if (more) {
         put_s();
         put_k(c + 1);
       }
       load_k(c + 2);
     }
-
-    if constexpr (OUT) {
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        const char* wb = lds + L::kW + (tile0 + ct) * (DELTA ? 4096 : 2048);
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-          if (s == 0 || deep) {
-            if constexpr (DELTA) {
-              const bf16x8 u0 = get(wb, 2 * s, lane), u1 = get(wb, 2 * s + 1, lane);
-              O[ct] = mma(rp[s][0], u1, O[ct]);
-              O[ct] = mma(rp[s][1], u0, O[ct]);
-              O[ct] = mma(rp[s][0], u0, O[ct]);
-            } else {
-              const bf16x8 v = get(wb, s, lane);
-              O[ct] = mma(rp[s][1], v, O[ct]);
-              O[ct] = mma(rp[s][0], v, O[ct]);
-            }
-          }
-      }
-      load_p(c + 1);
-      const __amdgpu_buffer_rsrc_t ro = os.next(c, last);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-          __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(short, __bf16(O[ct][e])), ro, o_off[ct],
-                                                e * p.o_tok * 2, 0);
-    }
+    if constexpr (!HELP) write_out(c);
     if constexpr (!DELTA) {
       if (more) {
         lds_barrier();                      // everybody is done with this chunk
         put_v(dec[(c + 1) % 3]);
-        if (wave == 0) make_decays(dec[(c + 2) % 3], rg, a.scale, lane);
-        rg = w.gate(a, c + 3);
         put_k(c + 1);
         put_s();
         load_k(c + 2);
@@ -1410,13 +1461,13 @@ Segments segments_of(const ChunkPlan& c) {
 }
 
 // Column tiles of 16 that a block takes: the fewest that keep the blocks at one per CU, because a chunk
-// takes a block the less time the fewer it has (four waves on one tile share a chunk's work; eight waves
+// takes a block the less time the fewer it has (four waves on one tile share a chunk's state; eight waves
 // of a tile each share its keys).  us per chunk of 64 tokens, dk = dv = 128, delta rule, by heads:
 //     heads              32     64    128    256
-//     1 tile (split)    1.9    3.4    6.7   12.8
-//     2 tiles (split)   2.8    3.3    6.4   12.3
-//     4 tiles (split)   3.8    4.1    5.0    9.3
-//     8 tiles           5.7    5.8    6.0    7.2
+//     1 tile (split)    1.7    3.3    6.4   12.3
+//     2 tiles (split)   2.6    3.0    6.1   11.6
+//     4 tiles (split)   3.8    4.0    4.9    9.3
+//     8 tiles           5.7    5.8    6.1    7.5
 // The plain rule's segments, which fill the chip by themselves, take whole heads.
 int tiles_of(int64_t heads, int dv, int most) {
   int t = 1;
@@ -1447,9 +1498,9 @@ struct Launch {
     if (tiles == kWhole) {
       linear_columns_kernel<DK, 1, kWhole, DELTA, OUT, LOCAL><<<grid, 64 * kWhole, 0, st>>>(p);
     } else if constexpr (!LOCAL) {
-      if (tiles == 1) linear_split_kernel<DK, 1, 1, DELTA, OUT><<<grid, 256, 0, st>>>(p);
-      else if (tiles == 2) linear_split_kernel<DK, 1, 2, DELTA, OUT><<<grid, 512, 0, st>>>(p);
-      else if constexpr (DK == 128) linear_split_kernel<DK, 2, 2, DELTA, OUT><<<grid, 512, 0, st>>>(p);
+      if (tiles == 1) linear_split_kernel<DK, 1, 1, DELTA, OUT><<<grid, kSplitThreads<1, 1, DELTA>, 0, st>>>(p);
+      else if (tiles == 2) linear_split_kernel<DK, 1, 2, DELTA, OUT><<<grid, kSplitThreads<1, 2, DELTA>, 0, st>>>(p);
+      else if constexpr (DK == 128) linear_split_kernel<DK, 2, 2, DELTA, OUT><<<grid, kSplitThreads<2, 2, DELTA>, 0, st>>>(p);
     }
   }
 
