@@ -1437,10 +1437,11 @@ struct Segments {
 // wait (two share a CU's matrix units: 9.4 us per chunk against 4.7).  Equal numbers for every request
 // suit requests alike, numbers by length suit others; the shorter segments are taken.  A split request
 // costs 3.2 + 5.6 us per chunk of a segment and some 20 us for two launches more and the join, one that
-// is not 2.2 (32 heads or fewer) or 3.1 us (64) per chunk.  dk = dv = 128, us split | whole:
-//     16384 tokens x 32 heads  265 | 548     4096 x 32  80 | 145     1536 x 32  45 | 53    1024 x 32  40 | 38
-//     16384 x 4                 59 | 470     4096 x 4   40 | 121     1024 x 4   24 | 34     640 x 4   22 | 23
-//     2 of 2048 x 32            80 |  98     2 of 1024 x 32  - | 50
+// is not 1.8 (32 heads or fewer) or 2.7 us (64) per chunk.  us, split | whole:
+//     dk = dv = 128:  4096 tokens x 32 heads  79 | 117    1536 x 32  45 | 48    1024 x 32  40 | 34
+//                     16384 x 4  59 | 405     1024 x 4    24 | 30     640 x 4   22 | 20
+//                     2 of 2048 x 32  80 | 86
+//     dk = dv = 64:   4096 x 16  33 | 91      2048 x 16   25 | 48     1024 x 16  21 | 26
 // The states of 64 segments are joined one after another in 18 us, hence no more.
 constexpr int kMaxSegments = 64;
 
