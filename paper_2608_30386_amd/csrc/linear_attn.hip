@@ -23,10 +23,9 @@ namespace {
 
 using dasc_wy::f32x4;
 
-// R consecutive bf16 (R = 2, 4, 8 or 16), widened
+// R consecutive bf16 (R = 2, 4, 8 or 16), two to a word
 template <int R>
-__device__ inline void load_bf16(const uint16_t* p, float* x) {
-  uint32_t w[R / 2];
+__device__ inline void load_bf16(const uint16_t* p, uint32_t (&w)[R / 2]) {
   if constexpr (R == 2) {
     w[0] = *reinterpret_cast<const uint32_t*>(p);
   } else if constexpr (R == 4) {
@@ -36,8 +35,11 @@ __device__ inline void load_bf16(const uint16_t* p, float* x) {
     for (int i = 0; i < R / 8; ++i)
       reinterpret_cast<uint4*>(w)[i] = reinterpret_cast<const uint4*>(p)[i];
   }
+}
+template <int N>
+__device__ inline void widen(const uint32_t (&w)[N], float (&x)[2 * N]) {
 #pragma unroll
-  for (int i = 0; i < R / 2; ++i) {
+  for (int i = 0; i < N; ++i) {
     x[2 * i] = bf16_lo(w[i]);
     x[2 * i + 1] = bf16_hi(w[i]);
   }
@@ -99,17 +101,32 @@ __global__ __launch_bounds__(256) void linear_steps_kernel(LinearArgs a, int64_t
   for (int r = 0; r < R; ++r)
     S[r] = from && in ? *reinterpret_cast<const f32x4*>(from + at + int64_t(r) * a.dv) : f32x4{0, 0, 0, 0};
 
-  for (int t = 0; t < sp.len; ++t) {
+  struct Token {
+    uint32_t k[R / 2], q[R / 2];
+    uint2 v;
+    float g, beta;
+  };
+  const auto load = [&](int t) {
     const int64_t row = sp.begin + t;
-    decay(S, a.io.g[row * a.io.g_tok + h * a.io.g_head]);
+    Token x;
+    x.g = a.io.g[row * a.io.g_tok + h * a.io.g_head];
+    if (DELTA) x.beta = a.io.beta[row * a.io.beta_tok + h * a.io.beta_head];
+    load_bf16<R>(a.io.k + row * a.io.k_tok + hk * a.io.k_head + rg * R, x.k);
+    if (OUT) load_bf16<R>(a.io.q + row * a.io.q_tok + hk * a.io.q_head + rg * R, x.q);
+    x.v = in ? *reinterpret_cast<const uint2*>(a.io.v + row * a.io.v_tok + h * a.io.v_head + col) : uint2{0, 0};
+    return x;
+  };
+  Token next = {};
+  if (sp.len > 0) next = load(0);
+  for (int t = 0; t < sp.len; ++t) {        // a token is asked for while the one before it is worked on
+    const Token x = next;
+    if (t + 1 < sp.len) next = load(t + 1);
+    const int64_t row = sp.begin + t;
+    decay(S, x.g);
     float k[R], q[R];
-    load_bf16<R>(a.io.k + row * a.io.k_tok + hk * a.io.k_head + rg * R, k);
-    if (OUT) load_bf16<R>(a.io.q + row * a.io.q_tok + hk * a.io.q_head + rg * R, q);
-    f32x4 v = {0, 0, 0, 0};
-    if (in) {
-      const uint2 b = *reinterpret_cast<const uint2*>(a.io.v + row * a.io.v_tok + h * a.io.v_head + col);
-      v = f32x4{bf16_lo(b.x), bf16_hi(b.x), bf16_lo(b.y), bf16_hi(b.y)};
-    }
+    widen(x.k, k);
+    if (OUT) widen(x.q, q);
+    const f32x4 v = {bf16_lo(x.v.x), bf16_hi(x.v.x), bf16_lo(x.v.y), bf16_hi(x.v.y)};
     f32x4 sk = {0, 0, 0, 0}, sq = {0, 0, 0, 0};
     float qk = 0;
 #pragma unroll
@@ -122,9 +139,8 @@ __global__ __launch_bounds__(256) void linear_steps_kernel(LinearArgs a, int64_t
     }
     f32x4 u = v;
     if (DELTA) {
-      const float b = a.io.beta[row * a.io.beta_tok + h * a.io.beta_head];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) u[e] = b * (v[e] - rows_sum(sk[e]));
+      for (int e = 0; e < 4; ++e) u[e] = x.beta * (v[e] - rows_sum(sk[e]));
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) S[r] += u * k[r];
