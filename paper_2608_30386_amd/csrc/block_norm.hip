@@ -6,6 +6,11 @@
 //
 // A row stays in registers from its first load to its last store, on 16 or 64 lanes or a block of up to
 // 16 waves, so every input is read once.  The sums are fp32.
+//
+// HBM bounds it: 8192 x 32 gated rows of 128 in bf16, 201 MB in 50 us (4.0 TB/s); 6001 rows of 2050, a gated
+// bf16 block around an fp32 residual, 172 MB in 51 us (3.4 TB/s); a large copy runs at 4.9.  A block that
+// takes several rows and keeps the weights in registers, which fewer waves then fit into: rows of 128 50 ->
+// 47 us, but 2050 51 -> 64 and 5000 108 -> 121.
 
 #include <hip/hip_runtime.h>
 

@@ -7,6 +7,10 @@
 // 4 cg.. .  The two sums over the rows that a token needs, S~^T k and S~^T q, are formed before
 // the update and summed over the row groups together; o = S~^T q + (q . k) u.  Everything is
 // fp32.
+//
+// A call reads and writes each state once, whatever its tokens, and that bounds it: 128 requests x 32 heads
+// of 128 x 128, a token each, take 101 us, 5.3 TB/s (a large copy runs at 4.9).  Each token more costs 4 us
+// of 64 requests and 1 us of one, the chain of its two sums.
 
 #include "linear_attn.h"
 
@@ -179,12 +183,13 @@ void launch_steps(const LinearArgs& a, hipStream_t st) {
 
 // Calls whose longest request has more tokens than this take the chunked form.  Token by token | in
 // chunks, us, dk = dv = 128, 32 heads:
-//     tokens                        4          8         16         32         64
-//     1 request, delta rule      - | -      15 | 16    25 | 16    46 | 17    87 | 19
-//     1 request, plain           - | -      13 |  7    22 |  7    39 |  7    74 |  7
-//     64 requests, delta rule    - | -      93 | 124  139 | 126  231 | 140  415 | 157
-//     64 requests, plain         - | -      89 |  91  129 |  94  208 |  99  364 | 107
-constexpr int kStepTokens = 8;
+//     tokens                        4          8         12         16         32
+//     1 request, delta rule     9 |  16    14 |  16    18 |  16    22 |  16    39 |  16
+//     1 request, plain          8 |   7    12 |   7    15 |   7    18 |   7    31 |   7
+//     8 requests, delta rule     - | -     18 |  25    23 |  26    27 |  26     - | -
+//     64 requests, delta rule  64 | 122    80 | 122    97 | 125   116 | 128   198 | 139
+//     64 requests, plain       63 |  89    74 |  90    88 |  92   103 |  94   165 |  97
+constexpr int kStepTokens = 12;
 
 bool takes_chunks(const ChunkPlan& c) { return c.max_len > kStepTokens && linear_chunk_supported(c); }
 

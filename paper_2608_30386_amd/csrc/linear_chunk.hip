@@ -17,6 +17,12 @@
 // of the matrix, because lane (q, n) then holds rows 8 q .. 8 q + 7 of each group of 32 in the tiles
 // 2 s and 2 s + 1.  Keys as K^T and values as B operands come from LDS through the transposing read.
 //
+// What bounds it, 32 heads of 128 x 128: few heads, the chain of a chunk, 1.7 us with three exchanges
+// through LDS, of which matrix instructions are a fifth (delta rule, 8192 tokens of one request: 229 us
+// and 50 for the factors); many heads, the issue of matrix and vector instructions, 40% of the time each
+// (8 requests of 777 tokens on average: 145 and 26 us; plain rule, 16384 tokens of one request: 265 us in
+// three launches).  Memory traffic would take 42, 35 and 83 us.
+//
 // Precision.  Keys, queries and values are bf16, products with them are exact.  A 32-bit operand of a
 // sum that reaches the state is cut into three bf16 planes of eight bits each, 24 bits in all, so the
 // state is as good as in fp32 arithmetic (two planes leave 5e-6 of its norm, three 2e-7).  What only
