@@ -239,7 +239,9 @@ __device__ inline void make_decays(Decays& d, float g, float scale, int lane) {
 __device__ inline float decay_of(double gt, double gs) { return dasc_wy::ex2(float(gt - gs)); }
 
 // The state's decay.  BRANCH: on the chunk's kind, which is the same in all lanes; without, an
-// instruction more for each element.
+// instruction more for each element.  (In the split walk a matrix product can stand right before the
+// branch; the compiler then left out the wait between it and the read of its result behind the branch,
+// and outputs of the last chunk were wrong.)
 template <bool BRANCH, int NT>
 __device__ inline void decay_state(f32x4 (&S)[NT], const Decays& d) {
   const float m = d.m;

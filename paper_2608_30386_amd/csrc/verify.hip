@@ -12,7 +12,7 @@
 // its 512 KB at 15 GB/s).
 //
 // Measured: 64 requests x 131071 bf16 tokens, one row of each model: 12.7 + 4.5 us, the 34 MB at 2.6 TB/s; a
-// request of 32003 fp32 tokens 5.2 + 3.4, two chains of dependent loads and a launch.
+// request of 32000 fp32 tokens 5.2 + 3.4, two chains of dependent loads and a launch.
 
 #include <hip/hip_runtime.h>
 
