@@ -1254,6 +1254,7 @@ __device__ inline void block_put(float* x, f32x4 v, int lane) {
 }
 
 // A wave per chunk and head, four of a block's waves on heads side by side, none waiting for another.
+// For the split walk it is bound by the packets it writes: 128 chunks of 32 heads, 217 MB in 52 us, 4.2 TB/s.
 // A and P have the same decays: both are formed transposed, block (t, s) at a time, whose lane (q, n)
 // holds columns 32 s + 8 q .. + 7 of row sigma(t, n).  A is inverted in place in LDS, in fp32: the
 // diagonal 16 x 16 blocks by substitution, a column per lane, all four at once; then the blocks (1, 0)
