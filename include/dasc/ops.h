@@ -78,9 +78,9 @@ int dasc_linear_attn_workspace_bytes(const dasc_shape *shape, int32_t n_req, int
  * and decays in fp32 (running sums of log-decays in 64 bits); keys and queries are taken as
  * they are.
  * Errors: DASC_E_INVAL (NULL shape, states, io or cu_seqlens; k, v or g NULL with n_tokens > 0; q
- * NULL with o given; neither o nor dst_slot given; misalignment or a bad stride; layer out of [0, L), n_req < 1, n_tokens < 0 or
- * above 2^31 - 1, max_len < 0, n_pool < 1, scale not finite), DASC_E_SHAPE (bad shape, dv % 4 != 0),
- * DASC_E_WORKSPACE, DASC_E_UNSUPPORTED (arch KDA, whose decay is by channel; dk not in
+ * NULL with o given; neither o nor dst_slot given; misalignment or a bad stride; layer out of
+ * [0, L), n_req < 1, n_tokens < 0 or above 2^31 - 1, max_len < 0, n_pool < 1, scale not finite),
+ * DASC_E_SHAPE (bad shape, dv % 4 != 0), DASC_E_WORKSPACE, DASC_E_UNSUPPORTED (arch KDA, whose decay is by channel; dk not in
  * {16, 32, 64, 128} or dv > 256), DASC_E_HIP. */
 int dasc_linear_attn(const dasc_shape *shape, int32_t layer, float *states, int64_t n_pool,
                      const int32_t *src_slot, const int32_t *dst_slot, const dasc_linear_io *io,
@@ -110,9 +110,9 @@ int dasc_verify_drafts_workspace_bytes(int32_t n_req, int64_t vocab, size_t *byt
  * The draw is exact: W_v = floor(min(w_v, 1) 2^36) (0 for negative values and NaN),
  * R = floor(u_sample 2^24) clamped to [0, 2^24 - 1], y = the lowest v with
  * W_0 + .. + W_v > floor(R * sum W / 2^24).  Integer sums make it independent of the order in
- * which the row is summed; a probability below 2^-36 is never drawn.  If all weights are 0, w = p_a; if those
- * are too, y = -1.  A drafted token outside [0, vocab) is not accepted.  n_draft is clamped to
- * max_draft; a negative one marks a request to leave out: all its tokens -1, n_emitted 0.
+ * which the row is summed; a probability below 2^-36 is never drawn.  If all weights are 0,
+ * w = p_a; if those are too, y = -1.  A drafted token outside [0, vocab) is not accepted.  n_draft
+ * is clamped to max_draft; a negative one marks a request to leave out: all its tokens -1, n_emitted 0.
  *   target: device [n_req, max_draft + 1, vocab], draft: device [n_req, max_draft, vocab] or
  *     NULL; both of type dtype (DASC_DTYPE_*), rows contiguous, strides of requests and
  *     positions in elements.  Aligned to their element.
@@ -169,8 +169,8 @@ typedef struct dasc_norm_io {
  * outer = 0 is an empty call.
  * Errors: DASC_E_INVAL (NULL io or y, neither x_out nor h_out, h_out without w_pre, a bad
  * dtype, act or stride, a gate without act or the reverse, a pointer not aligned to its element,
- * output rows that overlap, eps < 0, eps or scale not finite), DASC_E_SHAPE (outer < 0, inner or dim < 1,
- * outer * inner above 2^31 - 1), DASC_E_UNSUPPORTED (dim > 32768), DASC_E_HIP. */
+ * output rows that overlap, eps < 0, eps or scale not finite), DASC_E_SHAPE (outer < 0, inner or
+ * dim < 1, outer * inner above 2^31 - 1), DASC_E_UNSUPPORTED (dim > 32768), DASC_E_HIP. */
 int dasc_block_norm(const dasc_norm_io *io, dasc_stream_t stream);
 
 #ifdef __cplusplus
