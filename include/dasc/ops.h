@@ -74,7 +74,9 @@ int dasc_linear_attn_workspace_bytes(const dasc_shape *shape, int32_t n_req, int
  *   workspace: device, at least dasc_linear_attn_workspace_bytes, 16-byte aligned (may be NULL
  *     if that is 0); overlapping calls must not share one.
  * Log-decays may be any value: -inf clears the state, and no product of decays is formed but
- * those the rule has.  Heads that share a key head, values and outputs in bf16, states, sums
+ * those the rule has.  What is not finite stays where the rule has it: an infinity or NaN of a token
+ * reaches its own and later outputs of its request, heads and columns, no others (an infinite query's own
+ * outputs are infinite or NaN).  Heads that share a key head, values and outputs in bf16, states, sums
  * and decays in fp32 (running sums of log-decays in 64 bits); keys and queries are taken as
  * they are.
  * Errors: DASC_E_INVAL (NULL shape, states, io or cu_seqlens; k, v or g NULL with n_tokens > 0; q

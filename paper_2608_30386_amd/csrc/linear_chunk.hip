@@ -23,6 +23,13 @@
 // (8 requests of 777 tokens on average: 145 and 26 us; plain rule, 16384 tokens of one request: 265 us in
 // three launches).  Memory traffic would take 42, 35 and 83 us.
 //
+// What is not finite.  T and P are multiplied a block at a time, the zeros above their diagonals with it, and
+// zero times an infinity or NaN is NaN: one such value, key, state or factor reaches the outputs of tokens
+// before it in its chunk.  It also reaches the state, and a state once NaN or infinite is so to the end.  So
+// a walk looks at the last state of its columns, and where that is not finite takes those columns of the
+// request again token by token, from the source slot, which nothing has written yet; the other columns
+// keep theirs.  (A query that is not finite reaches its own outputs alone.)
+//
 // Precision.  Keys, queries and values are bf16, products with them are exact.  A 32-bit operand of a
 // sum that reaches the state is cut into three bf16 planes of eight bits each, 24 bits in all, so the
 // state is as good as in fp32 arithmetic (two planes leave 5e-6 of its norm, three 2e-7).  What only
@@ -32,9 +39,11 @@
 
 #include <hip/hip_runtime.h>
 
+#include <cstddef>
 #include <cstdint>
 
 #include "launch_common.h"
+#include "linear_steps.h"
 #include "wy_ops.h"
 
 namespace dasc {
@@ -63,6 +72,7 @@ struct ChunkArgs {
   float* carry_out;                          // and of the one that goes on in the next
   float* seg_state;                          // plain: [segments, H, dk, dv]
   double* seg_log2;                          // plain: [segments, H], the decay over a segment
+  int32_t* seg_bad;                          // plain: [requests, H, tiles of 16 columns], see the join
   int32_t seg_chunks;                        // plain: chunks of a segment
   int32_t seg_each;                          // plain: segments of every request, 0: as many as it has tokens for
   int32_t col_blocks;
@@ -257,6 +267,20 @@ __device__ inline void decay_state(f32x4 (&S)[NT], const Decays& d) {
   }
 }
 
+// Whether all of these are finite: zero times anything else is NaN
+template <int N>
+__device__ inline bool finite(const f32x4 (&x)[N]) {
+  float z = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z = fmaf(x[i][e], 0.0f, z);
+  return z == 0.0f;
+}
+
+// the wave's stores are done: what it stores next to the same place comes after them
+__device__ inline void stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // the block's waves see each other's LDS writes; loads from memory stay in flight
 __device__ inline void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
@@ -432,6 +456,7 @@ __device__ inline Walk walk_of(const ChunkArgs& p) {
     }
     c0 = int(j) * seg;
     w.chunks = all - c0 < seg || j + 1 == p.seg_each ? all - c0 : seg;
+    w.first = j == 0;
     w.last = c0 + w.chunks >= all;
   }
   c0 = uniform(c0);
@@ -442,6 +467,36 @@ __device__ inline Walk walk_of(const ChunkArgs& p) {
   w.pk_step = int64_t(a.H) * kPacket<PLANES>;
   return w;
 }
+
+// What only the end of a walk needs is not held in scalar registers over its chunks, which have none to spare
+// (with them the walk of a 32-head layer's prompts takes 160 us, without 143): the call's arguments are read
+// again from where the kernel found them, and the walk's own numbers wait in vector registers.
+__device__ inline ChunkArgs arguments_again() {
+  typedef const __attribute__((address_space(4))) uint32_t* Words;
+  static_assert(sizeof(ChunkArgs) % 4 == 0);
+  uint64_t at = reinterpret_cast<uint64_t>(__builtin_amdgcn_kernarg_segment_ptr());
+  asm volatile("" : "+s"(at));
+  struct { uint32_t w[sizeof(ChunkArgs) / 4]; } words;
+#pragma unroll
+  for (uint32_t i = 0; i < sizeof(ChunkArgs) / 4; ++i) words.w[i] = reinterpret_cast<Words>(at)[i];
+  return __builtin_bit_cast(ChunkArgs, words);
+}
+
+struct Kept {
+  int i, h, cb, ends;
+  int64_t unit;
+
+  __device__ inline explicit Kept(const Walk& w) : i(w.i), h(w.h), cb(w.cb), ends(w.first + 2 * w.last), unit(w.unit) {
+    asm volatile("" : "+v"(i), "+v"(h), "+v"(cb), "+v"(ends), "+v"(unit));
+  }
+  __device__ inline Walk walk() const {
+    Walk w{};
+    w.i = uniform(i), w.h = uniform(h), w.cb = uniform(cb), w.unit = uniform(unit);
+    const int e = uniform(ends);
+    w.first = e & 1, w.last = e & 2;
+    return w;
+  }
+};
 
 constexpr int kOutside = int(0x80000000u);  // an offset past the end of any resource
 
@@ -490,6 +545,7 @@ __global__ __launch_bounds__((kSplitThreads<CT, NG, DELTA>)) void linear_split_k
   const bool helper = HELP && uniform(int(threadIdx.x / NT)) != 0;
   const Walk w = walk_of<DELTA, true>(p);
   if (w.chunks < 0) return;
+  const Kept kept(w);
   const int k_col = key_column<U>(lane);
   const int h = w.h, hk = h / a.rep, dv = a.dv, chunks = w.chunks;
 
@@ -681,8 +737,27 @@ __global__ __launch_bounds__((kSplitThreads<CT, NG, DELTA>)) void linear_split_k
     }
   };
 
+  // Whether the last state of this group's columns, and of any group's, is finite, for every wave of the block
+  int* const verdict = reinterpret_cast<int*>(lds);       // (every wave is past its last read of LDS)
+  const auto vote = [&](bool bad) {
+    if (!helper && lane == 0) verdict[wave] = bad;
+    lds_barrier();
+    int mine = 0, all = 0;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const int x = verdict[4 * g] | verdict[4 * g + 1] | verdict[4 * g + 2] | verdict[4 * g + 3];
+      all |= x;
+      if (g == grp) mine = x;
+    }
+    if (uniform(all)) {                     // outputs will be written again, by another wave
+      stores_done();
+      lds_barrier();
+    }
+    return uniform(mine) != 0;
+  };
+
   if constexpr (HELP) {
-    if (helper) {                           // the same three barriers as the state's waves, below
+    if (helper) {                           // the same barriers as the state's waves, below
       if (chunks > 0) {
         load_k(0);
         load_q(0);
@@ -705,6 +780,7 @@ __global__ __launch_bounds__((kSplitThreads<CT, NG, DELTA>)) void linear_split_k
         write_out(c);
         lds_barrier();
       }
+      if (kept.walk().last) vote(false);
       return;
     }
   }
@@ -846,16 +922,28 @@ __global__ __launch_bounds__((kSplitThreads<CT, NG, DELTA>)) void linear_split_k
     lds_barrier();                          // the next chunk's keys and state are whole
   }
 
-  float* to = w.end<DELTA, false>(p, DK);
+  const ChunkArgs pe = arguments_again();
+  const Walk we = kept.walk();
+  if (we.last) {
+    bool bad = false;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) bad |= !finite(S[ct]);
+    if (vote(__any(bad))) {
+      const int tile = we.cb * TILES + tile0 + m;
+      if (m < CT && 16 * tile < pe.a.dv) walk_tokens<DK, 16, DELTA, OUT>(pe.a, we.i, we.h, 16 * tile, lane);
+      return;
+    }
+  }
+  float* to = we.end<DELTA, false>(pe, DK);
   if (to) {
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
-      if (col0 + 16 * ct < dv) {
+      if (col0 + 16 * ct < pe.a.dv) {
 #pragma unroll
         for (int t = 0; t < TW; ++t)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            to[int64_t(sigma(TW * m + t, 4 * q + e)) * dv + col0 + 16 * ct] = S[ct][t][e];
+            to[int64_t(sigma(TW * m + t, 4 * q + e)) * pe.a.dv + col0 + 16 * ct] = S[ct][t][e];
       }
   }
 }
@@ -896,11 +984,12 @@ __global__ __launch_bounds__(64 * NW, (kWavesPerSimd<CT, DELTA, OUT>)) void line
   const int tid = threadIdx.x, wave = uniform(tid / 64), lane = tid % 64, q = lane / 16, n = lane % 16;
   const Walk w = walk_of<DELTA, false>(p);
   if (w.chunks < 0) return;
+  const Kept kept(w);
   const int k_col = key_column<U>(lane), v_col = value_column<UV>(lane);
   const int h = w.h, hk = h / a.rep, dv = a.dv, chunks = w.chunks;
 
   // the state: lane (q, n) holds channels sigma(t, 4 q + i) of column n of each tile
-  const int col = 16 * CT * (w.cb * NW + wave) + n;
+  const int tile0 = CT * (w.cb * NW + wave), col = 16 * tile0 + n;
   f32x4 S[CT][KT];
   {
     const float* from = w.start<DELTA, LOCAL>(p, DK);
@@ -931,10 +1020,16 @@ __global__ __launch_bounds__(64 * NW, (kWavesPerSimd<CT, DELTA, OUT>)) void line
   const int k_off = (tid / U * p.k_tok + 8 * (tid % U)) * 2;
   const int q_off = (tid / U * p.q_tok + 8 * (tid % U)) * 2;
   const int v_off = vcol < dv ? (tid / UV * p.v_tok + vcol) * 2 : kOutside;
+  // columns that the join found not to be finite: the request's first segment takes them by token
+  bool left[CT];
   int o_off[CT];
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct)
-    o_off[ct] = col + 16 * ct < dv ? (8 * q * p.o_tok + col + 16 * ct) * 2 : kOutside;
+  for (int ct = 0; ct < CT; ++ct) {
+    const bool in = col + 16 * ct < dv;
+    left[ct] = !DELTA && OUT && p.seg_chunks && 16 * (tile0 + ct) < dv &&
+               uniform(p.seg_bad[(int64_t(w.i) * a.H + h) * (dv / 16) + tile0 + ct]) != 0;
+    o_off[ct] = in && !left[ct] ? (8 * q * p.o_tok + col + 16 * ct) * 2 : kOutside;
+  }
   const int last = chunks - 1;
   Stream ks = w.rows(kb, p.k_tok, DK), qs = w.rows(qb, p.q_tok, DK), vs = w.rows(vb, p.v_tok, dv),
          os = w.rows(ob, p.o_tok, dv), ps = w.packets<false>(p);
@@ -1175,35 +1270,49 @@ __global__ __launch_bounds__(64 * NW, (kWavesPerSimd<CT, DELTA, OUT>)) void line
     }
   }
 
-  float* to = w.end<DELTA, LOCAL>(p, DK);
-  if (LOCAL && tid == 0 && w.cb == 0) p.seg_log2[w.unit * a.H + h] = log2_sum;
-  if (to) {
+  const ChunkArgs pe = arguments_again();
+  const Walk we = kept.walk();
+  if (LOCAL && tid == 0 && we.cb == 0) pe.seg_log2[we.unit * pe.a.H + we.h] = log2_sum;
+  float* to = we.end<DELTA, LOCAL>(pe, DK);
+  const bool segment = !DELTA && pe.seg_chunks;
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-      if (col + 16 * ct < dv) {
-#pragma unroll
-        for (int t = 0; t < KT; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) to[int64_t(sigma(t, 4 * q + e)) * dv + col + 16 * ct] = S[ct][t][e];
+  for (int ct = 0; ct < CT; ++ct) {
+    if (!LOCAL && !segment && we.last) left[ct] = __any(!finite(S[ct])) && 16 * (tile0 + ct) < pe.a.dv;
+    if (left[ct]) {
+      if (!segment || we.first) {
+        stores_done();
+        walk_tokens<DK, 16, DELTA, OUT>(pe.a, we.i, we.h, 16 * (tile0 + ct), lane);
       }
+    } else if (to && col + 16 * ct < pe.a.dv) {
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[int64_t(sigma(t, 4 * q + e)) * pe.a.dv + col + 16 * ct] = S[ct][t][e];
+    }
   }
 }
 
 // ---- plain rule: the segments of a request joined ------------------------------------------------------
 
 // Segment j's start: its own from the request's first state, and what the segments before it add.
-// Replaces the segments' sums by their starts; with no output to come, writes the last state.
+// Replaces the segments' sums by their starts; with no output to come, writes the last state.  A block has
+// 16 columns of a head's state, a row on four lanes, so it sees whether all of them are finite to the end:
+// if not, the request's first segment takes them token by token and the others leave them out; with no
+// output to come, this block does.
 constexpr int kAhead = 8;
 
-__global__ __launch_bounds__(256) void linear_join_kernel(ChunkArgs p, int dk, bool finish) {
+template <int DK>
+__global__ __launch_bounds__(4 * DK) void linear_join_kernel(ChunkArgs p, bool finish) {
   const LinearArgs& a = p.a;
-  const int64_t per = int64_t(dk) * a.dv;
-  const int64_t x = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;     // dv is a multiple of 4
-  if (x >= per) return;
-  const int h = blockIdx.y, i = blockIdx.z;
+  const int64_t per = int64_t(DK) * a.dv;
+  // (the tiles of a head side by side on one XCD: two of them share a line)
+  uint32_t bid = blockIdx.x;
+  if (gridDim.x % 8 == 0) bid = bid % 8 * (gridDim.x / 8) + bid / 8;
+  const int tiles = a.dv / 16, tile = bid % tiles, h = bid / tiles % a.H, i = bid / tiles / a.H;
+  const int64_t x = threadIdx.x / 4 * a.dv + 16 * tile + threadIdx.x % 4 * 4;
   const int segs = segments(p, request_span(a, i).len);
   const int64_t u0 = first_segment(p, i);
-  const float* from = slot_state(a, a.src, i, h, dk);
+  const float* from = slot_state(a, a.src, i, h, DK);
   f32x4 S = from ? *reinterpret_cast<const f32x4*>(from + x) : f32x4{0, 0, 0, 0};
   const auto at = [&](int j) { return reinterpret_cast<f32x4*>(p.seg_state + ((u0 + j) * a.H + h) * per + x); };
   for (int j0 = 0; j0 < segs; j0 += kAhead) {       // what kAhead segments add, asked for together
@@ -1220,19 +1329,22 @@ __global__ __launch_bounds__(256) void linear_join_kernel(ChunkArgs p, int dk, b
       const int j = j0 + e;
       if (j >= segs) break;
       *at(j) = S;
-      if (j + 1 < segs || finish) {
-        if (end[e] > -0.72) {
-          const float m = expm1f(float(end[e] * 0.6931471805599453));
+      if (end[e] > -0.72) {
+        const float m = expm1f(float(end[e] * 0.6931471805599453));
 #pragma unroll
-          for (int i = 0; i < 4; ++i) S[i] = fmaf(S[i], m, S[i]) + add[e][i];
-        } else {
-          S = S * dasc_wy::ex2(float(end[e])) + add[e];
-        }
+        for (int i = 0; i < 4; ++i) S[i] = fmaf(S[i], m, S[i]) + add[e][i];
+      } else {
+        S = S * dasc_wy::ex2(float(end[e])) + add[e];
       }
     }
   }
-  if (finish) {
-    float* to = slot_state(a, a.dst, i, h, dk);
+  const bool bad = __syncthreads_or(!finite({S}));
+  if (!finish) {
+    if (threadIdx.x == 0) p.seg_bad[bid] = bad;
+  } else if (bad) {
+    if (threadIdx.x < 64) walk_tokens<DK, 16, false, false>(a, i, h, 16 * tile, threadIdx.x);
+  } else {
+    float* to = slot_state(a, a.dst, i, h, DK);
     if (to) *reinterpret_cast<f32x4*>(to + x) = S;
   }
 }
@@ -1553,8 +1665,9 @@ struct Launch {
     units = g.units;
     p.seg_state = reinterpret_cast<float*>(ws);
     p.seg_log2 = reinterpret_cast<double*>(ws + units * c.H * int64_t(DK) * c.dv * 4);
+    p.seg_bad = reinterpret_cast<int32_t*>(p.seg_log2 + units * c.H);
     walk<DK, false, false, true>(kWhole);
-    linear_join_kernel<<<dim3((DK * c.dv + 1023) / 1024, c.H, c.n_req), 256, 0, st>>>(p, DK, !out);
+    linear_join_kernel<DK><<<uint32_t(c.n_req * c.H * (c.dv / 16)), 4 * DK, 0, st>>>(p, !out);
     if (out) walk<DK, false, true, false>(kWhole);
   }
 };
@@ -1571,7 +1684,8 @@ int64_t linear_chunk_workspace(const ChunkPlan& c) {
     const int64_t step = window_units(c), carry = step < units_of(c, kC) ? 2 * int64_t(c.H) * c.dk * c.dv * 4 : 0;
     return step * c.H * kPacket<true> + carry;
   }
-  return segments_of(c).units * c.H * (int64_t(c.dk) * c.dv * 4 + 8);
+  const int64_t units = segments_of(c).units;
+  return units ? units * c.H * (int64_t(c.dk) * c.dv * 4 + 8) + int64_t(c.n_req) * c.H * (c.dv / 16) * 4 : 0;
 }
 
 void launch_linear_chunks(const ChunkPlan& c, const LinearArgs& a, void* ws, hipStream_t st) {
