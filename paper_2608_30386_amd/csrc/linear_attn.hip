@@ -146,9 +146,11 @@ extern "C" int dasc_linear_attn(const dasc_shape* shape, int32_t layer, float* s
   (void)hipGetLastError();
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   // The chunked form loads 16 bytes of a row at a time and counts the bytes of 64 rows in 31 bits, and
-  // its rows have to lie apart: what is past the last of them reads as zero there.
+  // its rows have to lie apart: what is past the last of them reads as zero there.  It multiplies factors
+  // of up to 2^16 by the scale before anything else.
   const auto apart = [](int64_t tok, int width) { return tok >= width && tok < (int64_t(1) << 24); };
-  const bool wide = io->v_tok % 8 == 0 && io->v_head % 8 == 0 && apart(io->k_tok, dk) && apart(io->v_tok, dv) &&
+  const bool wide = std::fabs(scale) < 0x1p100f && io->v_tok % 8 == 0 && io->v_head % 8 == 0 &&
+                    apart(io->k_tok, dk) && apart(io->v_tok, dv) &&
                     (!io->o || (apart(io->q_tok, dk) && apart(io->o_tok, dv)));
   const dasc::ChunkPlan plan{dk, dv, shape->n_heads, n_req, max_len, n_tokens, io->beta != nullptr};
   if (wide && dasc::takes_chunks(plan)) dasc::launch_linear_chunks(plan, a, workspace, st);

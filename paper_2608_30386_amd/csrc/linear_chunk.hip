@@ -6,9 +6,10 @@
 //     U = V   (plain rule)                   T = (I + A)^-1 Diag(beta),
 //                                            U = T (V - e^G (K S))   (delta rule)
 //     O = scale (e^G (Q S) + P U)            S <- e^{G_C} S + K^T (e^{G_C - G} U)
-// Every exponent is a difference of running sums in the order of the tokens, so no factor of a decay
-// overflows, whatever the log-decays are; the running sums are 64-bit, which keeps the difference
-// of two large ones exact.
+// Every exponent is a difference of running sums in the order of the tokens, so no factor passes the growth
+// over a chunk, one if nothing grows; the running sums are 64-bit, which keeps the difference of two large
+// ones exact.  Log-decays above kGrowth are left to the token-by-token form: over a state of zero their
+// product may pass what fp32 holds, and infinity times zero is NaN.
 //
 // A wave holds the whole state of 16 columns in accumulators and walks over the chunks.  An operand
 // of a matrix instruction is eight consecutive channels or tokens of a lane's row: accumulators chain
@@ -221,10 +222,16 @@ __device__ inline double from_lane(double x) {
   return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
 }
 
+// The most that a token's factor may grow by in chunks, in powers of two: 2^16 over a chunk, far from what
+// fp32 cannot hold.  Beyond it the chunk's decay is NaN, and so the state, which the walk's end finds.
+constexpr double kGrowth = 0.25;
+
 // One wave fills in a chunk's decays, one token per lane; g: the token's log-decay, 0 past the end.
-// A log-decay below -2000 (in powers of two) is as good as -2000: both are a decay of 0.
+// A log-decay below -2000 (in powers of two) is as good as -2000: both are a decay of 0, as is what the
+// rest of the chunk grows it to.
 __device__ inline void make_decays(Decays& d, float g, float scale, int lane) {
   double x = double(g) * 1.4426950408889634;
+  const bool grows = __any(x > kGrowth);
   if (x < -2000.0) x = -2000.0;
   x += from_lane<0x111, 0xF>(x);            // the lanes before it in a row of 16
   x += from_lane<0x112, 0xF>(x);
@@ -240,7 +247,7 @@ __device__ inline void make_decays(Decays& d, float g, float scale, int lane) {
   d.er[lane] = dasc_wy::ex2(float(end - x));
   if (lane == 0) {
     const bool near = end > -0.72;
-    d.m = near ? expm1f(float(end * 0.6931471805599453)) : dasc_wy::ex2(float(end));
+    d.m = grows ? __builtin_nanf("") : near ? expm1f(float(end * 0.6931471805599453)) : dasc_wy::ex2(float(end));
     d.near = near;
   }
 }
@@ -1241,7 +1248,8 @@ __global__ __launch_bounds__(64 * NW, (kWavesPerSimd<CT, DELTA, OUT>)) void line
     // the state
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) decay_state<true>(S[ct], d);
-    if constexpr (LOCAL) log2_sum += d.G[kC - 1];
+    // (what a chunk has cleared no later growth brings back)
+    if constexpr (LOCAL) log2_sum = d.G[kC - 1] < -1000.0 ? -1e30 : log2_sum + d.G[kC - 1];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       bf16x8 u[CT][3];

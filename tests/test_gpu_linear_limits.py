@@ -1,4 +1,4 @@
-"""dasc_linear_attn where its inputs are not finite: what a token may not reach (GPU).
+"""dasc_linear_attn where its inputs are not finite, or its decays grow: what a token may not reach (GPU).
 
 The chunked form multiplies whole blocks of a triangular matrix, zeros among them, and zero times an
 infinity is NaN: a token's NaN or infinity must still not reach the tokens before it, other columns or
@@ -13,7 +13,7 @@ import math
 import numpy as np
 import pytest
 
-from tests.test_gpu_linear_attn import call, make, views
+from tests.test_gpu_linear_attn import call, check, make, views
 from tests.test_gpu_linear_tiles import FULL, H, HQK, WALKS, lengths
 
 pytestmark = pytest.mark.gpu
@@ -166,3 +166,70 @@ def test_windows():
     assert torch.equal(p0[0], p1[0])
     fin = torch.isfinite(p1[1, 0])
     assert (~fin).sum() == d and (p1[1, 0][fin] - p0[1, 0][fin]).abs().max() < 1e-4 * p0[1].abs().max()
+
+
+@pytest.mark.parametrize("delta", [False, True])
+@pytest.mark.parametrize("dk,dv,n", FULL)
+def test_growth_over_a_state_of_zero(dk, dv, n, delta):
+    """Log-decays that sum to more than fp32's exponential holds, over a state that is zero until late."""
+    lens = [max(1, x) for x in lengths(n)]
+    m = make(340 + dk + n, lens, H, HQK, dk, dv, delta)
+    at = 0
+    for x in lens:
+        m["g"][at:at + x] = 1.5
+        late = at + max(0, x - 9)
+        m["qkv"][at:late, 2 * HQK * dk:2 * HQK * dk + H * dv] = 0
+        at += x
+    dst = list(range(n))
+    got = call(m, None, dst)
+    assert np.isfinite(got[0]).all() and np.isfinite(got[1]).all()
+    same(m, got, call(m, None, dst, max_len=0))
+    if n < 12:
+        check(m, None, dst, got)
+
+
+def test_growth_over_a_segment():
+    """A decay over a segment that fp32 does not hold, over a state of zero: 60 chunks of 64 heads go in
+    segments of 15, each of a growth of e^96."""
+    heads, n = 64, 3840
+    m = make(350, [n], heads, heads, 64, 64, False)
+    m["g"][:] = 0.1
+    m["g"][n - 50:] = -0.01
+    m["qkv"][:n - 50, 2 * heads * 64:] = 0
+    for out in (True, False):
+        got = call(m, None, [1], out=out)
+        assert np.isfinite(got[1]).all() and (not out or np.isfinite(got[0]).all())
+        same(m, got, call(m, None, [1], max_len=0, out=out))
+
+
+@pytest.mark.parametrize("delta", [False, True])
+def test_a_scale_near_the_largest_number(delta):
+    """Times a factor that grows a little it would pass fp32; over values of zero the outputs are zero."""
+    m = make(351, [100, 30], 2, 1, 64, 64, delta)
+    m["g"][:] = 0.1
+    m["qkv"][:, 2 * 64:2 * 64 + 2 * 64] = 0
+    check(m, None, [0, 1], call(m, None, [0, 1], scale=3e38), scale=3e38)
+
+
+def test_growth_after_a_reset():
+    """A segment of 127 chunks that begins with a reset and then grows, over values of zero, by as much as
+    the kernels let a reset shrink: the reset holds."""
+    import torch
+
+    import paper_2608_30386_amd as D
+    from tests.gpu_util import announce
+
+    heads, d, n = 64, 64, 4 * 127 * 64
+    gen = torch.Generator(device="cuda").manual_seed(24)
+    q, k = (torch.randn((n, 1, d), device="cuda", generator=gen).bfloat16() for _ in range(2))
+    v, o = torch.zeros((2, n, heads, d), dtype=torch.bfloat16, device="cuda")
+    g = torch.full((n, heads), 0.17, device="cuda")
+    g[0], g[127 * 64:] = -math.inf, 0.0
+    pool = torch.randn((2, 1, heads, d, d), device="cuda", generator=gen)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    announce(f"linear_attn: {n} tokens that grow after a reset")
+    for out in (o, None):
+        pool[1] = 3.0
+        D.dasc_linear_attn(D.Shape("gdn", 1, heads, 1, d, d), 0, pool, i32(0), i32(1), q, k, v, g, out, i32(0, n), n)
+        torch.cuda.synchronize()
+        assert not pool[1].any() and not o.any()
