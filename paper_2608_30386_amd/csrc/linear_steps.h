@@ -45,10 +45,17 @@ __device__ inline float rows_sum(float x) {
 }
 
 // S e^g.  A decay near one is applied as S + S (e^g - 1): rounded to fp32 itself it would be off
-// by up to 2^-25, the same way for the whole state, token after token.
+// by up to 2^-25, the same way for the whole state, token after token.  A growth that fp32 may not hold goes
+// in three steps, each of a whole number but the last: zero stays zero whatever it is, and a small state
+// comes out right (beyond e^264 nothing else does).
 template <int R>
 __device__ inline void decay(dasc_wy::f32x4 (&S)[R], float g) {
-  if (g > -0.5f) {
+  if (g > 64.0f) {
+    const float top = fminf(g, 264.0f), third = rintf(top * (1.0f / 3.0f)), e = expf(third);
+    const float rest = expf(top - 2.0f * third);
+#pragma unroll
+    for (int r = 0; r < R; ++r) S[r] = S[r] * e * e * rest;
+  } else if (g > -0.5f) {
     const float m = expm1f(g);
 #pragma unroll
     for (int r = 0; r < R; ++r)

@@ -233,3 +233,25 @@ def test_growth_after_a_reset():
         D.dasc_linear_attn(D.Shape("gdn", 1, heads, 1, d, d), 0, pool, i32(0), i32(1), q, k, v, g, out, i32(0, n), n)
         torch.cuda.synchronize()
         assert not pool[1].any() and not o.any()
+
+
+@pytest.mark.parametrize("hint", [0, 300])
+@pytest.mark.parametrize("delta", [False, True])
+def test_any_log_decay(hint, delta):
+    """Factors that fp32 does not hold, of states that are zero or small enough, and states cleared first."""
+    m = make(360, [70, 20, 5], 4, 2, 64, 64, delta)
+    m["g"][:, 0] = -1e30
+    m["g"][:, 1] = -300.0
+    m["g"][2:, 2] = -0.5
+    m["g"][1, 2] = 100.0                           # a state of zero, and one of 1e-30
+    m["g"][70:90, 3] = 0.0
+    m["g"][75, 3] = -math.inf                      # cleared, then a factor of e^95 with nothing written between
+    m["g"][76, 3] = 95.0
+    m["qkv"][:2, 2 * 2 * 64:2 * 2 * 64 + 4 * 64] = 0
+    m["qkv"][75:77, 2 * 2 * 64:2 * 2 * 64 + 4 * 64] = 0
+    m["pool"][0, 1, 2] *= 1e-30
+    m["pool"][1, 1, 2] = 0
+    if delta:
+        m["beta"][75:77] = 0
+        m["beta"][1, 2] = 0
+    check(m, [0, 1, 2], [3, 4, 5], call(m, [0, 1, 2], [3, 4, 5], max_len=hint))
