@@ -69,7 +69,9 @@ int dasc_linear_attn_workspace_bytes(const dasc_shape *shape, int32_t n_req, int
  *     token-by-token and the chunked form and decides nothing else: results do not depend on it
  *     beyond rounding.
  *   io: q, k, v and o 16-byte aligned, their strides multiples of 8 elements (o and v: of 4);
- *     all strides >= 0.  o must not overlap an input.  Rows of o of tokens that no request
+ *     all strides >= 0.  o must not overlap an input, nor its rows (token, head) each other: they
+ *     lie dv or more apart, all heads of a token (or tokens of a head) before the next one's.
+ *     Rows of o of tokens that no request
  *     takes are not written.
  *   workspace: device, at least dasc_linear_attn_workspace_bytes, 16-byte aligned (may be NULL
  *     if that is 0); overlapping calls must not share one.
@@ -80,7 +82,7 @@ int dasc_linear_attn_workspace_bytes(const dasc_shape *shape, int32_t n_req, int
  * and decays in fp32 (running sums of log-decays in 64 bits); keys and queries are taken as
  * they are.
  * Errors: DASC_E_INVAL (NULL shape, states, io or cu_seqlens; k, v or g NULL with n_tokens > 0; q
- * NULL with o given; neither o nor dst_slot given; misalignment or a bad stride; layer out of
+ * NULL with o given; neither o nor dst_slot given; misalignment, a bad stride or rows of o that overlap; layer out of
  * [0, L), n_req < 1, n_tokens < 0 or above 2^31 - 1, max_len < 0, n_pool < 1, scale not finite),
  * DASC_E_SHAPE (bad shape, dv % 4 != 0), DASC_E_WORKSPACE, DASC_E_UNSUPPORTED (arch KDA, whose decay is by channel; dk not in
  * {16, 32, 64, 128} or dv > 256), DASC_E_HIP. */

@@ -229,14 +229,7 @@ extern "C" int dasc_block_norm(const dasc_norm_io* io, dasc_stream_t stream) {
   if (a.gate && (a.gate_out < 0 || a.gate_in < 0)) return DASC_E_INVAL;
   if (a.x && (a.x_row_out < 0 || a.x_row_in < 0)) return DASC_E_INVAL;
   // rows of an output must not overlap
-  const auto apart = [&](int64_t so, int64_t si) {
-    if (so < 0 || si < 0) return false;
-    if (a.outer == 1) return a.inner == 1 || si >= a.dim;
-    if (a.inner == 1) return so >= a.dim;
-    const int64_t lo = so < si ? so : si, hi = so < si ? si : so;
-    const int64_t n = so < si ? a.outer : a.inner;      // rows that lie `lo` apart
-    return lo >= a.dim && hi / n >= lo;                 // hi >= n lo, without the product
-  };
+  const auto apart = [&](int64_t so, int64_t si) { return rows_apart(a.outer, so, a.inner, si, a.dim); };
   if (a.x_out && !apart(a.xo_out, a.xo_in)) return DASC_E_INVAL;
   if (a.h_out && !apart(a.h_row_out, a.h_row_in)) return DASC_E_INVAL;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);

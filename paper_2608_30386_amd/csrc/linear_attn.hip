@@ -126,6 +126,8 @@ extern "C" int dasc_linear_attn(const dasc_shape* shape, int32_t layer, float* s
   if (rc != DASC_OK) return rc;
   if (workspace_bytes < need || (need > 0 && !workspace)) return DASC_E_WORKSPACE;
   if (need > 0 && !aligned16(workspace)) return DASC_E_INVAL;
+  // rows of the output must not overlap
+  if (io->o && !dasc::rows_apart(n_tokens, io->o_tok, shape->n_heads, io->o_head, dv)) return DASC_E_INVAL;
 
   dasc::LinearArgs a;
   a.io = *io;

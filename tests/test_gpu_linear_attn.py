@@ -392,3 +392,22 @@ def test_rows_that_are_not_apart():
                        beta=m["beta"].cuda(), scale=0.3)
     torch.cuda.synchronize()
     check(m, [0], [1], (o.float().cpu().numpy(), pool.cpu().numpy()))
+
+
+@pytest.mark.parametrize("length", [1, 5, 150])
+@pytest.mark.parametrize("delta", [False, True])
+def test_an_output_with_heads_first(length, delta):
+    """o as [H, n_tokens, dv] in memory: strides in the other order."""
+    import torch
+
+    m = make(24, [length], 4, 2, 64, 64, delta)
+    H, Hqk, dk, dv = m["dims"]
+    q, k, v = (x.cuda() for x in views(m, m["qkv"]))
+    pool = m["pool"].cuda()
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    o = torch.full((H, length, dv + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+    D.dasc_linear_attn(D.Shape("gdn", m["L"], H, Hqk, dk, dv), 1, pool, i32(0), i32(1), q, k, v, m["g"].cuda(),
+                       o.transpose(0, 1)[..., :dv], i32(0, length), length,
+                       beta=m["beta"].cuda() if delta else None, scale=0.3)
+    torch.cuda.synchronize()
+    check(m, [0], [1], (o.transpose(0, 1)[..., :dv + 4].float().cpu().numpy(), pool.cpu().numpy()))

@@ -68,6 +68,12 @@ def test_linear_attn_argument_errors():
     assert linear(gdn(dv=260)) == E.DASC_E_UNSUPPORTED
 
 
+def test_linear_attn_refuses_an_output_whose_rows_overlap():
+    for bad in (dict(o_tok=0), dict(o_head=0), dict(o_head=60), dict(o_tok=252), dict(o_tok=64, o_head=64),
+                dict(o_tok=60, o_head=1024), dict(o_tok=64, o_head=252), dict(n_tok=1, o_head=32)):
+        assert linear(**bad) == E.DASC_E_INVAL, bad
+
+
 def test_linear_attn_workspace():
     out = C.c_size_t()
     ask = lambda sh, *a: LIB.dasc_linear_attn_workspace_bytes(  # noqa: E731
