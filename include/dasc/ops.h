@@ -82,7 +82,7 @@ int dasc_linear_attn_workspace_bytes(const dasc_shape *shape, int32_t n_req, int
  * and decays in fp32 (running sums of log-decays in 64 bits); keys and queries are taken as
  * they are.
  * Errors: DASC_E_INVAL (NULL shape, states, io or cu_seqlens; k, v or g NULL with n_tokens > 0; q
- * NULL with o given; neither o nor dst_slot given; misalignment, a bad stride or rows of o that overlap; layer out of
+ * NULL with o given; neither o nor dst_slot given with n_tokens > 0; misalignment, a bad stride or rows of o that overlap; layer out of
  * [0, L), n_req < 1, n_tokens < 0 or above 2^31 - 1, max_len < 0, n_pool < 1, scale not finite),
  * DASC_E_SHAPE (bad shape, dv % 4 != 0), DASC_E_WORKSPACE, DASC_E_UNSUPPORTED (arch KDA, whose decay is by channel; dk not in
  * {16, 32, 64, 128} or dv > 256), DASC_E_HIP. */

@@ -103,7 +103,7 @@ extern "C" int dasc_linear_attn(const dasc_shape* shape, int32_t layer, float* s
     return DASC_E_INVAL;
   if (!states || !cu_seqlens) return DASC_E_INVAL;
   if (n_tokens > 0 && (!io->k || !io->v || !io->g)) return DASC_E_INVAL;
-  if (!io->o && !dst_slot) return DASC_E_INVAL;
+  if (n_tokens > 0 && !io->o && !dst_slot) return DASC_E_INVAL;
   if (io->o && !io->q) return DASC_E_INVAL;
   using dasc::aligned16;
   if (!aligned16(states) || (io->o && !aligned16(io->q)) || !aligned16(io->k) || !aligned16(io->v) ||
@@ -128,6 +128,7 @@ extern "C" int dasc_linear_attn(const dasc_shape* shape, int32_t layer, float* s
   if (need > 0 && !aligned16(workspace)) return DASC_E_INVAL;
   // rows of the output must not overlap
   if (io->o && !dasc::rows_apart(n_tokens, io->o_tok, shape->n_heads, io->o_head, dv)) return DASC_E_INVAL;
+  if (n_tokens == 0 && !dst_slot) return DASC_OK;     // no output and no state to write
 
   dasc::LinearArgs a;
   a.io = *io;

@@ -74,6 +74,14 @@ def test_linear_attn_refuses_an_output_whose_rows_overlap():
         assert linear(**bad) == E.DASC_E_INVAL, bad
 
 
+def test_linear_attn_of_no_tokens_and_no_destination():
+    """A step that scores no tokens (an empty tensor's pointer is NULL) has nothing to do."""
+    none = dict(q=None, k=None, v=None, g=None, beta=None)
+    assert linear(n_tok=0, max_len=0, dst=None, o=None, **none) == E.DASC_OK
+    assert linear(n_tok=0, max_len=0, dst=None) == E.DASC_OK
+    assert linear(n_tok=0, dst=None, o=None, scale=math.nan) == E.DASC_E_INVAL
+
+
 def test_linear_attn_workspace():
     out = C.c_size_t()
     ask = lambda sh, *a: LIB.dasc_linear_attn_workspace_bytes(  # noqa: E731
