@@ -255,23 +255,34 @@ __device__ inline void make_decays(Decays& d, float g, float scale, int lane) {
 // D_ts for s <= t from the running sums
 __device__ inline float decay_of(double gt, double gs) { return dasc_wy::ex2(float(gt - gs)); }
 
-// The state's decay.  BRANCH: on the chunk's kind, which is the same in all lanes; without, an
-// instruction more for each element.  (In the split walk a matrix product can stand right before the
-// branch; the compiler then left out the wait between it and the read of its result behind the branch,
-// and outputs of the last chunk were wrong.)
-template <bool BRANCH, int NT>
+// Results of matrix instructions that are read behind a branch.  The compiler waits for a result within a
+// block of code, but not always on the paths that leave it: with a branch on the kind of the state's decay
+// the outputs of a prompt's last chunk were read two instructions after the product that forms them, eight
+// too few.  So the wait is written out where results cross a branch or leave the loop (ten instructions'
+// time, against eight that the next read waits in any case).
+#define DASC_SETTLE "s_nop 7\n\ts_nop 1"
+__device__ inline void settle(f32x4& x) { asm volatile(DASC_SETTLE : "+v"(x)); }
+template <int N>
+__device__ inline void settle(f32x4 (&x)[N]) {
+  static_assert(N == 1 || N == 2 || N == 4 || N == 8);
+  if constexpr (N == 1) settle(x[0]);
+  if constexpr (N == 2) asm volatile(DASC_SETTLE : "+v"(x[0]), "+v"(x[1]));
+  if constexpr (N == 4) asm volatile(DASC_SETTLE : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));
+  if constexpr (N == 8)
+    asm volatile(DASC_SETTLE
+                 : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]), "+v"(x[7]));
+}
+#undef DASC_SETTLE
+
+// The state's decay, without a branch on the chunk's kind: an instruction more for each element
+template <int NT>
 __device__ inline void decay_state(f32x4 (&S)[NT], const Decays& d) {
   const float m = d.m;
   const bool near = d.near;
-  if (BRANCH && !near) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) S[t] *= m;
-  } else {
+  for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) S[t][i] = fmaf(S[t][i], m, BRANCH || near ? S[t][i] : 0.0f);
-  }
+    for (int i = 0; i < 4; ++i) S[t][i] = fmaf(S[t][i], m, near ? S[t][i] : 0.0f);
 }
 
 // Whether all of these are finite: zero times anything else is NaN
@@ -733,6 +744,7 @@ __global__ __launch_bounds__((kSplitThreads<CT, NG, DELTA>)) void linear_split_k
             }
           }
       }
+      settle(O);
       load_p(c + 1);
       const __amdgpu_buffer_rsrc_t ro = os.next(c, last);
 #pragma unroll
@@ -869,6 +881,7 @@ __global__ __launch_bounds__((kSplitThreads<CT, NG, DELTA>)) void linear_split_k
             u = mma(rt[s][0], y1, u);
             u = mma(rt[s][0], y0, u);
           }
+        settle(u);
         uint2 h3[3];
         half_planes(u * er, h3);
         put_half(lds + L::kU + (tile0 + ct) * 6144, m, lane, h3);
@@ -892,7 +905,7 @@ __global__ __launch_bounds__((kSplitThreads<CT, NG, DELTA>)) void linear_split_k
 
     // the state
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) decay_state<false>(S[ct], d);
+    for (int ct = 0; ct < CT; ++ct) decay_state(S[ct], d);
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -907,6 +920,8 @@ __global__ __launch_bounds__((kSplitThreads<CT, NG, DELTA>)) void linear_split_k
           S[ct][t] = mma(k, get(ub, 3 * s, lane), S[ct][t]);
         }
       }
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) settle(S[ct]);
     if constexpr (HELP) {
       put_s();                              // (for nobody after the last chunk)
     } else if constexpr (DELTA) {
@@ -1247,7 +1262,7 @@ __global__ __launch_bounds__(64 * NW, (kWavesPerSimd<CT, DELTA, OUT>)) void line
 
     // the state
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) decay_state<true>(S[ct], d);
+    for (int ct = 0; ct < CT; ++ct) decay_state(S[ct], d);
     // (what a chunk has cleared no later growth brings back)
     if constexpr (LOCAL) log2_sum = d.G[kC - 1] < -1000.0 ? -1e30 : log2_sum + d.G[kC - 1];
 #pragma unroll
@@ -1271,6 +1286,8 @@ __global__ __launch_bounds__(64 * NW, (kWavesPerSimd<CT, DELTA, OUT>)) void line
           for (int ct = 0; ct < CT; ++ct) S[ct][t] = mma(k, u[ct][j], S[ct][t]);
       }
     }
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) settle(S[ct]);
     lds_barrier();                          // everybody is done with this chunk
     if (c + 1 < chunks) {
       stage();
