@@ -1622,13 +1622,19 @@ int tiles_of(int64_t heads, int dv, int most) {
   return t;
 }
 
-// Units of a window: packets of 1 GiB (270000 tokens of 8 heads) bound the workspace, whatever the
-// length; a longer call takes two launches for each window more.
+// The workspace's part for packets: 1 GiB (270000 tokens of 8 heads) bounds it, whatever the length.  It has
+// room for packets with planes, whichever the call takes: fewer heads of the same tokens do take them.
 constexpr int64_t kWindowBytes = int64_t(1) << 30;
 
-int64_t window_units(const ChunkPlan& c) {
-  const int64_t all = units_of(c, kC), fit = kWindowBytes / (c.H * int64_t(kPacket<true>));
-  return all <= fit ? all : fit > 0 ? fit : 1;
+int64_t packet_bytes(const ChunkPlan& c) {
+  const int64_t all = units_of(c, kC), unit = c.H * int64_t(kPacket<true>), fit = kWindowBytes / unit;
+  return (all <= fit ? all : fit > 0 ? fit : 1) * unit;
+}
+
+// Units of a window, of which a longer call has several and takes two launches for each
+int64_t window_units(const ChunkPlan& c, int64_t packet) {
+  const int64_t all = units_of(c, kC), fit = packet_bytes(c) / (c.H * packet);
+  return all <= fit ? all : fit;
 }
 
 struct Launch {
@@ -1658,8 +1664,8 @@ struct Launch {
     if (c.delta) {
       units = c.n_req;
       const int tiles = tiles_of(units * c.H, c.dv, kWhole);
-      const int64_t all = units_of(c, kC), step = window_units(c);
-      float* const carry = reinterpret_cast<float*>(ws + step * c.H * kPacket<true>);
+      const int64_t all = units_of(c, kC), step = window_units(c, tiles == kWhole ? kPacket<false> : kPacket<true>);
+      float* const carry = reinterpret_cast<float*>(ws + packet_bytes(c));
       const int64_t carried = int64_t(c.H) * DK * c.dv;
       p.packets = ws;
       for (int64_t u = 0, j = 0; u < all; u += step, ++j) {
@@ -1706,8 +1712,8 @@ bool linear_chunk_supported(const ChunkPlan& c) {
 
 int64_t linear_chunk_workspace(const ChunkPlan& c) {
   if (c.delta) {
-    const int64_t step = window_units(c), carry = step < units_of(c, kC) ? 2 * int64_t(c.H) * c.dk * c.dv * 4 : 0;
-    return step * c.H * kPacket<true> + carry;
+    const bool windows = window_units(c, kPacket<true>) < units_of(c, kC);
+    return packet_bytes(c) + (windows ? 2 * int64_t(c.H) * c.dk * c.dv * 4 : 0);
   }
   const int64_t units = segments_of(c).units;
   return units ? units * c.H * (int64_t(c.dk) * c.dv * 4 + 8) + int64_t(c.n_req) * c.H * (c.dv / 16) * 4 : 0;
