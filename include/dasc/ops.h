@@ -43,8 +43,9 @@ typedef struct dasc_linear_io {
   int64_t g_tok, g_head, beta_tok, beta_head, o_tok, o_head;
 } dasc_linear_io;
 
-/* Device workspace of dasc_linear_attn for these sizes (0 for many).  delta: whether beta is
- * given.  Errors: DASC_E_INVAL (NULL, n_req < 1, n_tokens < 0, max_len < 0), DASC_E_SHAPE. */
+/* Device workspace of dasc_linear_attn for these sizes (0 for many).  It does for every call of this
+ * shape with no more requests and tokens than these and none longer, so that one allocation serves
+ * an engine's largest batch and all smaller ones.  delta: whether beta is given.  Errors: DASC_E_INVAL (NULL, n_req < 1, n_tokens < 0, max_len < 0), DASC_E_SHAPE. */
 int dasc_linear_attn_workspace_bytes(const dasc_shape *shape, int32_t n_req, int64_t n_tokens,
                                      int32_t max_len, int32_t delta, size_t *bytes);
 

@@ -56,7 +56,7 @@ struct ChunkPlan {
 };
 
 bool linear_chunk_supported(const ChunkPlan& c);
-int64_t linear_chunk_workspace(const ChunkPlan& c);
+int64_t linear_chunk_workspace(ChunkPlan c);
 void launch_linear_chunks(const ChunkPlan& c, const LinearArgs& a, void* ws, hipStream_t st);
 void launch_linear_steps(const LinearArgs& a, int dk, hipStream_t st);
 

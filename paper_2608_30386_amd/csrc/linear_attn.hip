@@ -86,7 +86,7 @@ extern "C" int dasc_linear_attn_workspace_bytes(const dasc_shape* shape, int32_t
   if (!shape || !bytes || n_req < 1 || n_tokens < 0 || max_len < 0) return DASC_E_INVAL;
   if (!dasc::valid_shape(shape)) return DASC_E_SHAPE;
   const dasc::ChunkPlan c{shape->dk, shape->dv, shape->n_heads, n_req, max_len, n_tokens, delta != 0};
-  *bytes = dasc::takes_chunks(c) ? size_t(dasc::linear_chunk_workspace(c)) : 0;
+  *bytes = max_len > dasc::kStepTokens ? size_t(dasc::linear_chunk_workspace(c)) : 0;
   return DASC_OK;
 }
 

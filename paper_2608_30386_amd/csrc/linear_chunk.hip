@@ -1591,18 +1591,30 @@ struct Segments {
 // The states of 64 segments are joined one after another in 18 us, hence no more.
 constexpr int kMaxSegments = 64;
 
+// Segments, a head's blocks each, that the chip has CUs for; no more are ever made
+int64_t segment_room(const ChunkPlan& c) {
+  const int64_t cols = 16 * whole_tiles(c.dk);
+  return kCus / (c.H * ((c.dv + cols - 1) / cols));
+}
+
+int64_t longest(const ChunkPlan& c) {       // chunks of the longest request
+  return ((c.max_len < c.n_tokens ? c.max_len : c.n_tokens) + kC - 1) / kC;
+}
+
+// Whether splitting pays for a request of `all` chunks in segments of `seg`, and for any of this length
+bool split_pays(int64_t all, int64_t seg) { return 2 * all >= 5 * seg + 23; }
+bool may_split(const ChunkPlan& c) { return !c.delta && segment_room(c) >= 2 && split_pays(longest(c), 1); }
+
 Segments segments_of(const ChunkPlan& c) {
-  const int64_t cols = 16 * whole_tiles(c.dk), blocks = c.H * ((c.dv + cols - 1) / cols);
-  const int64_t room = kCus / blocks, tokens = c.max_len < c.n_tokens ? c.max_len : c.n_tokens;
-  const int64_t all = (tokens + kC - 1) / kC;
-  if (c.delta || room < 2) return {};
+  const int64_t room = segment_room(c), all = longest(c);
+  if (!may_split(c)) return {};
   const int64_t each = room / c.n_req;      // segments of every request, or numbers by length
   int64_t seg = each > 0 ? (all + each - 1) / each : all;
   const int64_t by_length = room > c.n_req ? c.n_tokens / kC / (room - c.n_req) + 1 : all;
   const bool alike = seg <= by_length;
   if (!alike) seg = by_length;
   if (seg < (all + kMaxSegments - 1) / kMaxSegments) seg = (all + kMaxSegments - 1) / kMaxSegments;
-  if (2 * all < 5 * seg + 23) return {};
+  if (!split_pays(all, seg)) return {};
   const int64_t n = (all + seg - 1) / seg;
   return {int(seg), alike ? int(n) : 0, alike ? n * c.n_req : units_of(c, seg * kC)};
 }
@@ -1705,18 +1717,24 @@ struct Launch {
 
 }  // namespace
 
+constexpr int64_t kMaxHeads = 1 << 21;      // of all requests: a grid counts threads in 32 bits
+
 bool linear_chunk_supported(const ChunkPlan& c) {
-  // (a grid counts threads in 32 bits)
-  return (c.dk == 64 || c.dk == 128) && c.dv % 16 == 0 && c.n_tokens > 0 && int64_t(c.n_req) * c.H <= (1 << 21);
+  return (c.dk == 64 || c.dk == 128) && c.dv % 16 == 0 && c.n_tokens > 0 && int64_t(c.n_req) * c.H <= kMaxHeads;
 }
 
-int64_t linear_chunk_workspace(const ChunkPlan& c) {
+// For this call and for every one with no more requests and tokens, none longer: a caller that allocates once,
+// for its largest, has enough for all.  More requests alone may need less (they are not split, or too many
+// for the chunked form), so what depends on their number is taken at its most.
+int64_t linear_chunk_workspace(ChunkPlan c) {
+  if (c.n_req * int64_t(c.H) > kMaxHeads) c.n_req = int32_t(kMaxHeads / c.H);
+  if (c.n_req == 0 || !linear_chunk_supported(c)) return 0;
   if (c.delta) {
     const bool windows = window_units(c, kPacket<true>) < units_of(c, kC);
     return packet_bytes(c) + (windows ? 2 * int64_t(c.H) * c.dk * c.dv * 4 : 0);
   }
-  const int64_t units = segments_of(c).units;
-  return units ? units * c.H * (int64_t(c.dk) * c.dv * 4 + 8) + int64_t(c.n_req) * c.H * (c.dv / 16) * 4 : 0;
+  const int64_t room = segment_room(c);     // segments, and so requests that are split
+  return may_split(c) ? room * c.H * (int64_t(c.dk) * c.dv * 4 + 8 + c.dv / 16 * 4) : 0;
 }
 
 void launch_linear_chunks(const ChunkPlan& c, const LinearArgs& a, void* ws, hipStream_t st) {

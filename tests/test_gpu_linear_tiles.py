@@ -132,3 +132,35 @@ def test_windows_of_a_call_with_many_heads():
     torch.cuda.synchronize()
     assert torch.equal(oa, ob) and torch.equal(a, b)
     assert torch.isfinite(oa.float()).all() and oa[-1].abs().max() > 0
+
+
+@pytest.mark.parametrize("delta", [False, True])
+def test_one_workspace_for_all_batches(delta):
+    """Allocated for the largest batch, used for smaller ones, which need their own parts of it; it ends
+    where the query says."""
+    import torch
+
+    heads, d = 16, 64
+    sh = D.Shape("gdn", 1, heads, heads, d, d)
+    batches = [[2000], [1500, 700], [1000] * 4, [64, 2000, 13], [300] * 12]
+    size = D.dasc_linear_attn_workspace_bytes(sh, 12, 4000, 2000, delta)
+    ws = torch.empty(size + 4096, dtype=torch.uint8, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(25)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=gen)  # noqa: E731
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    for lens in batches:
+        N, n = sum(lens), len(lens)
+        q, k = (torch.nn.functional.normalize(rnd(N, heads, d), dim=-1).bfloat16() for _ in range(2))
+        v, g = rnd(N, heads, d).bfloat16(), -rnd(N, heads).abs() * 0.1
+        beta = torch.sigmoid(rnd(N, heads)) if delta else None
+        pool, got = rnd(2 * n, 1, heads, d, d), []
+        announce(f"linear_attn in a shared workspace: {lens} delta={delta}")
+        for w in (None, ws[:size]):
+            ws.fill_(0xA5)
+            p, o = pool.clone(), torch.zeros_like(v)
+            D.dasc_linear_attn(sh, 0, p, i32(range(n)), i32(range(n, 2 * n)), q, k, v, g, o,
+                               i32(np.concatenate([[0], np.cumsum(lens)])), max(lens), beta=beta, workspace=w)
+            got.append((p, o))
+        torch.cuda.synchronize()
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+        assert (ws[size:] == 0xA5).all()

@@ -102,6 +102,35 @@ def test_linear_attn_workspace():
             assert linear(gdn(dk=128, dv=128), ws=ODD, **big, **over) == E.DASC_E_INVAL
 
 
+@pytest.mark.parametrize("delta", [0, 1])
+def test_a_workspace_does_for_every_smaller_call(delta):
+    out = C.c_size_t()
+
+    def ask(sh, n, tokens, longest):
+        assert LIB.dasc_linear_attn_workspace_bytes(C.byref(sh), n, tokens, longest, delta, C.byref(out)) == E.DASC_OK
+        return out.value
+
+    reqs = [1, 2, 3, 4, 5, 8, 31, 64, 300, 5000, 70000, 3000000]
+    longs = [0, 1, 12, 13, 64, 800, 833, 900, 1500, 4096, 16384, 100000]
+    for H, dk, dv in ((32, 128, 128), (4, 128, 256), (16, 64, 64), (1, 64, 16), (300, 128, 128), (8, 32, 64), (40000, 128, 256)):
+        sh = gdn(H=H, Hqk=1, dk=dk, dv=dv, L=1)
+        need = [[[ask(sh, n, min(f * longest, 2 ** 31 - 1), longest) for f in (1, 2, 7, 1000)] for longest in longs]
+                for n in reqs]
+        for i in range(len(reqs)):
+            for j in range(len(longs)):
+                for x in range(4):
+                    # one step down in each: fewer requests, fewer tokens, and none so long
+                    if i:
+                        assert need[i - 1][j][x] <= need[i][j][x], (H, dk, dv, reqs[i], longs[j], x)
+                    if j:
+                        assert need[i][j - 1][x] <= need[i][j][x], (H, dk, dv, reqs[i], longs[j], x)
+                    if x:
+                        assert need[i][j][x - 1] <= need[i][j][x], (H, dk, dv, reqs[i], longs[j], x)
+    # no tokens more, but a longer request
+    sh = gdn(H=32, dk=128, dv=128)
+    assert ask(sh, 4, 16384, 4096) <= ask(sh, 4, 16384, 9000)
+
+
 def verify(n=1, m=2, V=100, dtype=_lib.DASC_DTYPE_F32, ws=P, ws_bytes=1 << 40, strides=(300, 100, 200, 100), **over):
     p = dict(target=P, draft=P, tokens=P, count=None, u=P, r=P, out=P, emitted=P)
     p.update(over)
