@@ -53,17 +53,32 @@ void launch_steps(const LinearArgs& a, hipStream_t st) {
   }
 }
 
-// Calls whose longest request has more tokens than this take the chunked form.  Token by token | in
-// chunks, us, dk = dv = 128, 32 heads:
-//     tokens                        4          8         12         16         32
-//     1 request, delta rule     9 |  16    14 |  16    18 |  16    22 |  16    39 |  16
-//     1 request, plain          8 |   7    12 |   7    15 |   7    18 |   7    31 |   7
-//     8 requests, delta rule     - | -     18 |  25    23 |  26    27 |  26     - | -
-//     64 requests, delta rule  64 | 122    80 | 122    97 | 125   116 | 128   198 | 139
-//     64 requests, plain       63 |  89    74 |  90    88 |  92   103 |  94   165 |  97
-constexpr int kStepTokens = 12;
+// Calls whose longest request has more tokens than this take the chunked form.  A token costs the other form
+// the chain of its sums where there are few heads, and a pass over the state's registers where there are
+// many; a chunk of the delta rule costs two launches more than one of the plain rule.  Token by token | in
+// chunks, us, 32 heads, with an output:
+//     tokens                                4          8          12         16         20         24
+//     dk = dv = 128
+//     1 request, delta rule              9 |  15   13 |  15   18 |  15   22 |  15   27 |  15   31 |  15
+//     8 requests                        13 |  25   17 |  25   22 |  25   26 |  25   31 |  25   36 |  26
+//     64 requests                       57 | 117   72 | 120   91 | 122  110 | 123  128 | 130  148 | 132
+//     1 request, plain rule              8 |   7   12 |   7   15 |   7   19 |   7   22 |   7   26 |   7
+//     8 requests                        12 |  13   15 |  13   19 |  13   23 |  13   27 |  13   31 |  13
+//     64 requests                       55 |  82   66 |  84   81 |  85   96 |  86  109 |  87  123 |  89
+//     dk = dv = 64
+//     1 request, delta rule              8 |  14   11 |  14   15 |  14   18 |  14   22 |  14   25 |  14
+//     64 requests                       18 |  53   24 |  53   31 |  54   36 |  54   43 |  58   50 |  58
+//     1 request, plain rule              7 |   6    9 |   6   12 |   6   15 |   6   17 |   6   20 |   6
+//     64 requests                       16 |  25   21 |  25   25 |  25   29 |  26   34 |  26   38 |  26
+// (states only: the same places but for one request, delta rule: 14.)
+int step_tokens(const ChunkPlan& c) {
+  const bool few = int64_t(c.n_req) * c.H <= 256;
+  if (!c.delta) return few ? 4 : 11;
+  return few ? 11 : c.dk == 64 ? 26 : 19;
+}
+constexpr int kLeastSteps[2] = {4, 11};       // of any call: plain, delta
 
-bool takes_chunks(const ChunkPlan& c) { return c.max_len > kStepTokens && linear_chunk_supported(c); }
+bool takes_chunks(const ChunkPlan& c) { return c.max_len > step_tokens(c) && linear_chunk_supported(c); }
 
 bool bad_stride(int64_t s, int64_t multiple) { return s < 0 || s % multiple != 0; }
 
@@ -86,7 +101,7 @@ extern "C" int dasc_linear_attn_workspace_bytes(const dasc_shape* shape, int32_t
   if (!shape || !bytes || n_req < 1 || n_tokens < 0 || max_len < 0) return DASC_E_INVAL;
   if (!dasc::valid_shape(shape)) return DASC_E_SHAPE;
   const dasc::ChunkPlan c{shape->dk, shape->dv, shape->n_heads, n_req, max_len, n_tokens, delta != 0};
-  *bytes = max_len > dasc::kStepTokens ? size_t(dasc::linear_chunk_workspace(c)) : 0;
+  *bytes = max_len > dasc::kLeastSteps[delta != 0] ? size_t(dasc::linear_chunk_workspace(c)) : 0;
   return DASC_OK;
 }
 
