@@ -175,8 +175,10 @@ bool by_eight(const dasc_norm_io& a, int e, int r, int w) {
 // The shape of a row, us for 6000 rows of a gated bf16 block and an fp32 residual:
 // - accesses of eight elements where all rows are aligned to that (4096: 77, by four 83), of four where
 //   not (1500: 36.5, by eight 45; 2052: 50.6 and 62; 1999: 52 and 62);
-// - as many waves as there are 512s, and a third access where a little is left over (2050: 50 on four
-//   waves, 55 on five);
+// - a wave for every 512, or begun 512.  Where a little is left over two, four or sixteen of them, a third
+//   access instead of a wave that would have a SIMD to itself (or pass what a block may have): 1100 28.8 |
+//   29.7, 2050 50.7 | 55.3, 2178 57.1 | 63.2, 8194 184 | 232.  Not elsewhere: 1540 43.5 | 39.3, 2562
+//   75.4 | 67.6, 3330 91.6 | 79.7, 3970 114 | 95, 8002 228 | 187, and at eight or nine it is the same (4226 115 | 113);
 // - rows of up to 128 on 16 lanes, eight elements each.
 template <typename T, typename X>
 void launch_dim(const dasc_norm_io& a, bool eight, hipStream_t st) {
@@ -186,7 +188,8 @@ void launch_dim(const dasc_norm_io& a, bool eight, hipStream_t st) {
   else if (n <= 512) launch<T, X, 64, 2, 4>(a, 256, st);
   else if (n <= 1024) launch<T, X, 64, 4, 4>(a, 256, st);
   else if (eight && n <= 8192) launch<T, X, 0, 1, 8>(a, threads(8), st);
-  else if (over > 0 && over <= 64 * whole && whole <= 16) launch<T, X, 0, 3, 4>(a, 64 * whole, st);
+  else if (over > 0 && over <= 64 * whole && (whole == 2 || whole == 4 || whole == 16))
+    launch<T, X, 0, 3, 4>(a, 64 * whole, st);
   else if (n <= 8192) launch<T, X, 0, 2, 4>(a, threads(8), st);
   else if (n <= 16384) launch<T, X, 0, 4, 4>(a, threads(16), st);
   else launch<T, X, 0, 8, 4>(a, threads(32), st);
