@@ -19,6 +19,7 @@
 
 #include "dasc/ops.h"
 #include "launch_common.h"
+#include "output_rows.h"
 #include "row_io.h"
 
 namespace dasc {

@@ -21,6 +21,7 @@
 
 #include "launch_common.h"
 #include "linear_steps.h"
+#include "output_rows.h"
 
 namespace dasc {
 namespace {
