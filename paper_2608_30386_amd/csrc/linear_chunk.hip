@@ -73,7 +73,7 @@ struct ChunkArgs {
   float* carry_out;                          // and of the one that goes on in the next
   float* seg_state;                          // plain: [segments, H, dk, dv]
   double* seg_log2;                          // plain: [segments, H], the decay over a segment
-  int32_t* seg_bad;                          // plain: [requests, H, tiles of 16 columns], see the join
+  int32_t* seg_bad;                          // plain: [requests, H, tiles of 16 columns], not finite at the end
   int32_t seg_chunks;                        // plain: chunks of a segment
   int32_t seg_each;                          // plain: segments of every request, 0: as many as it has tokens for
   int32_t col_blocks;
@@ -1042,7 +1042,7 @@ __global__ __launch_bounds__(64 * NW, (kWavesPerSimd<CT, DELTA, OUT>)) void line
   const int k_off = (tid / U * p.k_tok + 8 * (tid % U)) * 2;
   const int q_off = (tid / U * p.q_tok + 8 * (tid % U)) * 2;
   const int v_off = vcol < dv ? (tid / UV * p.v_tok + vcol) * 2 : kOutside;
-  // columns that the join found not to be finite: the request's first segment takes them by token
+  // columns that the join has marked: the request's first segment takes them by token
   bool left[CT];
   int o_off[CT];
 #pragma unroll
@@ -1298,6 +1298,8 @@ __global__ __launch_bounds__(64 * NW, (kWavesPerSimd<CT, DELTA, OUT>)) void line
   const ChunkArgs pe = arguments_again();
   const Walk we = kept.walk();
   if (LOCAL && tid == 0 && we.cb == 0) pe.seg_log2[we.unit * pe.a.H + we.h] = log2_sum;
+  if (LOCAL && we.first && lane < CT && 16 * (tile0 + lane) < pe.a.dv)
+    pe.seg_bad[(int64_t(we.i) * pe.a.H + we.h) * (pe.a.dv / 16) + tile0 + lane] = 0;
   float* to = we.end<DELTA, LOCAL>(pe, DK);
   const bool segment = !DELTA && pe.seg_chunks;
 #pragma unroll
@@ -1320,25 +1322,21 @@ __global__ __launch_bounds__(64 * NW, (kWavesPerSimd<CT, DELTA, OUT>)) void line
 // ---- plain rule: the segments of a request joined ------------------------------------------------------
 
 // Segment j's start: its own from the request's first state, and what the segments before it add.
-// Replaces the segments' sums by their starts; with no output to come, writes the last state.  A block has
-// 16 columns of a head's state, a row on four lanes, so it sees whether all of them are finite to the end:
-// if not, the request's first segment takes them token by token and the others leave them out; with no
-// output to come, this block does.
+// Replaces the segments' sums by their starts; with no output to come (finish), leaves the last state in
+// place of the first segment's sum.  Marks the columns whose last state is not finite: those the request's
+// first segment takes token by token and the others leave out, or linear_finish_kernel does.
 constexpr int kAhead = 8;
 
-template <int DK>
-__global__ __launch_bounds__(4 * DK) void linear_join_kernel(ChunkArgs p, bool finish) {
+__global__ __launch_bounds__(256) void linear_join_kernel(ChunkArgs p, int dk, bool finish) {
   const LinearArgs& a = p.a;
-  const int64_t per = int64_t(DK) * a.dv;
-  // (the tiles of a head side by side on one XCD: two of them share a line)
-  uint32_t bid = blockIdx.x;
-  if (gridDim.x % 8 == 0) bid = bid % 8 * (gridDim.x / 8) + bid / 8;
-  const int tiles = a.dv / 16, tile = bid % tiles, h = bid / tiles % a.H, i = bid / tiles / a.H;
-  const int64_t x = threadIdx.x / 4 * a.dv + 16 * tile + threadIdx.x % 4 * 4;
+  const int64_t per = int64_t(dk) * a.dv;
+  const int64_t x = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;     // dv is a multiple of 16
+  if (x >= per) return;
+  const int h = blockIdx.y, i = blockIdx.z;
   const int segs = segments(p, request_span(a, i).len);
   const int64_t u0 = first_segment(p, i);
-  const float* from = slot_state(a, a.src, i, h, DK);
-  f32x4 S = from ? *reinterpret_cast<const f32x4*>(from + x) : f32x4{0, 0, 0, 0};
+  const float* from = slot_state(a, a.src, i, h, dk);
+  f32x4 S[1] = {from ? *reinterpret_cast<const f32x4*>(from + x) : f32x4{0, 0, 0, 0}};
   const auto at = [&](int j) { return reinterpret_cast<f32x4*>(p.seg_state + ((u0 + j) * a.H + h) * per + x); };
   for (int j0 = 0; j0 < segs; j0 += kAhead) {       // what kAhead segments add, asked for together
     f32x4 add[kAhead];
@@ -1353,25 +1351,34 @@ __global__ __launch_bounds__(4 * DK) void linear_join_kernel(ChunkArgs p, bool f
     for (int e = 0; e < kAhead; ++e) {
       const int j = j0 + e;
       if (j >= segs) break;
-      *at(j) = S;
+      if (!finish) *at(j) = S[0];
       if (end[e] > -0.72) {
         const float m = expm1f(float(end[e] * 0.6931471805599453));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) S[i] = fmaf(S[i], m, S[i]) + add[e][i];
+        for (int i = 0; i < 4; ++i) S[0][i] = fmaf(S[0][i], m, S[0][i]) + add[e][i];
       } else {
-        S = S * dasc_wy::ex2(float(end[e])) + add[e];
+        S[0] = S[0] * dasc_wy::ex2(float(end[e])) + add[e];
       }
     }
   }
-  const bool bad = __syncthreads_or(!finite({S}));
-  if (!finish) {
-    if (threadIdx.x == 0) p.seg_bad[bid] = bad;
-  } else if (bad) {
+  if (finish) *at(0) = S[0];
+  if (!finite(S)) p.seg_bad[(int64_t(i) * a.H + h) * (a.dv / 16) + x % a.dv / 16] = 1;
+}
+
+// States alone: the last state from where the join left it, 16 columns a block; or token by token
+template <int DK>
+__global__ __launch_bounds__(4 * DK) void linear_finish_kernel(ChunkArgs p) {
+  const LinearArgs& a = p.a;
+  const int tiles = a.dv / 16, tile = blockIdx.x % tiles, h = blockIdx.x / tiles % a.H, i = blockIdx.x / tiles / a.H;
+  if (p.seg_bad[blockIdx.x]) {
     if (threadIdx.x < 64) walk_tokens<DK, 16, false, false>(a, i, h, 16 * tile, threadIdx.x);
-  } else {
-    float* to = slot_state(a, a.dst, i, h, DK);
-    if (to) *reinterpret_cast<f32x4*>(to + x) = S;
+    return;
   }
+  float* to = slot_state(a, a.dst, i, h, DK);
+  if (!to) return;
+  const int64_t x = threadIdx.x / 4 * a.dv + 16 * tile + threadIdx.x % 4 * 4;
+  const float* S = p.seg_state + (first_segment(p, i) * a.H + h) * int64_t(DK) * a.dv;
+  *reinterpret_cast<f32x4*>(to + x) = *reinterpret_cast<const f32x4*>(S + x);
 }
 
 // ---- delta rule: T, P and the decays of every chunk -----------------------------------------------------
@@ -1710,8 +1717,9 @@ struct Launch {
     p.seg_log2 = reinterpret_cast<double*>(ws + units * c.H * int64_t(DK) * c.dv * 4);
     p.seg_bad = reinterpret_cast<int32_t*>(p.seg_log2 + units * c.H);
     walk<DK, false, false, true>(kWhole);
-    linear_join_kernel<DK><<<uint32_t(c.n_req * c.H * (c.dv / 16)), 4 * DK, 0, st>>>(p, !out);
+    linear_join_kernel<<<dim3((DK * c.dv + 1023) / 1024, c.H, c.n_req), 256, 0, st>>>(p, DK, !out);
     if (out) walk<DK, false, true, false>(kWhole);
+    else linear_finish_kernel<DK><<<uint32_t(c.n_req * c.H * (c.dv / 16)), 4 * DK, 0, st>>>(p);
   }
 };
 
