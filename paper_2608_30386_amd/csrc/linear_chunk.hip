@@ -73,7 +73,7 @@ struct ChunkArgs {
   float* carry_out;                          // and of the one that goes on in the next
   float* seg_state;                          // plain: [segments, H, dk, dv]
   double* seg_log2;                          // plain: [segments, H], the decay over a segment
-  int32_t* seg_bad;                          // plain: [requests, H, tiles of 16 columns], not finite at the end
+  int32_t* seg_bad;                          // plain: [requests, H, blocks of the join, tiles], not finite at the end
   int32_t seg_chunks;                        // plain: chunks of a segment
   int32_t seg_each;                          // plain: segments of every request, 0: as many as it has tokens for
   int32_t col_blocks;
@@ -498,6 +498,13 @@ __device__ inline ChunkArgs arguments_again() {
 #pragma unroll
   for (uint32_t i = 0; i < sizeof(ChunkArgs) / 4; ++i) words.w[i] = reinterpret_cast<Words>(at)[i];
   return __builtin_bit_cast(ChunkArgs, words);
+}
+
+// Whether the join found this tile of 16 columns not to be finite at the request's end: a lane asks for what
+// each of its blocks, of 1024 elements of a state, says
+__device__ inline int marked(const ChunkArgs& p, int dk, int i, int h, int tile, int lane) {
+  const int tiles = p.a.dv / 16, parts = dk * p.a.dv / 1024;
+  return lane < parts ? p.seg_bad[((int64_t(i) * p.a.H + h) * parts + lane) * tiles + tile] : 0;
 }
 
 struct Kept {
@@ -1049,7 +1056,7 @@ __global__ __launch_bounds__(64 * NW, (kWavesPerSimd<CT, DELTA, OUT>)) void line
   for (int ct = 0; ct < CT; ++ct) {
     const bool in = col + 16 * ct < dv;
     left[ct] = !DELTA && OUT && p.seg_chunks && 16 * (tile0 + ct) < dv &&
-               uniform(p.seg_bad[(int64_t(w.i) * a.H + h) * (dv / 16) + tile0 + ct]) != 0;
+               __any(marked(p, DK, w.i, h, tile0 + ct, lane));
     o_off[ct] = in && !left[ct] ? (8 * q * p.o_tok + col + 16 * ct) * 2 : kOutside;
   }
   const int last = chunks - 1;
@@ -1298,8 +1305,6 @@ __global__ __launch_bounds__(64 * NW, (kWavesPerSimd<CT, DELTA, OUT>)) void line
   const ChunkArgs pe = arguments_again();
   const Walk we = kept.walk();
   if (LOCAL && tid == 0 && we.cb == 0) pe.seg_log2[we.unit * pe.a.H + we.h] = log2_sum;
-  if (LOCAL && we.first && lane < CT && 16 * (tile0 + lane) < pe.a.dv)
-    pe.seg_bad[(int64_t(we.i) * pe.a.H + we.h) * (pe.a.dv / 16) + tile0 + lane] = 0;
   float* to = we.end<DELTA, LOCAL>(pe, DK);
   const bool segment = !DELTA && pe.seg_chunks;
 #pragma unroll
@@ -1328,10 +1333,10 @@ __global__ __launch_bounds__(64 * NW, (kWavesPerSimd<CT, DELTA, OUT>)) void line
 constexpr int kAhead = 8;
 
 __global__ __launch_bounds__(256) void linear_join_kernel(ChunkArgs p, int dk, bool finish) {
+  __shared__ int bad[16];
   const LinearArgs& a = p.a;
-  const int64_t per = int64_t(dk) * a.dv;
-  const int64_t x = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;     // dv is a multiple of 16
-  if (x >= per) return;
+  const int64_t per = int64_t(dk) * a.dv;                              // a multiple of 1024
+  const int64_t x = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;
   const int h = blockIdx.y, i = blockIdx.z;
   const int segs = segments(p, request_span(a, i).len);
   const int64_t u0 = first_segment(p, i);
@@ -1362,7 +1367,13 @@ __global__ __launch_bounds__(256) void linear_join_kernel(ChunkArgs p, int dk, b
     }
   }
   if (finish) *at(0) = S[0];
-  if (!finite(S)) p.seg_bad[(int64_t(i) * a.H + h) * (a.dv / 16) + x % a.dv / 16] = 1;
+  if (threadIdx.x < 16) bad[threadIdx.x] = 0;
+  __syncthreads();
+  if (!finite(S)) bad[x % a.dv / 16] = 1;
+  __syncthreads();
+  const int tiles = a.dv / 16;
+  if (threadIdx.x < tiles)
+    p.seg_bad[((int64_t(i) * a.H + h) * gridDim.x + blockIdx.x) * tiles + threadIdx.x] = bad[threadIdx.x];
 }
 
 // States alone: the last state from where the join left it, 16 columns a block; or token by token
@@ -1370,7 +1381,7 @@ template <int DK>
 __global__ __launch_bounds__(4 * DK) void linear_finish_kernel(ChunkArgs p) {
   const LinearArgs& a = p.a;
   const int tiles = a.dv / 16, tile = blockIdx.x % tiles, h = blockIdx.x / tiles % a.H, i = blockIdx.x / tiles / a.H;
-  if (p.seg_bad[blockIdx.x]) {
+  if (__syncthreads_or(marked(p, DK, i, h, tile, threadIdx.x))) {
     if (threadIdx.x < 64) walk_tokens<DK, 16, false, false>(a, i, h, 16 * tile, threadIdx.x);
     return;
   }
@@ -1717,7 +1728,7 @@ struct Launch {
     p.seg_log2 = reinterpret_cast<double*>(ws + units * c.H * int64_t(DK) * c.dv * 4);
     p.seg_bad = reinterpret_cast<int32_t*>(p.seg_log2 + units * c.H);
     walk<DK, false, false, true>(kWhole);
-    linear_join_kernel<<<dim3((DK * c.dv + 1023) / 1024, c.H, c.n_req), 256, 0, st>>>(p, DK, !out);
+    linear_join_kernel<<<dim3(DK * c.dv / 1024, c.H, c.n_req), 256, 0, st>>>(p, DK, !out);
     if (out) walk<DK, false, true, false>(kWhole);
     else linear_finish_kernel<DK><<<uint32_t(c.n_req * c.H * (c.dv / 16)), 4 * DK, 0, st>>>(p);
   }
@@ -1742,7 +1753,8 @@ int64_t linear_chunk_workspace(ChunkPlan c) {
     return packet_bytes(c) + (windows ? 2 * int64_t(c.H) * c.dk * c.dv * 4 : 0);
   }
   const int64_t room = segment_room(c);     // segments, and so requests that are split
-  return may_split(c) ? room * c.H * (int64_t(c.dk) * c.dv * 4 + 8 + c.dv / 16 * 4) : 0;
+  const int64_t state = int64_t(c.dk) * c.dv * 4;
+  return may_split(c) ? room * c.H * (state + 8 + state / 4096 * (c.dv / 16) * 4) : 0;
 }
 
 void launch_linear_chunks(const ChunkPlan& c, const LinearArgs& a, void* ws, hipStream_t st) {
