@@ -43,9 +43,10 @@ typedef struct dasc_linear_io {
   int64_t g_tok, g_head, beta_tok, beta_head, o_tok, o_head;
 } dasc_linear_io;
 
-/* Device workspace of dasc_linear_attn for these sizes (0 for many).  It does for every call of this
- * shape with no more requests and tokens than these and none longer, so that one allocation serves
- * an engine's largest batch and all smaller ones.  delta: whether beta is given.  Errors: DASC_E_INVAL (NULL, n_req < 1, n_tokens < 0, max_len < 0), DASC_E_SHAPE. */
+/* Device workspace of dasc_linear_attn for these sizes (0 for many).  It does for every call of
+ * this shape with no more requests and tokens than these and none longer, so that one allocation
+ * serves an engine's largest batch and all smaller ones.  delta: whether beta is given.
+ * Errors: DASC_E_INVAL (NULL, n_req < 1, n_tokens < 0, max_len < 0), DASC_E_SHAPE. */
 int dasc_linear_attn_workspace_bytes(const dasc_shape *shape, int32_t n_req, int64_t n_tokens,
                                      int32_t max_len, int32_t delta, size_t *bytes);
 
@@ -68,7 +69,8 @@ int dasc_linear_attn_workspace_bytes(const dasc_shape *shape, int32_t n_req, int
  *   cu_seqlens: device int32 [n_req + 1], ascending.  lens: device int32 [n_req] or NULL.
  *   max_len: tokens of the longest request, as the caller knows it.  It chooses between the
  *     token-by-token and the chunked form and decides nothing else: results do not depend on it
- *     beyond rounding.
+ *     beyond rounding (and an infinite query's own outputs, infinite in one form, may be NaN in
+ *     the other).
  *   io: q, k, v and o 16-byte aligned, their strides multiples of 8 elements (o and v: of 4);
  *     all strides >= 0.  o must not overlap an input, nor its rows (token, head) each other: they
  *     lie dv or more apart, all heads of a token (or tokens of a head) before the next one's.
@@ -76,16 +78,20 @@ int dasc_linear_attn_workspace_bytes(const dasc_shape *shape, int32_t n_req, int
  *     takes are not written.
  *   workspace: device, at least dasc_linear_attn_workspace_bytes, 16-byte aligned (may be NULL
  *     if that is 0); overlapping calls must not share one.
- * Log-decays may be any value: -inf clears the state, and no product of decays is formed but
- * those the rule has.  What is not finite stays where the rule has it: an infinity or NaN of a token
- * reaches its own and later outputs of its request, heads and columns, no others (an infinite query's own
- * outputs are infinite or NaN).  Heads that share a key head, values and outputs in bf16, states, sums
- * and decays in fp32 (running sums of log-decays in 64 bits); keys and queries are taken as
- * they are.
+ * Log-decays may be any value: -inf clears the state, and a state of zero stays zero whatever it
+ * grows by.  What is not finite stays where the rule has it: an infinity or NaN of a token reaches
+ * its own and later outputs of its request, heads and columns, no others.  Columns that end so, and
+ * heads with log-decays above 0.17, are taken token by token at any length: right, but slow.
+ * Heads may share a key head; keys and queries are taken as they are.
+ * Precision: values and outputs are bf16; states, sums and decays fp32 (running sums of
+ * log-decays 64-bit), and states are as good as fp32 arithmetic makes them.  The chunked form
+ * holds what only an output needs to 16 bits a factor before the output's rounding to bf16: an
+ * output whose terms cancel is good to 2^-14 |scale| |q_t| |column of S'_t|.
  * Errors: DASC_E_INVAL (NULL shape, states, io or cu_seqlens; k, v or g NULL with n_tokens > 0; q
- * NULL with o given; neither o nor dst_slot given with n_tokens > 0; misalignment, a bad stride or rows of o that overlap; layer out of
- * [0, L), n_req < 1, n_tokens < 0 or above 2^31 - 1, max_len < 0, n_pool < 1, scale not finite),
- * DASC_E_SHAPE (bad shape, dv % 4 != 0), DASC_E_WORKSPACE, DASC_E_UNSUPPORTED (arch KDA, whose decay is by channel; dk not in
+ * NULL with o given; neither o nor dst_slot given with n_tokens > 0; misalignment, a bad stride
+ * or rows of o that overlap; layer out of [0, L), n_req < 1, n_tokens < 0 or above 2^31 - 1,
+ * max_len < 0, n_pool < 1, scale not finite), DASC_E_SHAPE (bad shape, dv % 4 != 0),
+ * DASC_E_WORKSPACE, DASC_E_UNSUPPORTED (arch KDA, whose decay is by channel; dk not in
  * {16, 32, 64, 128} or dv > 256), DASC_E_HIP. */
 int dasc_linear_attn(const dasc_shape *shape, int32_t layer, float *states, int64_t n_pool,
                      const int32_t *src_slot, const int32_t *dst_slot, const dasc_linear_io *io,
@@ -100,7 +106,7 @@ int dasc_linear_attn(const dasc_shape *shape, int32_t layer, float *states, int6
 #define DASC_DTYPE_F32  2
 
 /* Device workspace of dasc_verify_drafts: partial sums of each request's row.
- * Errors: DASC_E_INVAL (NULL bytes, n_req < 0, vocab < 1). */
+ * Errors: DASC_E_INVAL (NULL bytes, n_req < 0, vocab < 1), DASC_E_SHAPE (vocab above 2^24). */
 int dasc_verify_drafts_workspace_bytes(int32_t n_req, int64_t vocab, size_t *bytes);
 
 /* Speculative sampling: for each request r, with n = n_draft[r] drafted tokens x_0 .. x_{n-1}

@@ -18,23 +18,29 @@
 // of the matrix, because lane (q, n) then holds rows 8 q .. 8 q + 7 of each group of 32 in the tiles
 // 2 s and 2 s + 1.  Keys as K^T and values as B operands come from LDS through the transposing read.
 //
-// What bounds it, 32 heads of 128 x 128: few heads, the chain of a chunk, 1.7 us with three exchanges
-// through LDS, of which matrix instructions are a fifth (delta rule, 8192 tokens of one request: 229 us
-// and 50 for the factors); many heads, the issue of matrix and vector instructions, 40% of the time each
-// (8 requests of 777 tokens on average: 145 and 26 us; plain rule, 16384 tokens of one request: 265 us in
-// three launches).  Memory traffic would take 42, 35 and 83 us.
+// What bounds it, 32 heads of 128 x 128.  Few heads: the chain of a chunk, 1.7 us with three exchanges
+// through LDS, of which matrix instructions are a fifth (delta rule, 8192 tokens of one request: 224 us
+// and 50 for the factors).  Many heads: a block for each request and head, one on a CU, so the call lasts
+// as long as its longest request (8 requests of 777 tokens on average, of 1300 at most: 148 us, of which a
+// wave lives half on average, and 26 for the factors); in a block, the issue of matrix and vector
+// instructions, 40% of its time each.  The plain rule's segments are of one length and bound by that issue
+// alone (16384 tokens of one request: 80, 8 and 152 us).  Memory traffic would take 42, 35 and 83 us.
 //
 // What is not finite.  T and P are multiplied a block at a time, the zeros above their diagonals with it, and
 // zero times an infinity or NaN is NaN: one such value, key, state or factor reaches the outputs of tokens
 // before it in its chunk.  It also reaches the state, and a state once NaN or infinite is so to the end.  So
 // a walk looks at the last state of its columns, and where that is not finite takes those columns of the
 // request again token by token, from the source slot, which nothing has written yet; the other columns
-// keep theirs.  (A query that is not finite reaches its own outputs alone.)
+// keep theirs.  (A query that is not finite reaches its own outputs alone.)  The look costs 0.3 us a call.
 //
 // Precision.  Keys, queries and values are bf16, products with them are exact.  A 32-bit operand of a
 // sum that reaches the state is cut into three bf16 planes of eight bits each, 24 bits in all, so the
-// state is as good as in fp32 arithmetic (two planes leave 5e-6 of its norm, three 2e-7).  What only
-// the output needs (S in Q S, P, U in P U) has two planes, 16 bits, before its rounding to bf16.
+// state is as good as in fp32 arithmetic (two planes leave 5e-6 of its norm, three 2e-7).  Of T Y, both
+// of whose operands are cut, the products of two lowest planes and of a lowest with a middle one are left
+// out, 2^-24 of the largest.  What only the output needs has 16 bits before its rounding to bf16, 8: S in
+// Q S and U in P U two planes, cut off and so up to 2^-16 towards zero, P two rounded ones, and of P U the
+// product of the two lower planes is left out, 2^-16.  An output whose terms cancel shows it, up to 2^-14 of
+// |scale| |q| |S|.  Decays are the hardware's exponentials, within an ulp.
 
 #include "linear_attn.h"
 
@@ -119,9 +125,11 @@ __device__ inline int64_t uniform(int64_t x) {
 
 __device__ inline int sigma(int t, int m) { return 32 * (t / 2) + 8 * (m / 4) + 4 * (t % 2) + m % 4; }
 
-// Rows in LDS lie 20 (or 12) 16-byte units apart, those of every other group of eight one unit on: the
-// transposing read's four rows of four units meet no bank twice, nor do the eight rows (0 .. 3 and 8 .. 11
-// of one unit) in which a row of A operands is read.  Every address is a lane's base and a constant.
+// Rows in LDS lie 20 (or 12) 16-byte units apart, those of every other group of eight one unit on.  That
+// spreads the transposing read's four rows of four units over the banks, and the eight rows (0 .. 3 and
+// 8 .. 11 of one unit) in which a row of A operands is read.  (Not everything: 19% of the LDS cycles of the
+// split walk and a third of those of the walk by columns are conflicts still; of which accesses is not
+// known.)  Every address is a lane's base and a constant.
 template <int U>
 constexpr int kStride = U + 4;
 template <int U>
@@ -1602,11 +1610,11 @@ struct Segments {
 // suit requests alike, numbers by length suit others; the shorter segments are taken.  A split request
 // costs 3.2 + 5.6 us per chunk of a segment and some 20 us for two launches more and the join, one that
 // is not 1.8 (32 heads or fewer) or 2.7 us (64) per chunk.  us, split | whole:
-//     dk = dv = 128:  4096 tokens x 32 heads  79 | 117    1536 x 32  45 | 48    1024 x 32  40 | 34
-//                     16384 x 4  59 | 405     1024 x 4    24 | 30     640 x 4   22 | 20
-//                     2 of 2048 x 32  80 | 86
-//     dk = dv = 64:   4096 x 16  33 | 91      2048 x 16   25 | 48     1024 x 16  21 | 26
-// The states of 64 segments are joined one after another in 18 us, hence no more.
+//     dk = dv = 128:  4096 tokens x 32 heads  82 | 117    1536 x 32  46 | 48    1024 x 32  40 | 34
+//                     16384 x 4  57 | 405     1024 x 4    24 | 30     640 x 4   22 | 21
+//                     2 of 2048 x 32  79 | 86
+//     dk = dv = 64:   4096 x 16  34 | 91      2048 x 16   25 | 48     1024 x 16  21 | 26
+// The states of 64 segments are joined one after another in 17 us, hence no more.
 constexpr int kMaxSegments = 64;
 
 // Segments, a head's blocks each, that the chip has CUs for; no more are ever made
