@@ -129,7 +129,8 @@ int dasc_verify_drafts_workspace_bytes(int32_t n_req, int64_t vocab, size_t *byt
  *     positions in elements.  Aligned to their element.
  *   draft_tokens: device int32 [n_req, max_draft]; u_accept: device fp32 [n_req, max_draft];
  *     u_sample: device fp32 [n_req]; n_draft: device int32 [n_req] or NULL.
- *   out_tokens: device int32 [n_req, max_draft + 1]; n_emitted: device int32 [n_req].
+ *   out_tokens: device int32 [n_req, max_draft + 1]; n_emitted: device int32 [n_req].  Neither
+ *     may overlap an input.
  * Errors: DASC_E_INVAL (NULL or misaligned pointer, n_req < 0, max_draft < 0, bad dtype or
  * stride), DASC_E_SHAPE (vocab < 1 or above 2^24, max_draft above 1023), DASC_E_WORKSPACE,
  * DASC_E_HIP. */
