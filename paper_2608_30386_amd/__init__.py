@@ -2,10 +2,18 @@
 
 Everything runs in the HIP library libdasc.so (built in-tree by
 ``python paper_2608_30386_amd/build.py``); this package only marshals arguments
-to its C ABI (include/dasc.h, include/dasc/ops.h).  Importing it without the built library raises
+to its C ABI (include/dasc.h, include/dasc/ops.h, include/dasc/cache.h).  Importing it without the built library raises
 ImportError -- there is no CPU fallback.
 """
 
+from .cache import (  # noqa: F401
+    dasc_beam_select,
+    dasc_beam_select_workspace_bytes,
+    dasc_cache_append,
+    dasc_cache_attn,
+    dasc_cache_attn_workspace_bytes,
+    dasc_move_slots,
+)
 from .dasc import (  # noqa: F401
     DascError,
     Shape,

@@ -1,4 +1,4 @@
-"""ctypes declarations of the C ABI in include/dasc.h and include/dasc/ops.h.
+"""ctypes declarations of the C ABI in include/dasc.h, include/dasc/ops.h and include/dasc/cache.h.
 
 Loading fails loudly: if libdasc.so has not been built, importing this module
 raises ImportError.  There is no fallback implementation.
@@ -50,6 +50,10 @@ EXPORTED_OPS = (
     "dasc_linear_attn_workspace_bytes", "dasc_linear_attn", "dasc_verify_drafts_workspace_bytes",
     "dasc_verify_drafts", "dasc_block_norm",
 )
+EXPORTED_CACHE = (
+    "dasc_cache_append", "dasc_cache_attn_workspace_bytes", "dasc_cache_attn",
+    "dasc_beam_select_workspace_bytes", "dasc_beam_select", "dasc_move_slots",
+)
 
 
 class Shape(C.Structure):
@@ -92,6 +96,27 @@ class NormIo(C.Structure):
                                  "xo_out", "xo_in", "h_row_out", "h_row_in", "outer")] + [
         (n, C.c_int32) for n in ("inner", "dim", "dtype", "res_dtype", "w_dtype", "act")] + [
         ("scale", C.c_float), ("eps", C.c_float)]
+
+
+class KvCache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v")] + [
+        (n, C.c_int64) for n in ("k_page", "k_tok", "k_head", "v_page", "v_tok", "v_head", "n_pages")] + [
+        (n, C.c_int32) for n in ("page_size", "n_kv_heads", "head_dim", "dtype")]
+
+
+class AppendIo(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "q_out", "k", "v", "slots", "pos", "inv_freq", "pair_axis")] + [
+        (n, C.c_int64) for n in ("q_tok", "q_head", "qo_tok", "qo_head", "k_tok", "k_head", "v_tok", "v_head",
+                                 "pos_tok", "pos_axis", "n_tokens")] + [
+        (n, C.c_int32) for n in ("n_q_heads", "n_axes", "rot", "adjacent")]
+
+
+class AttnIo(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "o", "lse", "block_table", "cu_seqlens", "kv_lens")] + [
+        (n, C.c_int64) for n in ("q_tok", "q_head", "o_tok", "o_head", "lse_tok", "lse_head", "table_req",
+                                 "n_tokens")] + [
+        (n, C.c_int32) for n in ("n_req", "n_q_heads", "table_width", "max_len", "max_kv", "causal",
+                                 "window")] + [("scale", C.c_float)]
 
 
 def _hip_runtimes() -> set:
@@ -146,6 +171,12 @@ def _load() -> C.CDLL:
         "dasc_verify_drafts": [I32, I32, I64, I32, P, I64, I64, P, I64, I64, P, P, P, P, P, P, P, SZ,
                                P],
         "dasc_block_norm": [P, P],
+        "dasc_cache_append": [P, P, P],
+        "dasc_cache_attn_workspace_bytes": [I32, I64, I32, I32, I32, I32, I32, C.POINTER(C.c_size_t)],
+        "dasc_cache_attn": [P, P, P, SZ, P],
+        "dasc_beam_select_workspace_bytes": [I32, I32, I64, I32, C.POINTER(C.c_size_t)],
+        "dasc_beam_select": [I32, I32, I64, I32, I32, P, I64, I64, P, P, P, P, P, P, P, SZ, P],
+        "dasc_move_slots": [P, I64, I64, I64, P, I64, P, I64, I32, I32, P],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)

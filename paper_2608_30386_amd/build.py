@@ -23,7 +23,7 @@ LIB = os.path.join(PKG, "libdasc.so")
 
 HIP_SOURCES = ["pack_restore.hip", "quant.hip", "refresh.hip", "refresh_wy.hip", "refresh_wy_gdn.hip",
                "refresh_noalloc.hip", "linear_attn.hip", "linear_chunk.hip",
-               "verify.hip", "block_norm.hip"]
+               "verify.hip", "block_norm.hip", "cache_append.hip", "cache_attn.hip", "beam.hip"]
 HOST_SOURCES = ["plan.cpp"]
 ARCH = "gfx950"
 

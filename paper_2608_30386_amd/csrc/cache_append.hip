@@ -1,0 +1,201 @@
+// Append to a paged cache: new queries and keys turned by their positions, keys and values written to
+// their slots.
+//
+// A pair (x, y) of a head turns by angle = pos * inv_freq: (x cos - y sin, x sin + y cos).  The angle of a far
+// position needs more than 24 bits, so its quarter turns are counted in 64-bit arithmetic, and the rest, at
+// most an eighth of a turn, goes through the series of sine and cosine in fp32.
+//
+// A block takes a few tokens: its threads first form the cosines and sines of the tokens' pairs, once for
+// all heads, in LDS, then move the heads in units of eight elements (two of them for pairs that lie apart).
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "cache_common.h"
+#include "launch_common.h"
+#include "output_rows.h"
+#include "row_io.h"
+
+namespace dasc {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxHalf = 128;            // pairs of a head
+constexpr int kMaxTokens = 8;            // of a block
+
+struct AppendArgs {
+  dasc_kv_cache c;
+  dasc_append_io io;
+  int64_t tok0;
+  int32_t tokens;                        // of a block
+  int32_t parts;                         // blocks that share a token's heads
+};
+
+// cos and sin of a quarter turn times x
+__device__ inline void turn(double quarters, float& c, float& s) {
+  const double n = rint(quarters);
+  const float z = float(quarters - n) * 1.57079632679f;      // at most pi / 4
+  const float w = z * z;
+  // Taylor series about 0: the first terms left out are below 2e-9
+  float sn = fmaf(w, 2.7557319e-6f, -1.9841270e-4f);
+  sn = fmaf(w, sn, 8.3333333e-3f);
+  sn = fmaf(w, sn, -1.6666667e-1f);
+  sn = fmaf(z * w, sn, z);
+  float cs = fmaf(w, -2.7557319e-7f, 2.4801587e-5f);
+  cs = fmaf(w, cs, -1.3888889e-3f);
+  cs = fmaf(w, cs, 4.1666667e-2f);
+  cs = fmaf(w, cs, -0.5f);
+  cs = fmaf(w, cs, 1.0f);
+  const double q = n - 4.0 * floor(0.25 * n);                // the quadrant
+  const bool odd = q == 1.0 || q == 3.0;
+  c = odd ? sn : cs;
+  s = odd ? cs : sn;
+  if (q == 1.0 || q == 2.0) c = -c;
+  if (q >= 2.0) s = -s;
+}
+
+template <typename T, int VEC, bool ADJ>
+__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
+  __shared__ float cosine[kMaxTokens * kMaxHalf], sine[kMaxTokens * kMaxHalf];
+  __shared__ int64_t place[kMaxTokens][2];                   // page and place in it; page -1: none
+  const dasc_append_io& io = a.io;
+  const int tid = threadIdx.x, half = io.rot / 2, d = a.c.head_dim;
+  const int64_t t0 = a.tok0 + int64_t(blockIdx.x) * a.tokens;
+  const int n = int(io.n_tokens - t0 < a.tokens ? io.n_tokens - t0 : a.tokens);
+  if (tid < n) {
+    const int64_t slot = io.slots[t0 + tid];
+    const bool in = slot >= 0 && slot / a.c.page_size < a.c.n_pages;
+    place[tid][0] = in ? slot / a.c.page_size : -1;
+    place[tid][1] = in ? slot % a.c.page_size : 0;
+  }
+  for (int i = tid; i < n * half; i += kThreads) {
+    const int t = i / half, p = i % half;
+    const int axis = io.pair_axis ? io.pair_axis[p] : 0;
+    float c = 1.0f, s = 0.0f;
+    if (axis >= 0 && axis < io.n_axes)
+      turn(double(io.pos[(t0 + t) * io.pos_tok + axis * io.pos_axis]) * double(io.inv_freq[p]) * 0.63661977236758134308,
+           c, s);
+    cosine[i] = c;
+    sine[i] = s;
+  }
+  __syncthreads();
+  // units of a head of q or k: those of pairs, then those of elements that stay; of v: elements
+  const int turned = ADJ ? io.rot / (2 * VEC) : half / VEC;
+  const int units = turned + (d - io.rot) / VEC, plain = d / VEC;
+  const int hq = io.q ? io.n_q_heads : 0, hk = a.c.n_kv_heads;
+  const int per = (hq + hk) * units + hk * plain;            // of a token
+  for (int i = blockIdx.y * kThreads + tid; i < n * per; i += a.parts * kThreads) {
+    const int t = i / per;
+    int u = i - t * per;
+    const int64_t tok = t0 + t, page = place[t][0], off = place[t][1];
+    const T* src;
+    T* dst;
+    bool v = false;
+    if (u < hq * units) {
+      const int h = u / units;
+      u -= h * units;
+      src = static_cast<const T*>(io.q) + tok * io.q_tok + h * io.q_head;
+      dst = static_cast<T*>(io.q_out) + tok * io.qo_tok + h * io.qo_head;
+    } else {
+      if (page < 0) continue;
+      u -= hq * units;
+      v = u >= hk * units;
+      if (v) u -= hk * units;
+      const int per_head = v ? plain : units, h = u / per_head;
+      u -= h * per_head;
+      src = v ? static_cast<const T*>(io.v) + tok * io.v_tok + h * io.v_head
+              : static_cast<const T*>(io.k) + tok * io.k_tok + h * io.k_head;
+      dst = v ? static_cast<T*>(a.c.v) + page * a.c.v_page + off * a.c.v_tok + h * a.c.v_head
+              : static_cast<T*>(a.c.k) + page * a.c.k_page + off * a.c.k_tok + h * a.c.k_head;
+    }
+    typedef Vec<T, VEC> V;
+    if (v || u >= turned) {
+      const int at = v ? u * VEC : io.rot + (u - turned) * VEC;
+      *reinterpret_cast<V*>(dst + at) = *reinterpret_cast<const V*>(src + at);
+      continue;
+    }
+    const int p = u * VEC;                                   // the first pair
+    const int x0 = ADJ ? 2 * p : p, y0 = ADJ ? 2 * p + VEC : p + half;
+    V x = *reinterpret_cast<const V*>(src + x0), y = *reinterpret_cast<const V*>(src + y0);
+    float f[2 * VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) f[e] = widen(x.e[e]);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) f[VEC + e] = widen(y.e[e]);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const int lo = ADJ ? 2 * e : e, hi = ADJ ? 2 * e + 1 : e + VEC;
+      const float c = cosine[t * half + p + e], s = sine[t * half + p + e], g = f[lo], h = f[hi];
+      f[lo] = fmaf(g, c, -(h * s));
+      f[hi] = fmaf(g, s, h * c);
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) narrow(f[e], x.e[e]);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) narrow(f[VEC + e], y.e[e]);
+    *reinterpret_cast<V*>(dst + x0) = x;
+    *reinterpret_cast<V*>(dst + y0) = y;
+  }
+}
+
+template <typename T, int VEC, bool ADJ>
+void launch(AppendArgs a, hipStream_t st) {
+  constexpr int64_t kBlocks = int64_t(1) << 20;
+  const int heads = (a.io.q ? a.io.n_q_heads : 0) + 2 * a.c.n_kv_heads;
+  a.tokens = 1;
+  const int work = heads * a.c.head_dim / VEC;
+  a.parts = (work + 4 * kThreads - 1) / (4 * kThreads);
+  if (a.parts > 32) a.parts = 32;
+  for (; a.tok0 < a.io.n_tokens; a.tok0 += kBlocks * a.tokens) {
+    const int64_t left = (a.io.n_tokens - a.tok0 + a.tokens - 1) / a.tokens;
+    append_kernel<T, VEC, ADJ><<<dim3(uint32_t(left < kBlocks ? left : kBlocks), a.parts), kThreads, 0, st>>>(a);
+  }
+}
+
+template <typename T>
+void launch_type(const AppendArgs& a, hipStream_t st) {
+  const bool adj = a.io.adjacent != 0;
+  const int rot = a.io.rot;
+  if (rot % 16 == 0) adj ? launch<T, 8, true>(a, st) : launch<T, 8, false>(a, st);
+  else adj ? launch<T, 1, true>(a, st) : launch<T, 1, false>(a, st);
+}
+
+}  // namespace
+}  // namespace dasc
+
+extern "C" int dasc_cache_append(const dasc_kv_cache* cache, const dasc_append_io* io, dasc_stream_t stream) {
+  using namespace dasc;
+  const int rc = check_cache(cache, 2);
+  if (rc != DASC_OK) return rc;
+  if (!io) return DASC_E_INVAL;
+  const dasc_kv_cache& c = *cache;
+  if (io->rot < 0 || io->rot % 2 || io->rot > c.head_dim || io->n_axes < 1 || io->n_axes > 8 || io->n_tokens < 0 ||
+      io->n_tokens > INT32_MAX || (io->q && (io->n_q_heads < 1 || io->n_q_heads > 65536)))
+    return DASC_E_SHAPE;
+  if (io->adjacent != 0 && io->adjacent != 1) return DASC_E_INVAL;
+  if (!rows_apart3(c.n_pages, c.k_page, c.page_size, c.k_tok, c.n_kv_heads, c.k_head, c.head_dim) ||
+      !rows_apart3(c.n_pages, c.v_page, c.page_size, c.v_tok, c.n_kv_heads, c.v_head, c.head_dim))
+    return DASC_E_INVAL;
+  if (io->n_tokens == 0) return DASC_OK;
+  if (!io->k || !io->v || !io->slots || (io->q != nullptr) != (io->q_out != nullptr)) return DASC_E_INVAL;
+  if (io->rot > 0 && (!io->pos || !io->inv_freq)) return DASC_E_INVAL;
+  if (!aligned_to(io->q, 2) || !aligned_to(io->q_out, 2) || !aligned_to(io->k, 2) || !aligned_to(io->v, 2) ||
+      !aligned_to(io->slots, 8) || !aligned_to(io->pos, 4) || !aligned_to(io->inv_freq, 4) ||
+      !aligned_to(io->pair_axis, 4))
+    return DASC_E_INVAL;
+  if (io->k_tok < 0 || io->k_head < 0 || io->v_tok < 0 || io->v_head < 0 || io->pos_tok < 0 || io->pos_axis < 0)
+    return DASC_E_INVAL;
+  if (io->q && (io->q_tok < 0 || io->q_head < 0 ||
+                !rows_apart(io->n_tokens, io->qo_tok, io->n_q_heads, io->qo_head, c.head_dim)))
+    return DASC_E_INVAL;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  AppendArgs a;
+  a.c = c;
+  a.io = *io;
+  a.tok0 = 0;
+  if (c.dtype == DASC_DTYPE_BF16) launch_type<bf16_t>(a, st);
+  else launch_type<f16_t>(a, st);
+  return launch_status();
+}

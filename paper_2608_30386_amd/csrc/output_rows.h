@@ -17,4 +17,27 @@ inline bool rows_apart(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t w
   return lo >= width && hi / n >= lo;           // hi >= n lo, without the product
 }
 
+// The same for n0 x n1 x n2 rows: in order of their strides, each kind as a whole within the next.
+inline bool rows_apart3(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2, int64_t s2, int64_t width) {
+  int64_t n[3] = {n0, n1, n2}, s[3] = {s0, s1, s2};
+  for (int i = 0; i < 3; ++i) {
+    if (s[i] < 0) return false;
+    if (n[i] == 0) return true;
+  }
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2 - i; ++j)
+      if (s[j] > s[j + 1]) {
+        const int64_t ts = s[j], tn = n[j];
+        s[j] = s[j + 1], n[j] = n[j + 1];
+        s[j + 1] = ts, n[j + 1] = tn;
+      }
+  int64_t span = width;                         // that the rows so far take
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] == 1) continue;
+    if (s[i] < span || s[i] > INT64_MAX / n[i]) return false;
+    span = s[i] * n[i];
+  }
+  return true;
+}
+
 }  // namespace dasc

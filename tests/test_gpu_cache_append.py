@@ -1,0 +1,186 @@
+"""The append to a paged cache against its formulas in 64 bits (GPU).
+
+Tolerance: x cos - y sin with cosine and sine good to 2^-22, two products and a sum in fp32 (2^-24 each of
+at most |x| + |y|), rounded once to the output's type by at most half a step, eps / 2 of the value:
+    eps / 2 |want| + (2^-22 + 2^-23) (|x| + |y|), and 2^-25 where fp16 ends.
+Everything that the call does not name stays as it was, bit by bit.
+"""
+
+import numpy as np
+import pytest
+
+import paper_2608_30386_amd as D
+from oracle import cache as OC
+from tests.gpu_util import announce
+
+pytestmark = pytest.mark.gpu
+
+
+def bits(t):
+    import torch
+
+    return t.contiguous().view(torch.int16).cpu().numpy()
+
+
+def case(dtype="bfloat16", n=5, hq=4, hkv=2, d=64, rot=64, page=16, heads_first=False, axes=1, adjacent=False, seed=0,
+         far=0, slots=None, pages=None, pair_axis=None, wide=False):
+    import torch
+
+    g = torch.Generator("cuda").manual_seed(seed)
+    dt = getattr(torch, dtype)
+    pages = pages or n // page + 3
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=g).to(dt)  # noqa: E731
+    kc, vc = (rnd(pages, hkv, page, d).transpose(1, 2) if heads_first else rnd(pages, page, hkv, d) for _ in range(2))
+    x = rnd(n, (hq + 2 * hkv) * d + (3 if wide else 0))[:, 3 if wide else 0:]
+    q, k, v = (x[:, a * d:b * d].unflatten(1, (b - a, d)) for a, b in ((0, hq), (hq, hq + hkv), (hq + hkv, hq + 2 * hkv)))
+    rng = np.random.default_rng(seed)
+    if slots is None:
+        slots = rng.permutation(pages * page)[:n]
+    pos = far + rng.integers(0, 5000, (n, axes))
+    inv = (1e4 ** (-np.arange(rot // 2) / max(1, rot // 2))).astype(np.float32)
+    if pair_axis is None and axes > 1:
+        pair_axis = rng.integers(0, axes, rot // 2)
+    return dict(kc=kc, vc=vc, q=q, k=k, v=v, slots=np.asarray(slots), pos=pos, inv=inv, axis=pair_axis,
+                adjacent=adjacent, dt=dt)
+
+
+def call(c, q_out="new", **over):
+    import torch
+
+    dev = lambda a, t: None if a is None else torch.tensor(np.asarray(a), dtype=t, device="cuda")  # noqa: E731
+    out = torch.empty(c["q"].shape, dtype=c["dt"], device="cuda") if q_out == "new" else q_out
+    rot = len(c["inv"]) > 0
+    D.dasc_cache_append(c["kc"], c["vc"], dev(c["slots"], torch.int64), c["k"], c["v"], q=c["q"], q_out=out,
+                        pos=dev(c["pos"], torch.int32) if rot else None, inv_freq=dev(c["inv"], torch.float32) if rot else None,
+                        pair_axis=dev(c["axis"], torch.int32), adjacent=c["adjacent"], **over)
+    torch.cuda.synchronize()
+    return out
+
+
+def near(got, x, c, dtype, rows=slice(None)):
+    import torch
+
+    x = x.double().cpu().numpy()
+    want = OC.rotate(x, c["pos"][rows], c["inv"], c["axis"], c["adjacent"])
+    half = len(c["inv"])
+    size = np.abs(x).copy()
+    lo, hi = (slice(0, 2 * half, 2), slice(1, 2 * half, 2)) if c["adjacent"] else (slice(0, half), slice(half, 2 * half))
+    both = np.abs(x[..., lo]) + np.abs(x[..., hi])
+    size[..., lo], size[..., hi] = both, both
+    tol = torch.finfo(c["dt"]).eps / 2 * np.abs(want) + (2.0 ** -22 + 2.0 ** -23) * size
+    if dtype == "float16":
+        tol = tol + 2.0 ** -25
+    err = np.abs(got.double().cpu().numpy() - want)
+    assert (err <= tol).all(), (err / tol).max()
+    rest = x[..., 2 * half:]
+    np.testing.assert_array_equal(got.double().cpu().numpy()[..., 2 * half:], rest)
+
+
+def check(c, dtype, q_out="new"):
+    import torch
+
+    kc0, vc0 = c["kc"].clone(), c["vc"].clone()
+    q0 = c["q"].clone()
+    out = call(c, q_out)
+    near(out, q0, c, dtype)
+    page, n_pages = c["kc"].shape[1], c["kc"].shape[0]
+    on = np.nonzero((c["slots"] >= 0) & (c["slots"] < page * n_pages))[0]
+    at = torch.tensor(c["slots"][on], device="cuda")
+    rows = torch.tensor(on, device="cuda")
+    near(c["kc"][at // page, at % page], c["k"][rows], c, dtype, on)
+    np.testing.assert_array_equal(bits(c["vc"][at // page, at % page]), bits(c["v"][rows]))
+    kc1, vc1 = c["kc"].clone(), c["vc"].clone()
+    kc1[at // page, at % page] = kc0[at // page, at % page]
+    vc1[at // page, at % page] = vc0[at // page, at % page]
+    np.testing.assert_array_equal(bits(kc1), bits(kc0))
+    np.testing.assert_array_equal(bits(vc1), bits(vc0))
+
+
+CASES = [
+    dict(n=1), dict(n=5, hq=1, hkv=1, d=8, rot=8, page=1), dict(n=33, d=128, rot=128, hq=7, hkv=1, page=24),
+    dict(n=70, d=256, rot=64, hq=16, hkv=2), dict(n=9, d=96, rot=24, hq=3, hkv=3), dict(n=9, d=40, rot=6, hq=3, hkv=1),
+    dict(n=9, d=64, rot=2), dict(n=9, d=64, rot=0), dict(n=300, d=64, rot=32, axes=3, heads_first=True),
+    dict(n=20, d=72, rot=72, axes=2, wide=True), dict(n=17, d=128, rot=128, wide=True, heads_first=True),
+    dict(n=40, d=128, rot=128, far=2 ** 31 - 6000), dict(n=40, d=64, rot=64, far=-4000),
+    dict(n=3, hq=40, hkv=40, d=256, rot=256, page=3),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("c", CASES, ids=lambda c: "-".join(f"{k}{v}" for k, v in c.items()))
+def test_append(c, adjacent, dtype):
+    announce(f"append {c} {dtype} adjacent {adjacent}")
+    check(case(dtype=dtype, adjacent=adjacent, seed=len(c), **c), dtype)
+
+
+def test_slots_outside_the_cache_and_axes_outside_the_positions():
+    announce("append: slots and axes out of range")
+    check(case(n=6, slots=[-1, 3, 10 ** 12, 20, -2 ** 62, 3 * 16], pages=3, axes=2,
+               pair_axis=[0, 1, 2, -1] * 8), "bfloat16")
+
+
+def test_queries_in_place_and_keys_alone():
+    import torch
+
+    announce("append: in place")
+    c = case(n=50, hq=8)
+    check(c, "bfloat16", q_out=c["q"])
+    c, e = case(n=50, seed=3), case(n=50, seed=3)
+    call(c)
+    c["q"] = None
+    D.dasc_cache_append(e["kc"], e["vc"], torch.tensor(e["slots"], device="cuda"), e["k"], e["v"],
+                        pos=torch.tensor(e["pos"], dtype=torch.int32, device="cuda"),
+                        inv_freq=torch.tensor(e["inv"], device="cuda"))
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(bits(c["kc"]), bits(e["kc"]))
+    np.testing.assert_array_equal(bits(c["vc"]), bits(e["vc"]))
+
+
+def test_pages_of_two_layers_side_by_side_beyond_32_bits():
+    """A slot whose offset passes 2^32 elements, in a cache whose pages hold two layers."""
+    import torch
+
+    announce("append: offsets beyond 32 bits")
+    pages = 2 ** 21 // 16 + 9
+    both = torch.zeros(pages, 2, 2, 16, 2, 512, dtype=torch.bfloat16, device="cuda")    # layer, k or v
+    n = 4
+    c = case(n=n, hq=2, hkv=2, d=256, rot=256, slots=[pages * 16 - 1, 0, pages * 16 - 20, -1], pages=2)
+    c["kc"], c["vc"] = both[:, 1, 0, :, :, :256], both[:, 1, 1, :, :, :256]
+    call(c)
+    for i in (0, 1, 2):
+        p, t = divmod(int(c["slots"][i]), 16)
+        near(both[p, 1, 0, t, :, :256][None], c["k"][i:i + 1], c, "bfloat16", [i])
+        assert torch.equal(both[p, 1, 1, t, :, :256], c["v"][i])
+    assert int((both != 0).any(-1).sum()) == 3 * 2 * 2
+
+
+def test_empty_other_stream_and_graph():
+    import torch
+
+    announce("append: empty call, stream, graph")
+    c = case(n=5)
+    e = dict(c, q=c["q"][:0], k=c["k"][:0], v=c["v"][:0], slots=c["slots"][:0], pos=c["pos"][:0])
+    call(e)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    want = call(c)
+    np.testing.assert_array_equal(bits(call(c, stream=s)), bits(want))
+    slots = torch.tensor(c["slots"], device="cuda")
+    pos, inv = torch.tensor(c["pos"], dtype=torch.int32, device="cuda"), torch.tensor(c["inv"], device="cuda")
+    out = torch.empty_like(want)
+    run = lambda: D.dasc_cache_append(c["kc"], c["vc"], slots, c["k"], c["v"], q=c["q"], q_out=out, pos=pos,  # noqa: E731
+                                      inv_freq=inv)
+    run()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run()
+    for i in range(3):
+        pos.add_(1)
+        g.replay()
+        got, keys = out.clone(), c["kc"].clone()
+        run()
+        torch.cuda.synchronize()
+        np.testing.assert_array_equal(bits(got), bits(out))
+        np.testing.assert_array_equal(bits(keys), bits(c["kc"]))
