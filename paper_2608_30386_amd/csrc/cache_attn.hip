@@ -27,6 +27,15 @@
 #include "output_rows.h"
 #include "wy_ops.h"
 
+#ifndef DASC_WQ256
+#define DASC_SIMD256 1
+#define DASC_WQ256 4
+#define DASC_SIMD128 2
+#define DASC_WQ128 8
+#define DASC_SIMD64 2
+#define DASC_WQ64 8
+#endif
+
 namespace dasc {
 namespace {
 
@@ -64,6 +73,12 @@ __device__ inline bool odd_value(u32x4 v) {
 
 // See the note on waits in linear_chunk.hip: results of matrix instructions that cross a branch
 __device__ inline void settle(f32x16& x) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(x)); }
+template <int N>
+__device__ inline void settle(f32x16 (&x)[N]) {
+  settle(x[0]);
+#pragma unroll
+  for (int i = 1; i < N; ++i) asm volatile("" : "+v"(x[i]));
+}
 
 // ---- work -------------------------------------------------------------------------------------
 
@@ -76,6 +91,7 @@ struct AttnArgs {
   dasc_kv_cache c;
   dasc_attn_io io;
   Divisor group, page;
+  uint32_t k_page, k_tok, v_page, v_tok;  // the cache's strides of pages and tokens
   int32_t index0;                         // first piece of this launch
   int32_t target;                         // pieces of a key head to aim at
   int32_t split;                          // whether tiles may be split
@@ -168,7 +184,7 @@ __device__ inline bool locate(const AttnArgs& a, int index, Piece& p) {
   return false;
 }
 
-// ---- the kernel ---------------------------------------------------------------------------------
+// ---- what the kernels share -----------------------------------------------------------------------
 
 // WQ waves of 32 rows each, WK of them on the same rows with KW keys each; D: head_dim rounded up
 template <typename T, int D, int WQ, int WK, int KW>
@@ -179,10 +195,14 @@ struct Form {
   static constexpr int kLoads = kKeys * kChunks / kThreads;   // of a thread, keys and values each
   static constexpr int kRowBytes = 2 * D;
   static constexpr int kKv = kKeys * kRowBytes;
-  static constexpr int kScratch = kWaves * 16 * 32 * 4;       // weights of 16 keys a wave
   static constexpr int kMerge = WK > 1 ? (WK - 1) * WQ * 32 * (D + 2) * 4 : 0;
-  static constexpr int kLds = 2 * kKv + kScratch > kMerge ? 2 * kKv + kScratch : kMerge;
 };
+
+// Tiles of many rows: waves of 32 rows each, waves of a SIMD, keys of a step
+constexpr int wide_wq(int D) { return D == 256 ? DASC_WQ256 : D == 128 ? DASC_WQ128 : DASC_WQ64; }
+constexpr int wide_simd(int D) { return D == 256 ? DASC_SIMD256 : D == 128 ? DASC_SIMD128 : DASC_SIMD64; }
+constexpr int wide_keys(int D) { return D == 256 ? 32 : 64; }
+constexpr int few_keys(int D, int wk) { return 32 * wk; }
 
 // Where 16-byte chunk c of row r lies: lanes of a read that take the same chunk of many rows (keys), or a few
 // chunks of four rows (values), meet different banks
@@ -192,72 +212,406 @@ __device__ inline int value_chunk(int r, int c) {
   return D == 64 ? c ^ ((r >> 1 & 1) << 2) : c ^ ((r & 3) << 2);
 }
 
+// The positions that token t of the request sees: lo .. hi
+struct Sight { int lo, hi; };
+__device__ inline Sight sight(const AttnArgs& a, const Piece& p, int t) {
+  const int64_t here = int64_t(p.kv) - p.len + t;
+  const int64_t hi = a.io.causal && here < p.kv - 1 ? here : p.kv - 1;
+  const int64_t lo = a.io.window > 0 && here - a.io.window >= 0 ? here - a.io.window + 1 : 0;
+  return {int(lo > INT32_MAX ? INT32_MAX : lo), int(hi < -1 ? -1 : hi)};
+}
+
+// A lane's row of a tile
+struct Row {
+  bool real;               // not one that pads the tile
+  int tok;                 // token of the request
+  int64_t qh;              // query head
+  int lo, hi;              // positions that it sees (a row that pads the tile: all)
+  int all_lo, all_hi;      // positions that every row of the wave sees
+};
+__device__ inline Row row_of(const AttnArgs& a, const Piece& p, int head, int r) {
+  Row x;
+  const int row = p.row0 + r, G = a.group.d;
+  x.real = r < p.rows;
+  x.tok = x.real ? int(a.group.of(row)) : 0;
+  x.qh = int64_t(head) * G + (x.real ? row - x.tok * G : 0);
+  const Sight s = sight(a, p, x.tok);
+  x.lo = x.real ? s.lo : 0;
+  x.hi = x.real ? s.hi : INT32_MAX;
+  x.all_lo = x.lo;
+  x.all_hi = x.hi;
+#pragma unroll
+  for (int i = 1; i < 32; i *= 2) {
+    const int lo = __shfl_xor(x.all_lo, i), hi = __shfl_xor(x.all_hi, i);
+    x.all_lo = lo > x.all_lo ? lo : x.all_lo;
+    x.all_hi = hi < x.all_hi ? hi : x.all_hi;
+  }
+  x.all_lo = __builtin_amdgcn_readfirstlane(x.all_lo);
+  x.all_hi = __builtin_amdgcn_readfirstlane(x.all_hi);
+  return x;
+}
+
+// The operand Q of a lane's row: channels 16 s + 8 half + {0..7} of each step s
+template <typename T, int D>
+__device__ inline void load_query(const AttnArgs& a, const Piece& p, const Row& row, int half, typename T::x8 (&q)[D / 16]) {
+  const auto* at = static_cast<const typename T::elem*>(a.io.q) + (int64_t(p.tok0) + row.tok) * a.io.q_tok + row.qh * a.io.q_head;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    const int c = 16 * s + 8 * half;
+    u32x4 v = {0, 0, 0, 0};
+    if (row.real && c < a.c.head_dim) v = *reinterpret_cast<const u32x4*>(at + c);
+    q[s] = __builtin_bit_cast(typename T::x8, v);
+  }
+}
+
+// Key of element e of score tile t, from the wave's first
+__device__ inline int key_at(int t, int e, int half) { return t * 32 + 8 * (e / 4) + 4 * half + e % 4; }
+
+// A lane's places in LDS.  Chunk 2 i + half of row n lies at key[i % 4] + (i / 4) * 128, and of the rows that step
+// 16 u of the keys takes the columns of tile i at value[i % 4] + (i / 4) * 256 (D = 64: value[i]), for rows
+// that are multiples of 32 (keys) and 16 (values) apart swap the same chunks.
+struct Places { int key[4], value[4]; };
+template <int D>
+__device__ inline Places places_of(int lane) {
+  Places x;
+  const int n = lane % 32, half = lane / 32, r = 4 * half + lane % 16 / 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x.key[i] = n * 2 * D + key_chunk(n, 2 * i + half) * 16;
+    const int c = i * 32 + lane % 32 / 16 * 16 + lane % 4 * 4;
+    x.value[i] = r * 2 * D + value_chunk<D>(r, c / 8) * 16 + c % 8 * 2;
+  }
+  return x;
+}
+
+// Nothing moves across.  Left alone, the compiler waits for each operand right before its product, an LDS access's
+// time each; so the order of reads, products and arithmetic in the inner loops is the one that is written.
+__device__ inline void hold() { __builtin_amdgcn_sched_barrier(0); }
+
+// S^T = K Q^T of NS tiles of 32 keys, four operands on their way
+template <typename T, int D, int NS>
+__device__ inline void scores(const char* lk, const Places& at, const typename T::x8 (&q)[D / 16], f32x16 (&s)[NS]) {
+  constexpr int kSteps = D / 16, kAhead = 4;
+  const auto read = [&](int j) {
+    const int t = j / kSteps, i = j % kSteps;
+    return *reinterpret_cast<const typename T::x8*>(lk + at.key[i % 4] + t * 64 * D + i / 4 * 128);
+  };
+  typename T::x8 k[kAhead];
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) k[j] = read(j);
+#pragma unroll
+  for (int t = 0; t < NS; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[t][e] = 0;
+  hold();
+#pragma unroll
+  for (int j = 0; j < NS * kSteps; ++j) {
+    s[j / kSteps] = T::mfma(k[j % kAhead], q[j % kSteps], s[j / kSteps]);
+    if (j + kAhead < NS * kSteps) k[j % kAhead] = read(j + kAhead);
+    hold();
+  }
+}
+
+// Scores that are not seen become -inf.  have: the positions of the wave that have a page.
+template <int NS>
+__device__ inline void hide(f32x16 (&s)[NS], int half, int key0, uint64_t have, const Row& row) {
+  constexpr uint64_t kAll = NS == 2 ? ~uint64_t(0) : (uint64_t(1) << 32) - 1;
+  if (have == kAll && key0 >= row.all_lo && key0 + NS * 32 - 1 <= row.all_hi) return;
+  settle(s);
+#pragma unroll
+  for (int t = 0; t < NS; ++t) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int i = key_at(t, e, half);
+      s[t][e] = (have >> i & 1) && key0 + i >= row.lo && key0 + i <= row.hi ? s[t][e] : -__builtin_inff();
+    }
+  }
+}
+
+// The row's running base m of the weights 2^(s - m), sum l (of this half's keys) and output O, before scores
+// with maximum `top` (of this half's) join them.  The base follows the maximum only where that has left it by more
+// than 2^8 in some row: weights up to 2^8 lose nothing, and most steps leave O alone.
+template <int NO>
+__device__ inline void rebase(float top, float scale2, float& m, float& l, f32x16 (&o)[NO]) {
+  top = fmaxf(top, __shfl_xor(top, 32)) * scale2;
+  if (__any(top > m + 8.0f)) {
+    const float next = fmaxf(m, top);
+    const float shrink = __builtin_amdgcn_exp2f(m - (next > -__builtin_inff() ? next : 0.0f));
+    m = next;
+    l *= shrink;
+    settle(o);
+#pragma unroll
+    for (int i = 0; i < NO; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[i][e] *= shrink;
+  }
+}
+template <int NS, int NO>
+__device__ inline void rebase(f32x16 (&s)[NS], float scale2, float& m, float& l, f32x16 (&o)[NO]) {
+  settle(s);
+  float top = -__builtin_inff();
+#pragma unroll
+  for (int t = 0; t < NS; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
+  rebase(top, scale2, m, l, o);
+}
+
+// Scores to weights, eight keys of each half: rounded to the type as an operand, their sum in fp32
+template <typename T, int NS>
+__device__ inline typename T::x8 weights(const f32x16 (&s)[NS], int t, int u, float scale2, float base, float& l) {
+  typename T::x8 w;
+  float x[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(s[t][8 * u + e], scale2, -base));
+#pragma unroll
+  for (int e = 0; e < 8; ++e) w[e] = typename T::elem(x[e]);
+  l += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+  return w;
+}
+__device__ inline float base_of(float m) { return m > -__builtin_inff() ? m : 0.0f; }
+
+// V^T of 16 keys from row r0 (a multiple of 16) of lv, columns 32 i ..
+template <typename T, int D>
+__device__ inline typename T::x8 value_operand(const char* lv, const Places& at, int r0, int i) {
+  union { s16x4 h[2]; typename T::x8 v; } x;
+  const char* p = lv + at.value[i % 4] + r0 * 2 * D + i / 4 * 256;
+  x.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
+  x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * D));
+  return x.v;
+}
+
+// O^T += V^T P^T.  The weights of 16 keys are formed while the products of the 16 before run.
+template <typename T, int D, int NS>
+__device__ inline void values(const char* lv, const Places& at, const f32x16 (&s)[NS], float scale2, float m, float& l,
+                              f32x16 (&o)[D / 32]) {
+  constexpr int kDt = D / 32, kGroups = NS * 2, kAhead = 4, kSlice = 8 / kDt;
+  const auto read = [&](int j) { return value_operand<T, D>(lv, at, j / kDt * 16, j % kDt); };
+  typename T::x8 v[kAhead], w, next;
+  const float base = base_of(m);
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) v[j] = read(j);
+  w = weights<T>(s, 0, 0, scale2, base, l);
+  hold();
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) {
+#pragma unroll
+    for (int i = 0; i < kDt; ++i) {
+      const int j = g * kDt + i;
+      o[i] = T::mfma(v[j % kAhead], w, o[i]);
+      if (j + kAhead < kGroups * kDt) v[j % kAhead] = read(j + kAhead);
+      if (g + 1 < kGroups) {
+        float sum = 0;
+#pragma unroll
+        for (int e = i * kSlice; e < (i + 1) * kSlice; ++e) {
+          const float x = __builtin_amdgcn_exp2f(fmaf(s[(g + 1) / 2][8 * ((g + 1) % 2) + e], scale2, -base));
+          next[e] = typename T::elem(x);
+          sum += x;
+        }
+        l += sum;
+      }
+      hold();
+    }
+    w = next;
+  }
+}
+
+// The same where a value that some rows do not see is not finite.  Such values count as 0 in the product, and
+// another product counts, for each row and column, those that the row sees: infinities in ones, negative ones
+// in 128s, NaN in 16384s.  They are added after.
+template <typename T, int D, int NS>
+__device__ inline void careful(const char* lv, const Places& at, int half, int key0, uint64_t have, const Row& row,
+                               const f32x16 (&s)[NS], float scale2, float m, float& l, f32x16 (&o)[D / 32]) {
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  typedef typename T::x8 x8;
+  const short top = short(T::kExp & 0xFFFFu);
+  x8 all[NS][2];
+#pragma unroll
+  for (int t = 0; t < NS; ++t)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) all[t][u] = weights<T>(s, t, u, scale2, base_of(m), l);
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+    f32x16 odd;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) odd[e] = 0;
+#pragma unroll
+    for (int t = 0; t < NS; ++t)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        __builtin_amdgcn_sched_barrier(0);
+        const s16x8 v = __builtin_bit_cast(s16x8, value_operand<T, D>(lv, at, t * 32 + u * 16, i));
+        s16x8 fine;
+        x8 kind, seen;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int k = key_at(t, 8 * u + e, half);
+          const bool in = (have >> k & 1) && key0 + k >= row.lo && key0 + k <= row.hi, is = (v[e] & top) == top;
+          seen[e] = typename T::elem(in ? 1.0f : 0.0f);
+          fine[e] = is ? short(0) : v[e];
+          kind[e] = typename T::elem(!is ? 0.0f : v[e] == top ? 1.0f : v[e] == short(top | 0x8000) ? 128.0f : 16384.0f);
+        }
+        o[i] = T::mfma(__builtin_bit_cast(x8, fine), all[t][u], o[i]);
+        odd = T::mfma(kind, seen, odd);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+    settle(o[i]);
+    settle(odd);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int n = int(odd[e]);
+      const float inf = __builtin_inff();
+      o[i][e] += ((n & 127) ? inf : 0.0f) + ((n >> 7 & 127) ? -inf : 0.0f) + (n >> 14 ? __builtin_nanf("") : 0.0f);
+    }
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// A row's result: to the workspace if its tile is split, else to the output
+template <typename T, int D>
+__device__ inline void write_row(const AttnArgs& a, const Piece& p, const Row& row, int64_t slot, int half, float m,
+                                 float l, const f32x16 (&o)[D / 32]) {
+  if (!row.real) return;
+  if (p.splits > 1) {
+    if (half == 0) {
+      a.ml[slot * 2] = m;
+      a.ml[slot * 2 + 1] = l;
+    }
+    float* out = a.part + slot * D;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        *reinterpret_cast<float4*>(out + i * 32 + 8 * b + 4 * half) =
+            make_float4(o[i][4 * b], o[i][4 * b + 1], o[i][4 * b + 2], o[i][4 * b + 3]);
+    return;
+  }
+  typedef typename T::elem elem;
+  typedef elem e4 __attribute__((ext_vector_type(4)));
+  const int64_t t = int64_t(p.tok0) + row.tok;
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  elem* out = static_cast<elem*>(a.io.o) + t * a.io.o_tok + row.qh * a.io.o_head;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const int c = i * 32 + 8 * b + 4 * half;
+      e4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = elem(o[i][4 * b + e] * inv);
+      if (c < a.c.head_dim) *reinterpret_cast<e4*>(out + c) = x;
+    }
+  if (a.io.lse && half == 0) a.io.lse[t * a.io.lse_tok + row.qh * a.io.lse_head] = m * 0.69314718056f + logf(l);
+}
+
+// The block's piece; false if there is none.  The first block of a split tile says so to those that join.
+template <int ROWS, int KEYS>
+__device__ inline bool take_piece(const AttnArgs& a, int head, int index, Piece& p) {
+  const bool any = locate<ROWS, KEYS>(a, index, p);
+  if (a.split && head == 0 && threadIdx.x == 0)
+    a.meta[index] = any && p.index == 0 && p.splits > 1 ? make_int4(p.req, p.row0, p.rows, p.splits) : make_int4(0, 0, 0, 0);
+  return any;
+}
+
+// The steps of KEYS positions of a piece, and the positions that every row of its tile sees
+struct Steps { int begin, end, all_lo, all_hi; };
+template <int KEYS>
+__device__ inline Steps steps_of(const AttnArgs& a, const Piece& p) {
+  const Sight first = sight(a, p, int(a.group.of(p.row0))), last = sight(a, p, int(a.group.of(p.row0 + p.rows - 1)));
+  const int64_t begin = first.lo / KEYS, end = last.hi < first.lo ? begin : last.hi / KEYS + 1;
+  return {int(begin + (end - begin) * p.index / p.splits), int(begin + (end - begin) * (p.index + 1) / p.splits),
+          last.lo, first.hi};
+}
+
+// A piece from start to end with care for values that are not finite, for the kernels below, whose loops have no
+// register to spare for it.  WQ waves of 32 rows, and WK on the same ones, of which the first does the work.
+template <typename T, int D, int WQ, int WK>
+__device__ __attribute__((noinline)) void careful_piece(const AttnArgs* args, int head, int index, char* lds) {
+  constexpr int KW = 32, kThreads = 64 * WQ * WK, kChunks = D / 8;
+  typedef typename T::elem elem;
+  const AttnArgs a = *args;
+  const int tid = threadIdx.x, lane = tid % 64, n = lane % 32, half = lane / 32, wave = tid / 64 % WQ;
+  Piece p;
+  if (!locate<32 * WQ, WK == 1 ? wide_keys(D) : few_keys(D, WK)>(a, index, p)) return;
+  const Steps steps = steps_of<WK == 1 ? wide_keys(D) : few_keys(D, WK)>(a, p);
+  const int per = (WK == 1 ? wide_keys(D) : few_keys(D, WK)) / KW;
+  const Places at = places_of<D>(lane);
+  const Row row = row_of(a, p, head, wave * 32 + n);
+  typename T::x8 q[D / 16];
+  load_query<T, D>(a, p, row, half, q);
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[i][e] = 0;
+  float m = -__builtin_inff(), l = 0;
+  const int32_t* table = a.io.block_table + int64_t(p.req) * a.io.table_req;
+  const elem* const kc = static_cast<const elem*>(a.c.k) + head * a.c.k_head;
+  const elem* const vc = static_cast<const elem*>(a.c.v) + head * a.c.v_head;
+  const auto page_of = [&](int key) {
+    if (key >= p.kv) return -1;
+    const int b = table[a.page.of(key)];
+    return b >= 0 && b < a.c.n_pages ? b : -1;
+  };
+#pragma unroll 1
+  for (int step = steps.begin * per; step < steps.end * per; ++step) {
+    const int key0 = step * KW;
+    __syncthreads();
+#pragma unroll 1
+    for (int i = tid; i < KW * kChunks; i += kThreads) {
+      const int r = i / kChunks, c = i % kChunks, key = key0 + r;
+      const int64_t b = page_of(key), off = key - int(a.page.of(key) * a.page.d);
+      u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
+      if (b >= 0 && c * 8 < a.c.head_dim) {
+        k = *reinterpret_cast<const u32x4*>(kc + b * a.c.k_page + off * a.c.k_tok + c * 8);
+        v = *reinterpret_cast<const u32x4*>(vc + b * a.c.v_page + off * a.c.v_tok + c * 8);
+      }
+      *reinterpret_cast<u32x4*>(lds + r * 2 * D + key_chunk(r, c) * 16) = k;
+      *reinterpret_cast<u32x4*>(lds + KW * 2 * D + r * 2 * D + value_chunk<D>(r, c) * 16) = v;
+    }
+    __syncthreads();
+    const uint64_t have = __ballot(lane < KW && page_of(key0 + lane) >= 0);
+    f32x16 s[1];
+    scores<T, D>(lds, at, q, s);
+    hide(s, half, key0, have, row);
+    rebase(s, a.scale2, m, l, o);
+    careful<T, D>(lds + KW * 2 * D, at, half, key0, have, row, s, a.scale2, m, l, o);
+  }
+  if (tid / 64 >= WQ) return;
+  settle(o);
+  l += __shfl_xor(l, 32);
+  write_row<T, D>(a, p, row, (int64_t(index) * gridDim.y + head) * (32 * WQ) + wave * 32 + n, half, m, l, o);
+}
+__device__ inline const AttnArgs* kernel_args() {
+  return (const AttnArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+}
+
+// ---- few rows -------------------------------------------------------------------------------------
+
 template <typename T, int D, int WQ, int WK, int KW>
 __global__ __launch_bounds__(64 * WQ * WK) void attn_kernel(AttnArgs a) {
   typedef Form<T, D, WQ, WK, KW> F;
-  typedef typename T::x8 x8;
   typedef typename T::elem elem;
-  constexpr int kSub = KW / 32;                  // tiles of 32 keys of a wave
-  constexpr int kDt = D / 32, kSteps = D / 16;
-  __shared__ __attribute__((aligned(16))) char lds[F::kLds];
+  __shared__ __attribute__((aligned(16))) char lds[2 * F::kKv > F::kMerge ? 2 * F::kKv : F::kMerge];
   char* const lk = lds;
   char* const lv = lds + F::kKv;
   const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, n = lane % 32, half = lane / 32;
   const int wq = wave % WQ, wk = wave / WQ;
   const int head = blockIdx.y, index = a.index0 + blockIdx.x;
   Piece p;
-  const bool any = locate<F::kRows, F::kKeys>(a, index, p);
-  if (a.split && head == 0 && tid == 0)
-    a.meta[index] = any && p.index == 0 && p.splits > 1 ? make_int4(p.req, p.row0, p.rows, p.splits) : make_int4(0, 0, 0, 0);
-  if (!any) return;
-  const int d = a.c.head_dim, G = a.group.d;
-
-  // the row of this lane: its token, its query head, the keys it sees
-  const int row = p.row0 + wq * 32 + n;
-  const bool real = row < p.row0 + p.rows;
-  const int tok = real ? int(a.group.of(row)) : 0;
-  const int64_t qh = int64_t(head) * G + (real ? row - tok * G : 0);
-  const auto seen = [&](int t, int64_t& lo, int64_t& hi) {    // by token t of the request
-    const int64_t here = int64_t(p.kv) - p.len + t;
-    hi = a.io.causal && here < p.kv - 1 ? here : p.kv - 1;
-    lo = a.io.window > 0 && here - a.io.window >= 0 ? here - a.io.window + 1 : 0;
-  };
-  int64_t lo64, hi64, first_lo, first_hi, last_lo, last_hi;
-  seen(tok, lo64, hi64);
-  seen(int(a.group.of(p.row0)), first_lo, first_hi);
-  seen(int(a.group.of(p.row0 + p.rows - 1)), last_lo, last_hi);
-  // rows that pad the tile see everything and are not written
-  const int lo = real ? int(lo64 > INT32_MAX ? INT32_MAX : lo64) : 0;
-  const int hi = real ? int(hi64 < -1 ? -1 : hi64) : INT32_MAX;
-  int all_lo = lo, all_hi = hi;                  // what every row of the wave sees
+  if (!take_piece<F::kRows, F::kKeys>(a, head, index, p)) return;
+  const Row row = row_of(a, p, head, wq * 32 + n);
+  const Steps steps = steps_of<F::kKeys>(a, p);
+  const Places at = places_of<D>(lane);
+  typename T::x8 q[D / 16];
+  load_query<T, D>(a, p, row, half, q);
+  f32x16 o[D / 32];
 #pragma unroll
-  for (int s = 1; s < 32; s *= 2) {
-    const int x = __shfl_xor(all_lo, s), y = __shfl_xor(all_hi, s);
-    all_lo = x > all_lo ? x : all_lo;
-    all_hi = y < all_hi ? y : all_hi;
-  }
-  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
-  all_hi = __builtin_amdgcn_readfirstlane(all_hi);
-  // this piece's steps: of the tile's range, the part `index`
-  const int64_t begin = first_lo / F::kKeys, end = last_hi < first_lo ? begin : last_hi / F::kKeys + 1;
-  const int step0 = int(begin + (end - begin) * p.index / p.splits);
-  const int step1 = int(begin + (end - begin) * (p.index + 1) / p.splits);
-
-  x8 q[kSteps];
-  const elem* qrow = static_cast<const elem*>(a.io.q) + (int64_t(p.tok0) + tok) * a.io.q_tok + qh * a.io.q_head;
-#pragma unroll
-  for (int s = 0; s < kSteps; ++s) {
-    const int at = 16 * s + 8 * half;
-    u32x4 v = {0, 0, 0, 0};
-    if (real && at < d) v = *reinterpret_cast<const u32x4*>(qrow + at);
-    q[s] = __builtin_bit_cast(x8, v);
-  }
-  f32x16 o[kDt];
-#pragma unroll
-  for (int i = 0; i < kDt; ++i)
+  for (int i = 0; i < D / 32; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[i][e] = 0;
   float m = -__builtin_inff(), l = 0;
+  const int d = a.c.head_dim;
 
   const int32_t* table = a.io.block_table + int64_t(p.req) * a.io.table_req;
   const auto page_of = [&](int key) {            // -1: none
@@ -268,7 +622,7 @@ __global__ __launch_bounds__(64 * WQ * WK) void attn_kernel(AttnArgs a) {
   const elem* const kc = static_cast<const elem*>(a.c.k) + head * a.c.k_head;
   const elem* const vc = static_cast<const elem*>(a.c.v) + head * a.c.v_head;
 
-  for (int step = step0; step < step1; ++step) {
+  for (int step = steps.begin; step < steps.end; ++step) {
     const int key0 = step * F::kKeys;
     u32x4 kr[F::kLoads], vr[F::kLoads];
     bool odd = false;
@@ -291,110 +645,22 @@ __global__ __launch_bounds__(64 * WQ * WK) void attn_kernel(AttnArgs a) {
       *reinterpret_cast<u32x4*>(lk + r * F::kRowBytes + key_chunk(r, c) * 16) = kr[i];
       *reinterpret_cast<u32x4*>(lv + r * F::kRowBytes + value_chunk<D>(r, c) * 16) = vr[i];
     }
-    // whether some row of the block does not see some position of the step
-    const bool cut = key0 < last_lo || key0 + F::kKeys - 1 > first_hi;
+    const bool cut = key0 < steps.all_lo || key0 + F::kKeys - 1 > steps.all_hi;
     const bool watch = __syncthreads_or(odd) && cut;
-
     const int wkey = key0 + wk * KW;             // this wave's keys
     const uint64_t have = __ballot(lane < KW && page_of(wkey + lane) >= 0);
-    const bool masked = have != (KW == 64 ? ~uint64_t(0) : (uint64_t(1) << KW) - 1) || wkey < all_lo ||
-                        wkey + KW - 1 > all_hi;
-    f32x16 s[kSub];
-#pragma unroll
-    for (int t = 0; t < kSub; ++t) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[t][e] = 0;
-      const int r = wk * KW + t * 32 + n;
-#pragma unroll
-      for (int i = 0; i < kSteps; ++i) {
-        const x8 k = *reinterpret_cast<const x8*>(lk + r * F::kRowBytes + key_chunk(r, 2 * i + half) * 16);
-        s[t] = T::mfma(k, q[i], s[t]);
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < kSub; ++t) settle(s[t]);
-    const auto visible = [&](int t, int e) {     // key of element e of s[t]
-      const int i = t * 32 + 8 * (e / 4) + 4 * half + e % 4;
-      return (have >> i & 1) && wkey + i >= lo && wkey + i <= hi;
-    };
-    if (masked) {
-#pragma unroll
-      for (int t = 0; t < kSub; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[t][e] = visible(t, e) ? s[t][e] : -__builtin_inff();
-    }
-    float top = -__builtin_inff();
-#pragma unroll
-    for (int t = 0; t < kSub; ++t)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float next = fmaxf(m, top * a.scale2);
-    const float base = next > -__builtin_inff() ? next : 0.0f;
-    const float shrink = __builtin_amdgcn_exp2f(m - base);
-    m = next;
-    float sum = 0;
-#pragma unroll
-    for (int t = 0; t < kSub; ++t)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[t][e] = __builtin_amdgcn_exp2f(fmaf(s[t][e], a.scale2, -base));
-        sum += s[t][e];
-      }
-    l = l * shrink + sum;
-#pragma unroll
-    for (int i = 0; i < kDt; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) o[i][e] *= shrink;
+    f32x16 s[KW / 32];
+    scores<T, D>(lk + wk * KW * F::kRowBytes, at, q, s);
+    hide(s, half, wkey, have, row);
+    rebase(s, a.scale2, m, l, o);
     if (watch) {
-      // the products one by one, 16 keys at a time, without those that are not seen (weight -1)
-      float* const w = reinterpret_cast<float*>(lds + 2 * F::kKv) + wave * 16 * 32;
-#pragma unroll
-      for (int t = 0; t < kSub; ++t)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          dasc_wy::wave_lds_sync();
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            w[(8 * (e / 4) + 4 * half + e % 4) * 32 + n] = visible(t, 8 * u + e) ? s[t][8 * u + e] : -1.0f;
-          dasc_wy::wave_lds_sync();
-          for (int k = 0; k < 16; ++k) {
-            const float x = w[k * 32 + n];
-            const int r = wk * KW + t * 32 + u * 16 + k;
-            if (!(x < 0.0f))
-#pragma unroll
-              for (int i = 0; i < kDt; ++i)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                  const int c = i * 32 + 8 * (e / 4) + 4 * half + e % 4;
-                  const elem v = *reinterpret_cast<const elem*>(lv + r * F::kRowBytes + value_chunk<D>(r, c / 8) * 16 + c % 8 * 2);
-                  o[i][e] = fmaf(x, float(v), o[i][e]);
-                }
-          }
-        }
-    } else {
-#pragma unroll
-      for (int t = 0; t < kSub; ++t)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          x8 w;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] = elem(s[t][8 * u + e]);
-          // rows of the transposing read: this lane's place in four keys of 16 columns
-          const int r = wk * KW + t * 32 + u * 16 + 4 * half + lane % 16 / 4;
-#pragma unroll
-          for (int i = 0; i < kDt; ++i) {
-            const int c = i * 32 + lane % 32 / 16 * 16 + lane % 4 * 4;
-            union { s16x4 h[2]; x8 v; } x;
-            x.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lv + r * F::kRowBytes + value_chunk<D>(r, c / 8) * 16 + c % 8 * 2));
-            x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lv + (r + 8) * F::kRowBytes + value_chunk<D>(r + 8, c / 8) * 16 + c % 8 * 2));
-            o[i] = T::mfma(x.v, w, o[i]);
-          }
-        }
+      careful_piece<T, D, WQ, WK>(kernel_args(), head, index, lds);
+      return;
     }
-#pragma unroll
-    for (int i = 0; i < kDt; ++i) settle(o[i]);
+    values<T, D>(lv + wk * KW * F::kRowBytes, at, s, a.scale2, m, l, o);
   }
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) settle(o[i]);
   l += __shfl_xor(l, 32);
 
   // waves that share rows meet in LDS
@@ -407,7 +673,7 @@ __global__ __launch_bounds__(64 * WQ * WK) void attn_kernel(AttnArgs a) {
         mine[n * 2 + 1] = l;
       }
 #pragma unroll
-      for (int i = 0; i < kDt; ++i)
+      for (int i = 0; i < D / 32; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) mine[64 + (i * 16 + e) * 64 + lane] = o[i][e];
     }
@@ -421,44 +687,239 @@ __global__ __launch_bounds__(64 * WQ * WK) void attn_kernel(AttnArgs a) {
       m = next;
       l = l * f + ol * g;
 #pragma unroll
-      for (int i = 0; i < kDt; ++i)
+      for (int i = 0; i < D / 32; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[i][e] = o[i][e] * f + other[64 + (i * 16 + e) * 64 + lane] * g;
     }
   }
-  if (!real) return;
-  if (p.splits > 1) {
-    const int64_t slot = (int64_t(index) * gridDim.y + head) * F::kRows + wq * 32 + n;
-    if (half == 0) {
-      a.ml[slot * 2] = m;
-      a.ml[slot * 2 + 1] = l;
+  write_row<T, D>(a, p, row, (int64_t(index) * gridDim.y + head) * F::kRows + wq * 32 + n, half, m, l, o);
+}
+
+// ---- many rows --------------------------------------------------------------------------------------
+
+// From the scores S(u) of 32 keys to the next: the products of S(u + 1) run while the weights of S(u) are formed, and
+// the products of those while S(u + 1)'s maximum is taken.  lk: keys of u + 1, lv: values of u.  `mask` hides what
+// is not seen of S(u + 1).
+template <typename T, int D, typename M>
+__device__ inline void advance(const char* lk, const char* lv, const Places& at, const typename T::x8 (&q)[D / 16],
+                               float scale2, f32x16 (&s)[1], float& m, float& l, f32x16 (&o)[D / 32], const M& mask) {
+  constexpr int kSteps = D / 16, kDt = D / 32, kSlice = 16 / kSteps, kMax = 16 / (2 * kDt - 2) + 1;
+  const auto read_k = [&](int j) { return *reinterpret_cast<const typename T::x8*>(lk + at.key[j % 4] + j / 4 * 128); };
+  const auto read_v = [&](int j) { return value_operand<T, D>(lv, at, j / kDt * 16, j % kDt); };
+  typename T::x8 k[4], v[4], w[2];
+  f32x16 next[1];
+  const float base = base_of(m);
+  float part[2] = {0, 0};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) k[j] = read_k(j);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) next[0][e] = 0;
+  hold();
+#pragma unroll
+  for (int j = 0; j < kSteps; ++j) {
+    next[0] = T::mfma(k[j % 4], q[j], next[0]);
+    if (j + 4 < kSteps) k[j % 4] = read_k(j + 4);
+#pragma unroll
+    for (int e = j * kSlice; e < (j + 1) * kSlice; ++e) {
+      const float x = __builtin_amdgcn_exp2f(fmaf(s[0][e], scale2, -base));
+      w[e / 8][e % 8] = typename T::elem(x);
+      part[e % 2] += x;
     }
-    float* out = a.part + slot * D;
-#pragma unroll
-    for (int i = 0; i < kDt; ++i)
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const int c = i * 32 + 8 * b + 4 * half;
-        *reinterpret_cast<float4*>(out + c) = make_float4(o[i][4 * b], o[i][4 * b + 1], o[i][4 * b + 2], o[i][4 * b + 3]);
-      }
-    return;
+    // (else the weights would move to where they are used, past the branch)
+    if ((j + 1) * kSlice % 8 == 0) {
+      u32x4 x = __builtin_bit_cast(u32x4, w[((j + 1) * kSlice - 1) / 8]);
+      asm volatile("" : "+v"(x));
+      w[((j + 1) * kSlice - 1) / 8] = __builtin_bit_cast(typename T::x8, x);
+    }
+    asm volatile("" : "+v"(part[0]), "+v"(part[1]));
+    hold();
   }
-  const int64_t t = int64_t(p.tok0) + tok;
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  elem* out = static_cast<elem*>(a.io.o) + t * a.io.o_tok + qh * a.io.o_head;
-  typedef elem e4 __attribute__((ext_vector_type(4)));
+  l += part[0] + part[1];
 #pragma unroll
-  for (int i = 0; i < kDt; ++i)
+  for (int j = 0; j < 4; ++j) v[j] = read_v(j);
+  mask(next);
+  float top = -__builtin_inff();
+  hold();
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int c = i * 32 + 8 * b + 4 * half;
-      e4 x;
+  for (int j = 0; j < 2 * kDt; ++j) {
+    o[j % kDt] = T::mfma(v[j % 4], w[j / kDt], o[j % kDt]);
+    if (j + 4 < 2 * kDt) v[j % 4] = read_v(j + 4);
+    // two products later the next scores are there, whichever way the branch before went
+    if (j == 1) asm volatile("" : "+v"(next[0]));
+    if (j >= 2) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = elem(o[i][4 * b + e] * inv);
-      if (c < d) *reinterpret_cast<e4*>(out + c) = x;
+      for (int e = (j - 2) * kMax; e < (j - 1) * kMax && e < 16; ++e) top = fmaxf(top, next[0][e]);
     }
-  if (a.io.lse && half == 0)
-    a.io.lse[t * a.io.lse_tok + qh * a.io.lse_head] = m * 0.69314718056f + logf(l);
+    hold();
+  }
+  rebase(top, scale2, m, l, o);
+  s[0] = next[0];
+}
+
+// WQ waves of 32 rows each go over the keys together, 32 at a time, a product ahead (advance()).  Keys are in LDS
+// two steps ahead and values one, so the block meets once a step; the loads of both are issued at a step's
+// start and stored at its end.  ONE: a load's rows always lie in one page, whose address is then the same for a wave.
+template <typename T, int D, int WQ, int SIMD, bool ONE>
+__global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD))) void attn_wide_kernel(AttnArgs a) {
+  constexpr int KW = wide_keys(D), NS = KW / 32;
+  typedef Form<T, D, WQ, 1, KW> F;
+  typedef typename T::elem elem;
+  constexpr int kKeyBuffers = NS + 1;
+  __shared__ __attribute__((aligned(16))) char lds[(kKeyBuffers + 2) * F::kKv];
+  char* const lds_v = lds + kKeyBuffers * F::kKv;
+  const int tid = threadIdx.x, lane = tid % 64, n = lane % 32, half = lane / 32;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int head = blockIdx.y, index = a.index0 + blockIdx.x;
+  Piece p;
+  if (!take_piece<F::kRows, F::kKeys>(a, head, index, p)) return;
+  const Steps steps = steps_of<F::kKeys>(a, p);
+  const Places at = places_of<D>(lane);
+  const Row row = row_of(a, p, head, wave * 32 + n);
+  // the steps that some row of the wave sees something of
+  const int w0 = wave * 32, r0 = w0 < p.rows ? w0 : p.rows - 1, r1 = w0 + 31 < p.rows ? w0 + 31 : p.rows - 1;
+  const int first = sight(a, p, int(a.group.of(p.row0 + r0))).lo / F::kKeys;
+  const int end_hi = sight(a, p, int(a.group.of(p.row0 + r1))).hi, last = end_hi < 0 ? -1 : end_hi / F::kKeys;
+  typename T::x8 q[D / 16];
+  load_query<T, D>(a, p, row, half, q);
+  f32x16 o[D / 32], s[1];
+  float m = -__builtin_inff(), l = 0;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[i][e] = 0;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) s[0][e] = -__builtin_inff();
+  const int d = a.c.head_dim;
+
+  const int32_t* table = a.io.block_table + int64_t(p.req) * a.io.table_req;
+  const elem* const kc = static_cast<const elem*>(a.c.k) + head * a.c.k_head;
+  const elem* const vc = static_cast<const elem*>(a.c.v) + head * a.c.v_head;
+  // Lane r of a wave knows where row r of a step lies.  Its entry of the table is asked for a step ahead, and looked
+  // at when it is there.  Loads have no branch: what is not there is loaded from page 0 and put into LDS as zeros.
+  int entry, inside;                               // of the step to be loaded next: the entry, the place in the page
+  const auto ask = [&](int step) {
+    int key = (step < steps.end ? step : steps.end - 1) * F::kKeys + lane % KW;
+    key = key < p.kv ? key : p.kv - 1;
+    const int at = a.page.of(key);
+    entry = table[at];
+    inside = key - at * int(a.page.d);
+  };
+  const auto there = [&](int step) {               // the positions of the step that have a page
+    return __ballot(lane < KW && step < steps.end && step * F::kKeys + lane < p.kv && entry >= 0 && entry < a.c.n_pages);
+  };
+  const auto rows_at = [&](uint32_t page_stride, uint32_t tok_stride) {
+    const uint32_t b = entry >= 0 && entry < a.c.n_pages ? entry : 0;
+    return uint64_t(b) * page_stride + uint64_t(uint32_t(inside)) * tok_stride;
+  };
+  constexpr uint64_t kAll = KW == 64 ? ~uint64_t(0) : (uint64_t(1) << 32) - 1;
+  constexpr int kRow = F::kThreads / F::kChunks, kWaveRows = 64 / F::kChunks;   // rows of a load of the block, of a wave
+  const int chunk = tid % F::kChunks, column = chunk * 8 < d ? chunk * 8 : 0;
+  const uint64_t k_lane = uint64_t(ONE ? lane / F::kChunks : 0) * a.k_tok + column;
+  const uint64_t v_lane = uint64_t(ONE ? lane / F::kChunks : 0) * a.v_tok + column;
+  const auto load = [&](const elem* base, uint64_t rows, uint64_t lane_off, u32x4 (&x)[F::kLoads]) {
+#pragma unroll
+    for (int i = 0; i < F::kLoads; ++i) {
+      uint64_t at;
+      if constexpr (ONE) {                         // the rows of a wave's load follow the first, in its page
+        const int r = i * kRow + wave * kWaveRows;
+        at = uint32_t(__builtin_amdgcn_readlane(int(uint32_t(rows)), r)) |
+             uint64_t(uint32_t(__builtin_amdgcn_readlane(int(uint32_t(rows >> 32)), r))) << 32;
+      } else {
+        at = __shfl((unsigned long long)rows, i * kRow + tid / F::kChunks);
+      }
+      x[i] = *reinterpret_cast<const u32x4*>(base + at + lane_off);
+    }
+  };
+  const int row_in = tid / F::kChunks;             // (kRow is a multiple of eight: loads swap the same chunks)
+  const int k_place = row_in * F::kRowBytes + key_chunk(row_in, chunk) * 16;
+  const int v_place = row_in * F::kRowBytes + value_chunk<D>(row_in, chunk) * 16;
+  const auto store = [&](char* to, uint64_t have, u32x4 (&x)[F::kLoads]) {
+    if (have != kAll || d < D) {
+#pragma unroll
+      for (int i = 0; i < F::kLoads; ++i)
+        if (!(have >> (i * kRow + row_in) & 1) || chunk * 8 >= d) x[i] = u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < F::kLoads; ++i) *reinterpret_cast<u32x4*>(to + i * kRow * F::kRowBytes) = x[i];
+  };
+  // Whether the values of a step have to be watched: some row of the block does not see some of its positions, and
+  // a value is not finite.  The block meets.
+  const auto meet = [&](int step, const u32x4 (&x)[F::kLoads]) {
+    if (step >= steps.end || (step * F::kKeys >= steps.all_lo && step * F::kKeys + F::kKeys - 1 <= steps.all_hi)) {
+      __syncthreads();
+      return false;
+    }
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < F::kLoads; ++i) odd |= odd_value<T>(x[i]);
+    return __syncthreads_or(odd) != 0;
+  };
+
+  if (steps.begin < steps.end) {
+    u32x4 kr[F::kLoads], vr[F::kLoads];
+    const bool alike = a.k_page == a.v_page && a.k_tok == a.v_tok;
+    uint64_t k_rows, v_rows, v_next;               // of the keys to be loaded next, of the values, and after them
+    const auto find = [&] {
+      k_rows = rows_at(a.k_page, a.k_tok);
+      v_next = alike ? k_rows : rows_at(a.v_page, a.v_tok);
+    };
+    // have: of the present step; have1, have2: of the two after
+    ask(steps.begin);
+    uint64_t have = there(steps.begin), have1, have2;
+    find();
+    ask(steps.begin + 1);
+    load(kc, k_rows, k_lane, kr);
+    load(vc, v_next, v_lane, vr);
+    store(lds + k_place, have, kr);
+    store(lds_v + v_place, have, vr);
+    have1 = there(steps.begin + 1);
+    find();
+    ask(steps.begin + 2);
+    load(kc, k_rows, k_lane, kr);
+    v_rows = v_next;
+    store(lds + F::kKv + k_place, have1, kr);
+    bool watch = meet(steps.begin, vr);
+    if (!watch) {
+      scores<T, D>(lds, at, q, s);
+      hide(s, half, steps.begin * F::kKeys, have & 0xFFFFFFFFu, row);
+      rebase(s, a.scale2, m, l, o);
+    }
+    const auto mask_of = [&](int step, uint64_t all, int t) {
+      return [&, step, all, t](f32x16 (&x)[1]) {
+        hide(x, half, step * F::kKeys + t * 32, all >> (32 * t) & 0xFFFFFFFFu, row);
+      };
+    };
+    int kb = 0;                                    // the buffer of the present step's keys
+    for (int step = steps.begin; step < steps.end && !watch; ++step) {
+      const char* const lv = lds_v + ((step - steps.begin) & 1) * F::kKv;
+      const int kb1 = kb + 1 == kKeyBuffers ? 0 : kb + 1, kb2 = kb1 + 1 == kKeyBuffers ? 0 : kb1 + 1;
+      have2 = there(step + 2);
+      find();
+      load(kc, k_rows, k_lane, kr);
+      load(vc, v_rows, v_lane, vr);
+      v_rows = v_next;
+      ask(step + 3);
+      if (step + 1 >= first && step <= last) {     // else nothing of this step or the next is seen by the wave
+        if constexpr (NS == 2)
+          advance<T, D>(lds + kb * F::kKv + 32 * F::kRowBytes, lv, at, q, a.scale2, s, m, l, o, mask_of(step, have, 1));
+        advance<T, D>(lds + kb1 * F::kKv, lv + (NS - 1) * 32 * F::kRowBytes, at, q, a.scale2, s, m, l, o,
+                      mask_of(step + 1, have1, 0));
+      }
+      store(lds + kb2 * F::kKv + k_place, have2, kr);
+      store(lds_v + ((step + 1 - steps.begin) & 1) * F::kKv + v_place, have1, vr);
+      watch = meet(step + 1, vr);
+      have = have1;
+      have1 = have2;
+      kb = kb1;
+    }
+    if (watch) {
+      careful_piece<T, D, WQ, 1>(kernel_args(), head, index, lds);
+      return;
+    }
+  }
+  settle(o);
+  l += __shfl_xor(l, 32);
+  write_row<T, D>(a, p, row, (int64_t(index) * gridDim.y + head) * F::kRows + wave * 32 + n, half, m, l, o);
 }
 
 // The pieces of a split tile: o = sum 2^(m_i - m) O_i / sum 2^(m_i - m) l_i
@@ -502,6 +963,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 
 // How a call runs: the form by the rows of its longest request, pieces by the tiles that it can have
 struct Launch {
+  int form;                      // 0: 32 rows, 1: 64, 2: many
   int rows, keys;                // of a tile and a step
   int64_t pieces;                // of a key head, at most
   bool split;
@@ -511,13 +973,24 @@ struct Launch {
 constexpr float kLog2e = 1.44269504089f;
 constexpr int kBlocks = 512;     // that a split call aims at
 
+int dim_of(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
+
+void shape_of(Launch& x, int D) {
+  if (x.form == 2) {
+    x.rows = 32 * wide_wq(D);
+    x.keys = wide_keys(D);
+  } else {
+    x.rows = 32 << x.form;
+    x.keys = x.form == 1 || D == 256 ? 64 : 128;
+  }
+}
+
 Launch launch_of(int n_req, int64_t n_tokens, int group, int n_kv_heads, int head_dim, int max_len, int max_kv) {
   Launch x;
   const int64_t most = n_tokens < max_len ? n_tokens : max_len;
   const int64_t rows = most * group;
-  x.rows = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
-  const int wk = x.rows == 32 ? (head_dim > 128 ? 2 : 4) : x.rows == 64 ? 2 : 1;
-  x.keys = wk * (x.rows == 128 && head_dim <= 128 ? 64 : 32);
+  x.form = rows <= 32 ? 0 : rows <= 64 ? 1 : 2;
+  shape_of(x, dim_of(head_dim));
   const int64_t tiles = n_tokens * group / x.rows + n_req;
   x.target = kBlocks / n_kv_heads;
   if (x.target < 1) x.target = 1;
@@ -526,9 +999,7 @@ Launch launch_of(int n_req, int64_t n_tokens, int group, int n_kv_heads, int hea
   return x;
 }
 
-int dim_of(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
-
-template <typename T, int D, int WQ, int WK, int KW>
+template <typename T, int D, int FORM>
 void launch_form(AttnArgs a, const Launch& x, hipStream_t st) {
   constexpr int64_t kMost = int64_t(1) << 21;     // a grid counts threads in 32 bits
   const auto grid = [&](int64_t i) {
@@ -537,16 +1008,23 @@ void launch_form(AttnArgs a, const Launch& x, hipStream_t st) {
   };
   for (int64_t i = 0; i < x.pieces; i += kMost) {
     const dim3 g = grid(i);
-    attn_kernel<T, D, WQ, WK, KW><<<g, 64 * WQ * WK, 0, st>>>(a);
+    if constexpr (FORM == 0) attn_kernel<T, D, 1, D == 256 ? 2 : 4, 32><<<g, D == 256 ? 128 : 256, 0, st>>>(a);
+    else if constexpr (FORM == 1) attn_kernel<T, D, 2, 2, 32><<<g, 256, 0, st>>>(a);
+    else if (a.page.d % (512 / D) == 0)     // the rows of a wave's load are of one page
+      attn_wide_kernel<T, D, wide_wq(D), wide_simd(D), true><<<g, 64 * wide_wq(D), 0, st>>>(a);
+    else attn_wide_kernel<T, D, wide_wq(D), wide_simd(D), false><<<g, 64 * wide_wq(D), 0, st>>>(a);
   }
-  if (x.split) attn_join_kernel<T, D, 32 * WQ><<<grid(0), 256, 0, st>>>(a);   // few pieces
+  constexpr int kRows = FORM == 2 ? 32 * wide_wq(D) : 32 << FORM;
+  if (x.split) attn_join_kernel<T, D, kRows><<<grid(0), 256, 0, st>>>(a);   // few pieces
 }
 
 template <typename T, int D>
 void launch_rows(const AttnArgs& a, const Launch& x, hipStream_t st) {
-  if (x.rows == 32) launch_form<T, D, 1, D == 256 ? 2 : 4, 32>(a, x, st);
-  else if (x.rows == 64) launch_form<T, D, 2, 2, 32>(a, x, st);
-  else launch_form<T, D, 4, 1, D == 256 ? 32 : 64>(a, x, st);
+  switch (x.form) {
+    case 0: launch_form<T, D, 0>(a, x, st); break;
+    case 1: launch_form<T, D, 1>(a, x, st); break;
+    default: launch_form<T, D, 2>(a, x, st); break;
+  }
 }
 
 template <typename T>
@@ -591,15 +1069,17 @@ extern "C" int dasc_cache_attn_workspace_bytes(int32_t n_req, int64_t n_tokens, 
   const int64_t D = dim_of(head_dim);
   int target = kBlocks / n_kv_heads;
   if (target < 1) target = 1;
-  for (const int rows : {32, 64, 128}) {
-    if (int64_t(rows) / 2 >= int64_t(max_len) * group && rows > 32) continue;   // no request fills it
-    int64_t tiles = n_tokens * group / rows + n_req;
+  for (int form = 0; form < 3; ++form) {
+    if (form > 0 && int64_t(max_len) * group <= (16 << form)) continue;   // no request that takes it
+    Launch x;
+    x.form = form;
+    shape_of(x, int(D));
+    int64_t tiles = n_tokens * group / x.rows + n_req;
     if (tiles > 2 * target) tiles = 2 * target;
     const int64_t pieces = tiles + target;
-    const int64_t need = pieces * 16 + pieces * n_kv_heads * rows * (D + 2) * 4;
-    if (size_t(need) > *bytes) *bytes = size_t(need);
+    const int64_t need = pieces * 16 + pieces * n_kv_heads * x.rows * (D + 2) * 4;
+    if (max_kv > kMinSteps * x.keys && size_t(need) > *bytes) *bytes = size_t(need);
   }
-  if (max_kv <= kMinSteps * 32) *bytes = 0;
   return DASC_OK;
 }
 
@@ -633,6 +1113,12 @@ extern "C" int dasc_cache_attn(const dasc_kv_cache* cache, const dasc_attn_io* i
   AttnArgs a;
   a.c = *cache;
   a.io = *io;
+  for (const int64_t stride : {cache->k_page, cache->k_tok, cache->v_page, cache->v_tok})
+    if (stride > UINT32_MAX) return DASC_E_UNSUPPORTED;
+  a.k_page = uint32_t(cache->k_page);
+  a.k_tok = uint32_t(cache->k_tok);
+  a.v_page = uint32_t(cache->v_page);
+  a.v_tok = uint32_t(cache->v_tok);
   a.group = divisor(group);
   a.page = divisor(cache->page_size);
   a.target = x.target;
