@@ -33,7 +33,9 @@
 #define DASC_SIMD128 2
 #define DASC_WQ128 8
 #define DASC_SIMD64 2
-#define DASC_WQ64 8
+#define DASC_WQ64 4
+#define DASC_KW128 64
+#define DASC_KW64 64
 #endif
 
 namespace dasc {
@@ -90,9 +92,9 @@ struct Divisor {                          // n / d for 0 <= n < 2^31: (n * mul) 
 struct AttnArgs {
   dasc_kv_cache c;
   dasc_attn_io io;
-  Divisor group, page;
+  Divisor group, page, heads;
   uint32_t k_page, k_tok, v_page, v_tok;  // the cache's strides of pages and tokens
-  int32_t index0;                         // first piece of this launch
+  int64_t block0;                         // first block of this launch: piece * n_kv_heads + head
   int32_t target;                         // pieces of a key head to aim at
   int32_t split;                          // whether tiles may be split
   float scale2;                           // scale * log2 e
@@ -105,6 +107,19 @@ struct Piece {
   int32_t req, row0, rows, tok0, len, kv; // rows of the tile, the request's first token, tokens and positions
   int32_t index, splits;
 };
+
+// Blocks are numbered by piece, then by head: the long pieces of all heads come first, and heads that are a
+// multiple of eight apart share the L2 of an XCD.
+__device__ inline void block_of(const AttnArgs& a, int& head, int& index) {
+  if (a.block0 == 0) {
+    index = int(a.heads.of(blockIdx.x));
+    head = int(blockIdx.x) - index * a.c.n_kv_heads;
+  } else {
+    const int64_t x = a.block0 + blockIdx.x;
+    index = int(x / a.c.n_kv_heads);
+    head = int(x % a.c.n_kv_heads);
+  }
+}
 
 // How request r is cut: its tiles of ROWS rows, and the keys of its last one in steps of KEYS
 struct Cut { int32_t tok0, len, kv, tiles, steps; };
@@ -150,6 +165,33 @@ __device__ inline bool locate(const AttnArgs& a, int index, Piece& p) {
     per = int64_t((all + a.target - 1) / a.target);
     if (per < kMinSteps) per = kMinSteps;
   }
+  const auto take = [&](const Cut& c, int splits, int r0, int at, int rest) {
+    const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
+    const int tiles = of(c.tiles);
+    p.splits = of(splits);
+    const int tile = tiles - 1 - rest / p.splits;          // the longest first
+    p.index = rest % p.splits;
+    p.req = r0 + at;
+    p.tok0 = of(c.tok0);
+    p.len = of(c.len);
+    p.kv = of(c.kv);
+    p.row0 = tile * ROWS;
+    const int left = p.len * int(a.group.d) - p.row0;
+    p.rows = left < ROWS ? left : ROWS;
+  };
+  if (!a.split && a.io.n_req <= 64) {     // whole tiles: the longest request's first
+    const Cut c = cut_of<ROWS, KEYS>(a, lane);
+    int64_t before = 0;
+    for (int j = 0; j < a.io.n_req; ++j) {
+      const int steps = __builtin_amdgcn_readlane(c.steps, j), tiles = __builtin_amdgcn_readlane(c.tiles, j);
+      before += steps > c.steps || (steps == c.steps && j < lane) ? tiles : 0;
+    }
+    const uint64_t in = __ballot(before <= index && index < before + c.tiles);
+    if (!in) return false;
+    const int at = __builtin_ctzll(in);
+    take(c, 1, 0, at, __builtin_amdgcn_readlane(int(index - before), at));
+    return true;
+  }
   int64_t before = 0;
   for (int r0 = 0; r0 < a.io.n_req; r0 += 64) {
     const Cut c = cut_of<ROWS, KEYS>(a, r0 + lane);
@@ -164,19 +206,7 @@ __device__ inline bool locate(const AttnArgs& a, int index, Piece& p) {
     const uint64_t past = __ballot(before + upto > index);
     if (past) {
       const int at = __builtin_ctzll(past);
-      const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
-      const int rest = of(int(index - (before + upto - mine)));
-      const int tiles = of(c.tiles);
-      p.splits = of(splits);
-      const int tile = tiles - 1 - rest / p.splits;        // the longest first
-      p.index = rest % p.splits;
-      p.req = r0 + at;
-      p.tok0 = of(c.tok0);
-      p.len = of(c.len);
-      p.kv = of(c.kv);
-      p.row0 = tile * ROWS;
-      const int left = p.len * int(a.group.d) - p.row0;
-      p.rows = left < ROWS ? left : ROWS;
+      take(c, splits, r0, at, __builtin_amdgcn_readlane(int(index - (before + upto - mine)), at));
       return true;
     }
     before += __shfl((long long)upto, 63);
@@ -201,7 +231,7 @@ struct Form {
 // Tiles of many rows: waves of 32 rows each, waves of a SIMD, keys of a step
 constexpr int wide_wq(int D) { return D == 256 ? DASC_WQ256 : D == 128 ? DASC_WQ128 : DASC_WQ64; }
 constexpr int wide_simd(int D) { return D == 256 ? DASC_SIMD256 : D == 128 ? DASC_SIMD128 : DASC_SIMD64; }
-constexpr int wide_keys(int D) { return D == 256 ? 32 : 64; }
+constexpr int wide_keys(int D) { return D == 256 ? 32 : D == 128 ? DASC_KW128 : DASC_KW64; }
 constexpr int few_keys(int D, int wk) { return 32 * wk; }
 
 // Where 16-byte chunk c of row r lies: lanes of a read that take the same chunk of many rows (keys), or a few
@@ -580,7 +610,7 @@ __device__ __attribute__((noinline)) void careful_piece(const AttnArgs* args, in
   if (tid / 64 >= WQ) return;
   settle(o);
   l += __shfl_xor(l, 32);
-  write_row<T, D>(a, p, row, (int64_t(index) * gridDim.y + head) * (32 * WQ) + wave * 32 + n, half, m, l, o);
+  write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * (32 * WQ) + wave * 32 + n, half, m, l, o);
 }
 __device__ inline const AttnArgs* kernel_args() {
   return (const AttnArgs*)__builtin_amdgcn_kernarg_segment_ptr();
@@ -597,7 +627,8 @@ __global__ __launch_bounds__(64 * WQ * WK) void attn_kernel(AttnArgs a) {
   char* const lv = lds + F::kKv;
   const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, n = lane % 32, half = lane / 32;
   const int wq = wave % WQ, wk = wave / WQ;
-  const int head = blockIdx.y, index = a.index0 + blockIdx.x;
+  int head, index;
+  block_of(a, head, index);
   Piece p;
   if (!take_piece<F::kRows, F::kKeys>(a, head, index, p)) return;
   const Row row = row_of(a, p, head, wq * 32 + n);
@@ -692,7 +723,7 @@ __global__ __launch_bounds__(64 * WQ * WK) void attn_kernel(AttnArgs a) {
         for (int e = 0; e < 16; ++e) o[i][e] = o[i][e] * f + other[64 + (i * 16 + e) * 64 + lane] * g;
     }
   }
-  write_row<T, D>(a, p, row, (int64_t(index) * gridDim.y + head) * F::kRows + wq * 32 + n, half, m, l, o);
+  write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * F::kRows + wq * 32 + n, half, m, l, o);
 }
 
 // ---- many rows --------------------------------------------------------------------------------------
@@ -769,7 +800,8 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
   char* const lds_v = lds + kKeyBuffers * F::kKv;
   const int tid = threadIdx.x, lane = tid % 64, n = lane % 32, half = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
-  const int head = blockIdx.y, index = a.index0 + blockIdx.x;
+  int head, index;
+  block_of(a, head, index);
   Piece p;
   if (!take_piece<F::kRows, F::kKeys>(a, head, index, p)) return;
   const Steps steps = steps_of<F::kKeys>(a, p);
@@ -919,7 +951,7 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
   }
   settle(o);
   l += __shfl_xor(l, 32);
-  write_row<T, D>(a, p, row, (int64_t(index) * gridDim.y + head) * F::kRows + wave * 32 + n, half, m, l, o);
+  write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * F::kRows + wave * 32 + n, half, m, l, o);
 }
 
 // The pieces of a split tile: o = sum 2^(m_i - m) O_i / sum 2^(m_i - m) l_i
@@ -927,13 +959,16 @@ template <typename T, int D, int ROWS>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   typedef typename T::elem elem;
   constexpr int kLanes = D / 4;                  // of a row
-  const int index = a.index0 + blockIdx.x, head = blockIdx.y, heads = gridDim.y;
+  int head, index;
+  block_of(a, head, index);
+  const int heads = a.c.n_kv_heads;
   const int4 t = a.meta[index];                  // request, first row, rows, pieces
   if (t.w < 2) return;
   const int c = threadIdx.x % kLanes * 4, n = int(a.io.n_tokens), G = a.group.d;
   int tok0 = a.io.cu_seqlens[t.x];
   tok0 = tok0 < 0 ? 0 : tok0 > n ? n : tok0;
-  for (int r = threadIdx.x / kLanes; r < t.z; r += 256 / kLanes) {
+  const int r1 = int(blockIdx.y) * 32 + 32 < t.z ? blockIdx.y * 32 + 32 : t.z;
+  for (int r = blockIdx.y * 32 + threadIdx.x / kLanes; r < r1; r += 256 / kLanes) {
     const auto slot = [&](int i) { return (int64_t(index + i) * heads + head) * ROWS + r; };
     float m = -__builtin_inff(), l = 0;
     for (int i = 0; i < t.w; ++i) m = fmaxf(m, a.ml[slot(i) * 2]);
@@ -972,6 +1007,11 @@ struct Launch {
 
 constexpr float kLog2e = 1.44269504089f;
 constexpr int kBlocks = 512;     // that a split call aims at
+constexpr int kUnits = 256;      // compute units
+constexpr int kMostPieces = 16;  // of a tile of many rows
+
+// Blocks of a compute unit
+constexpr int wide_blocks(int D) { return 4 * wide_simd(D) / wide_wq(D); }
 
 int dim_of(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
@@ -985,29 +1025,47 @@ void shape_of(Launch& x, int D) {
   }
 }
 
-Launch launch_of(int n_req, int64_t n_tokens, int group, int n_kv_heads, int head_dim, int max_len, int max_kv) {
+Launch launch_of(int n_req, int64_t n_tokens, int group, int n_kv_heads, int head_dim, int max_len, int max_kv,
+                 int64_t window) {
   Launch x;
   const int64_t most = n_tokens < max_len ? n_tokens : max_len;
   const int64_t rows = most * group;
   x.form = rows <= 32 ? 0 : rows <= 64 ? 1 : 2;
   shape_of(x, dim_of(head_dim));
   const int64_t tiles = n_tokens * group / x.rows + n_req;
-  x.target = kBlocks / n_kv_heads;
-  if (x.target < 1) x.target = 1;
-  x.split = tiles < 2 * x.target && max_kv > kMinSteps * x.keys;
+  const int64_t steps = (int64_t(max_kv) + x.keys - 1) / x.keys;
+  x.target = 1;
+  x.split = false;
+  if (x.form == 2) {
+    // Blocks go over the chip in rounds: a tile is cut into as many pieces as leave least of the last one empty.
+    // (Requests end inside a tile, each in the middle of one on average.)
+    const int64_t about = (n_tokens * group + (n_req - 1) * int64_t(x.rows / 2) + x.rows - 1) / x.rows * n_kv_heads;
+    const int64_t slots = kUnits * wide_blocks(dim_of(head_dim));
+    const int64_t reach = window > 0 && window + x.rows / group + 1 < max_kv ? window + x.rows / group + 1 : max_kv;
+    const double length = double(reach) / x.keys;            // steps of a tile
+    double best = 1e30;
+    int at = 1;
+    for (int n = 1; n <= kMostPieces && (n == 1 || n * kMinSteps <= length) && (n == 1 || about < 2 * slots); ++n) {
+      // a piece's start and end cost as much as four steps, and its part of the join as much again
+      const double time = double((about * n + slots - 1) / slots) * (length / n + (n > 1 ? 8 : 4));
+      if (time < best) best = time, at = n;
+    }
+    x.split = at > 1;
+    x.target = int(x.split ? (about * at + n_kv_heads - 1) / n_kv_heads : 1);
+  } else {
+    x.target = kBlocks / n_kv_heads < 1 ? 1 : kBlocks / n_kv_heads;
+    x.split = tiles < 2 * x.target && steps > kMinSteps;
+  }
   x.pieces = x.split ? tiles + x.target : tiles;
   return x;
 }
 
 template <typename T, int D, int FORM>
 void launch_form(AttnArgs a, const Launch& x, hipStream_t st) {
-  constexpr int64_t kMost = int64_t(1) << 21;     // a grid counts threads in 32 bits
-  const auto grid = [&](int64_t i) {
-    a.index0 = int32_t(i);
-    return dim3(uint32_t(x.pieces - i < kMost ? x.pieces - i : kMost), a.c.n_kv_heads);
-  };
-  for (int64_t i = 0; i < x.pieces; i += kMost) {
-    const dim3 g = grid(i);
+  constexpr int64_t kMost = int64_t(1) << 22;     // a grid counts threads in 32 bits
+  const int64_t blocks = x.pieces * a.c.n_kv_heads;
+  for (a.block0 = 0; a.block0 < blocks; a.block0 += kMost) {
+    const uint32_t g = uint32_t(blocks - a.block0 < kMost ? blocks - a.block0 : kMost);
     if constexpr (FORM == 0) attn_kernel<T, D, 1, D == 256 ? 2 : 4, 32><<<g, D == 256 ? 128 : 256, 0, st>>>(a);
     else if constexpr (FORM == 1) attn_kernel<T, D, 2, 2, 32><<<g, 256, 0, st>>>(a);
     else if (a.page.d % (512 / D) == 0)     // the rows of a wave's load are of one page
@@ -1015,7 +1073,9 @@ void launch_form(AttnArgs a, const Launch& x, hipStream_t st) {
     else attn_wide_kernel<T, D, wide_wq(D), wide_simd(D), false><<<g, 64 * wide_wq(D), 0, st>>>(a);
   }
   constexpr int kRows = FORM == 2 ? 32 * wide_wq(D) : 32 << FORM;
-  if (x.split) attn_join_kernel<T, D, kRows><<<grid(0), 256, 0, st>>>(a);   // few pieces
+  a.block0 = 0;
+  if (x.split)                                    // few pieces
+    attn_join_kernel<T, D, kRows><<<dim3(uint32_t(blocks), kRows / 32), 256, 0, st>>>(a);
 }
 
 template <typename T, int D>
@@ -1074,9 +1134,10 @@ extern "C" int dasc_cache_attn_workspace_bytes(int32_t n_req, int64_t n_tokens, 
     Launch x;
     x.form = form;
     shape_of(x, int(D));
-    int64_t tiles = n_tokens * group / x.rows + n_req;
-    if (tiles > 2 * target) tiles = 2 * target;
-    const int64_t pieces = tiles + target;
+    // (a tile is cut only where there are few tiles)
+    const int64_t tiles = n_tokens * group / x.rows + n_req;
+    const int64_t most = form == 2 ? 2 * (2 * kUnits * wide_blocks(int(D)) / n_kv_heads + 2) : 2 * target;
+    const int64_t pieces = (tiles < most ? tiles : most) * (form == 2 ? kMostPieces + 1 : 1) + (form == 2 ? kMostPieces : target);
     const int64_t need = pieces * 16 + pieces * n_kv_heads * x.rows * (D + 2) * 4;
     if (max_kv > kMinSteps * x.keys && size_t(need) > *bytes) *bytes = size_t(need);
   }
@@ -1109,7 +1170,7 @@ extern "C" int dasc_cache_attn(const dasc_kv_cache* cache, const dasc_attn_io* i
   const int group = io->n_q_heads / cache->n_kv_heads;
   const int most = io->table_width * cache->page_size;
   const Launch x = launch_of(io->n_req, io->n_tokens, group, cache->n_kv_heads, cache->head_dim, io->max_len,
-                             io->max_kv < most ? io->max_kv : most);
+                             io->max_kv < most ? io->max_kv : most, io->window);
   AttnArgs a;
   a.c = *cache;
   a.io = *io;
@@ -1120,6 +1181,7 @@ extern "C" int dasc_cache_attn(const dasc_kv_cache* cache, const dasc_attn_io* i
   a.v_page = uint32_t(cache->v_page);
   a.v_tok = uint32_t(cache->v_tok);
   a.group = divisor(group);
+  a.heads = divisor(cache->n_kv_heads);
   a.page = divisor(cache->page_size);
   a.target = x.target;
   a.split = x.split;
