@@ -129,8 +129,8 @@ int dasc_cache_attn_workspace_bytes(int32_t n_req, int64_t n_tokens, int32_t n_q
  * < 0, causal not 0 or 1, scale not finite or below 2^-126), DASC_E_SHAPE (n_pages or page_size < 1,
  * head_dim < 8 or above 256 or no multiple of 8, n_kv_heads < 1, n_q_heads no multiple of it or
  * above 65535, n_tokens < 0 or above 2^31 - 1, n_tokens times heads per key head or table_width *
- * page_size above 2^31 - 1), DASC_E_UNSUPPORTED (a page's or a token's stride above 2^32 - 1),
- * DASC_E_WORKSPACE, DASC_E_HIP. */
+ * page_size above 2^31 - 1), DASC_E_UNSUPPORTED (a page's stride above 2^32 - 1, a
+ * token's above 2^27 - 1), DASC_E_WORKSPACE, DASC_E_HIP. */
 int dasc_cache_attn(const dasc_kv_cache *cache, const dasc_attn_io *io, void *workspace,
                     size_t workspace_bytes, dasc_stream_t stream);
 

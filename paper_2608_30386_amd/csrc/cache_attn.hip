@@ -21,6 +21,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "cache_common.h"
 #include "launch_common.h"
@@ -50,14 +51,18 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // ---- types ------------------------------------------------------------------------------------
 
+using dasc_wy::f32x4;
+
 struct Bf16 {
   typedef bf16x8 x8;
+  __device__ static f32x4 mfma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   typedef __bf16 elem;
   static constexpr uint32_t kExp = 0x7F807F80u;      // exponents of two elements
   __device__ static f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 struct F16 {
   typedef f16x8 x8;
+  __device__ static f32x4 mfma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
   typedef _Float16 elem;
   static constexpr uint32_t kExp = 0x7C007C00u;
   __device__ static f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
@@ -75,8 +80,9 @@ __device__ inline bool odd_value(u32x4 v) {
 
 // See the note on waits in linear_chunk.hip: results of matrix instructions that cross a branch
 __device__ inline void settle(f32x16& x) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(x)); }
-template <int N>
-__device__ inline void settle(f32x16 (&x)[N]) {
+__device__ inline void settle(f32x4& x) { asm volatile("s_nop 7\n\ts_nop 3" : "+v"(x)); }
+template <typename V, int N>
+__device__ inline void settle(V (&x)[N]) {
   settle(x[0]);
 #pragma unroll
   for (int i = 1; i < N; ++i) asm volatile("" : "+v"(x[i]));
@@ -97,6 +103,7 @@ struct AttnArgs {
   int64_t block0;                         // first block of this launch: piece * n_kv_heads + head
   int32_t target;                         // pieces of a key head to aim at
   int32_t split;                          // whether tiles may be split
+  int32_t least;                          // steps that a piece has at least
   float scale2;                           // scale * log2 e
   int4* meta;                             // [pieces]: of a tile's first piece, request, first row, rows, splits
   float* ml;                              // [pieces, n_kv_heads, rows of a tile, 2]
@@ -163,7 +170,7 @@ __device__ inline bool locate(const AttnArgs& a, int index, Piece& p) {
 #pragma unroll
     for (int s = 1; s < 64; s *= 2) all += __shfl_xor((unsigned long long)all, s);
     per = int64_t((all + a.target - 1) / a.target);
-    if (per < kMinSteps) per = kMinSteps;
+    if (per < a.least) per = a.least;
   }
   const auto take = [&](const Cut& c, int splits, int r0, int at, int rest) {
     const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
@@ -232,14 +239,15 @@ struct Form {
 constexpr int wide_wq(int D) { return D == 256 ? DASC_WQ256 : D == 128 ? DASC_WQ128 : DASC_WQ64; }
 constexpr int wide_simd(int D) { return D == 256 ? DASC_SIMD256 : D == 128 ? DASC_SIMD128 : DASC_SIMD64; }
 constexpr int wide_keys(int D) { return D == 256 ? 32 : D == 128 ? DASC_KW128 : DASC_KW64; }
-constexpr int few_keys(int D, int wk) { return 32 * wk; }
+constexpr int few_keys(int wk) { return 32 * wk; }
+constexpr int few_simd(int form, int D) { return form == 0 ? (D == 256 ? 1 : 2) : D == 64 ? 2 : 1; }   // waves of a SIMD, blocks of a CU
 
 // Where 16-byte chunk c of row r lies: lanes of a read that take the same chunk of many rows (keys), or a few
 // chunks of four rows (values), meet different banks
 __device__ inline int key_chunk(int r, int c) { return c ^ (r & 7); }
 template <int D>
 __device__ inline int value_chunk(int r, int c) {
-  return D == 64 ? c ^ ((r >> 1 & 1) << 2) : c ^ ((r & 3) << 2);
+  return c ^ (D == 64 ? (r >> 1 & 1) << 2 : (r & 3) << 2) ^ (r >> 2 & 1) << 1;
 }
 
 // The positions that token t of the request sees: lo .. hi
@@ -259,6 +267,7 @@ struct Row {
   int lo, hi;              // positions that it sees (a row that pads the tile: all)
   int all_lo, all_hi;      // positions that every row of the wave sees
 };
+template <int R = 32>
 __device__ inline Row row_of(const AttnArgs& a, const Piece& p, int head, int r) {
   Row x;
   const int row = p.row0 + r, G = a.group.d;
@@ -271,7 +280,7 @@ __device__ inline Row row_of(const AttnArgs& a, const Piece& p, int head, int r)
   x.all_lo = x.lo;
   x.all_hi = x.hi;
 #pragma unroll
-  for (int i = 1; i < 32; i *= 2) {
+  for (int i = 1; i < R; i *= 2) {
     const int lo = __shfl_xor(x.all_lo, i), hi = __shfl_xor(x.all_hi, i);
     x.all_lo = lo > x.all_lo ? lo : x.all_lo;
     x.all_hi = hi < x.all_hi ? hi : x.all_hi;
@@ -361,8 +370,9 @@ __device__ inline void hide(f32x16 (&s)[NS], int half, int key0, uint64_t have, 
 // The row's running base m of the weights 2^(s - m), sum l (of this half's keys) and output O, before scores
 // with maximum `top` (of this half's) join them.  The base follows the maximum only where that has left it by more
 // than 2^8 in some row: weights up to 2^8 lose nothing, and most steps leave O alone.
-template <int NO>
-__device__ inline void rebase(float top, float scale2, float& m, float& l, f32x16 (&o)[NO]) {
+template <typename V, int NO>
+__device__ inline void rebase(float top, float scale2, float& m, float& l, V (&o)[NO]) {
+  constexpr int kE = sizeof(V) / 4;
   top = fmaxf(top, __shfl_xor(top, 32)) * scale2;
   if (__any(top > m + 8.0f)) {
     const float next = fmaxf(m, top);
@@ -373,7 +383,7 @@ __device__ inline void rebase(float top, float scale2, float& m, float& l, f32x1
 #pragma unroll
     for (int i = 0; i < NO; ++i)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) o[i][e] *= shrink;
+      for (int e = 0; e < kE; ++e) o[i][e] *= shrink;
   }
 }
 template <int NS, int NO>
@@ -411,42 +421,7 @@ __device__ inline typename T::x8 value_operand(const char* lv, const Places& at,
   return x.v;
 }
 
-// O^T += V^T P^T.  The weights of 16 keys are formed while the products of the 16 before run.
-template <typename T, int D, int NS>
-__device__ inline void values(const char* lv, const Places& at, const f32x16 (&s)[NS], float scale2, float m, float& l,
-                              f32x16 (&o)[D / 32]) {
-  constexpr int kDt = D / 32, kGroups = NS * 2, kAhead = 4, kSlice = 8 / kDt;
-  const auto read = [&](int j) { return value_operand<T, D>(lv, at, j / kDt * 16, j % kDt); };
-  typename T::x8 v[kAhead], w, next;
-  const float base = base_of(m);
-#pragma unroll
-  for (int j = 0; j < kAhead; ++j) v[j] = read(j);
-  w = weights<T>(s, 0, 0, scale2, base, l);
-  hold();
-#pragma unroll
-  for (int g = 0; g < kGroups; ++g) {
-#pragma unroll
-    for (int i = 0; i < kDt; ++i) {
-      const int j = g * kDt + i;
-      o[i] = T::mfma(v[j % kAhead], w, o[i]);
-      if (j + kAhead < kGroups * kDt) v[j % kAhead] = read(j + kAhead);
-      if (g + 1 < kGroups) {
-        float sum = 0;
-#pragma unroll
-        for (int e = i * kSlice; e < (i + 1) * kSlice; ++e) {
-          const float x = __builtin_amdgcn_exp2f(fmaf(s[(g + 1) / 2][8 * ((g + 1) % 2) + e], scale2, -base));
-          next[e] = typename T::elem(x);
-          sum += x;
-        }
-        l += sum;
-      }
-      hold();
-    }
-    w = next;
-  }
-}
-
-// The same where a value that some rows do not see is not finite.  Such values count as 0 in the product, and
+// O^T += V^T P^T where a value that some rows do not see is not finite.  Such values count as 0 in the product, and
 // another product counts, for each row and column, those that the row sees: infinities in ones, negative ones
 // in 128s, NaN in 16384s.  They are added after.
 template <typename T, int D, int NS>
@@ -497,22 +472,24 @@ __device__ inline void careful(const char* lv, const Places& at, int half, int k
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// A row's result: to the workspace if its tile is split, else to the output
-template <typename T, int D>
-__device__ inline void write_row(const AttnArgs& a, const Piece& p, const Row& row, int64_t slot, int half, float m,
-                                 float l, const f32x16 (&o)[D / 32]) {
+// A row's result: to the workspace if its tile is split, else to the output.  g: the lane's part of the row, columns
+// 4 g + {0..3} of each 8 (of 32 rows), or of each 16.
+template <typename T, int D, typename V, int N>
+__device__ inline void write_row(const AttnArgs& a, const Piece& p, const Row& row, int64_t slot, int g, float m, float l,
+                                 const V (&o)[N]) {
   if (!row.real) return;
+  constexpr int kFours = D / N == 32 ? 4 : 1, kWidth = D / N == 32 ? 8 : 16;
   if (p.splits > 1) {
-    if (half == 0) {
+    if (g == 0) {
       a.ml[slot * 2] = m;
       a.ml[slot * 2 + 1] = l;
     }
     float* out = a.part + slot * D;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i)
+    for (int i = 0; i < N; ++i)
 #pragma unroll
-      for (int b = 0; b < 4; ++b)
-        *reinterpret_cast<float4*>(out + i * 32 + 8 * b + 4 * half) =
+      for (int b = 0; b < kFours; ++b)
+        *reinterpret_cast<float4*>(out + (i * kFours + b) * kWidth + 4 * g) =
             make_float4(o[i][4 * b], o[i][4 * b + 1], o[i][4 * b + 2], o[i][4 * b + 3]);
     return;
   }
@@ -522,16 +499,16 @@ __device__ inline void write_row(const AttnArgs& a, const Piece& p, const Row& r
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   elem* out = static_cast<elem*>(a.io.o) + t * a.io.o_tok + row.qh * a.io.o_head;
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i)
+  for (int i = 0; i < N; ++i)
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int c = i * 32 + 8 * b + 4 * half;
+    for (int b = 0; b < kFours; ++b) {
+      const int c = (i * kFours + b) * kWidth + 4 * g;
       e4 x;
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] = elem(o[i][4 * b + e] * inv);
       if (c < a.c.head_dim) *reinterpret_cast<e4*>(out + c) = x;
     }
-  if (a.io.lse && half == 0) a.io.lse[t * a.io.lse_tok + row.qh * a.io.lse_head] = m * 0.69314718056f + logf(l);
+  if (a.io.lse && g == 0) a.io.lse[t * a.io.lse_tok + row.qh * a.io.lse_head] = m * 0.69314718056f + logf(l);
 }
 
 // The block's piece; false if there is none.  The first block of a split tile says so to those that join.
@@ -555,16 +532,16 @@ __device__ inline Steps steps_of(const AttnArgs& a, const Piece& p) {
 
 // A piece from start to end with care for values that are not finite, for the kernels below, whose loops have no
 // register to spare for it.  WQ waves of 32 rows, and WK on the same ones, of which the first does the work.
-template <typename T, int D, int WQ, int WK>
+template <typename T, int D, int ROWS, int WQ, int WK>
 __device__ __attribute__((noinline)) void careful_piece(const AttnArgs* args, int head, int index, char* lds) {
   constexpr int KW = 32, kThreads = 64 * WQ * WK, kChunks = D / 8;
   typedef typename T::elem elem;
   const AttnArgs a = *args;
   const int tid = threadIdx.x, lane = tid % 64, n = lane % 32, half = lane / 32, wave = tid / 64 % WQ;
   Piece p;
-  if (!locate<32 * WQ, WK == 1 ? wide_keys(D) : few_keys(D, WK)>(a, index, p)) return;
-  const Steps steps = steps_of<WK == 1 ? wide_keys(D) : few_keys(D, WK)>(a, p);
-  const int per = (WK == 1 ? wide_keys(D) : few_keys(D, WK)) / KW;
+  if (!locate<ROWS, WK == 1 ? wide_keys(D) : few_keys(WK)>(a, index, p)) return;
+  const Steps steps = steps_of<WK == 1 ? wide_keys(D) : few_keys(WK)>(a, p);
+  const int per = (WK == 1 ? wide_keys(D) : few_keys(WK)) / KW;
   const Places at = places_of<D>(lane);
   const Row row = row_of(a, p, head, wave * 32 + n);
   typename T::x8 q[D / 16];
@@ -610,7 +587,7 @@ __device__ __attribute__((noinline)) void careful_piece(const AttnArgs* args, in
   if (tid / 64 >= WQ) return;
   settle(o);
   l += __shfl_xor(l, 32);
-  write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * (32 * WQ) + wave * 32 + n, half, m, l, o);
+  write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * ROWS + wave * 32 + n, half, m, l, o);
 }
 __device__ inline const AttnArgs* kernel_args() {
   return (const AttnArgs*)__builtin_amdgcn_kernarg_segment_ptr();
@@ -618,112 +595,286 @@ __device__ inline const AttnArgs* kernel_args() {
 
 // ---- few rows -------------------------------------------------------------------------------------
 
-template <typename T, int D, int WQ, int WK, int KW>
-__global__ __launch_bounds__(64 * WQ * WK) void attn_kernel(AttnArgs a) {
-  typedef Form<T, D, WQ, WK, KW> F;
+// A tile of 32 keys and R = 16 or 32 rows.  Of 16 rows, on 16 x 16 x 32 products: lane (g, n) = (lane / 16, lane % 16)
+// has keys 4 g + {0..3} of each 16 of row n, so both tiles of S^T again form the operand P^T, keys 4 g + {0..3} and
+// 16 + 4 g + {0..3} of a product.
+template <typename T, int D, int R>
+struct Tile {
+  typedef std::conditional_t<R == 32, f32x16, f32x4> Acc;
+  static constexpr int kS = 32 / R, kE = R == 32 ? 16 : 4, kO = D / R, kQ = R == 32 ? D / 16 : D / 32;
+  typedef typename T::x8 x8;
+  typename T::x8 q[kQ];
+  Acc s[kS], o[kO];
+  float m, l;
+  int key_place[R == 32 ? 4 : 2], value_place[R == 32 ? 4 : 8];
+
+  __device__ void start(const AttnArgs& a, const Piece& p, const Row& row, int lane) {
+    const int n = lane % R, g = lane / R;
+#pragma unroll
+    for (int i = 0; i < (R == 32 ? 4 : 2); ++i) key_place[i] = n * 2 * D + key_chunk(n, i * (64 / R) + g) * 16;
+    const int r = 4 * g + lane % 16 / 4;
+#pragma unroll
+    for (int i = 0; i < (R == 32 ? 4 : 8); ++i) {
+      const int c = i * R + (R == 32 ? lane % 32 / 16 * 16 : 0) + lane % 4 * 4;
+      value_place[i] = r * 2 * D + value_chunk<D>(r, c / 8) * 16 + c % 8 * 2;
+    }
+    const auto* at = static_cast<const typename T::elem*>(a.io.q) + (int64_t(p.tok0) + row.tok) * a.io.q_tok + row.qh * a.io.q_head;
+#pragma unroll
+    for (int i = 0; i < kQ; ++i) {
+      const int c = (i * (64 / R) + g) * 8;
+      u32x4 v = {0, 0, 0, 0};
+      if (row.real && c < a.c.head_dim) v = *reinterpret_cast<const u32x4*>(at + c);
+      q[i] = __builtin_bit_cast(x8, v);
+    }
+    m = -__builtin_inff();
+    l = 0;
+#pragma unroll
+    for (int i = 0; i < kO; ++i)
+#pragma unroll
+      for (int e = 0; e < kE; ++e) o[i][e] = 0;
+  }
+  __device__ static int key_of(int t, int e, int lane) {
+    return R == 32 ? 8 * (e / 4) + 4 * (lane / 32) + e % 4 : 16 * t + 4 * (lane / 16) + e;
+  }
+  __device__ x8 key_operand(const char* lk, int j) const {      // of product j: tile j / kQ, channels j % kQ
+    const int t = j / kQ, i = j % kQ;
+    if constexpr (R == 32) return *reinterpret_cast<const x8*>(lk + key_place[i % 4] + i / 4 * 128);
+    else return *reinterpret_cast<const x8*>(lk + key_place[i % 2] + i / 2 * 128 + t * 32 * D);
+  }
+  __device__ x8 value_operand(const char* lv, int j) const {    // of product j: R = 32: keys j / kO, columns j % kO
+    union { s16x4 h[2]; x8 v; } x;
+    const int i = j % kO;
+    const char* p;
+    if constexpr (R == 32) p = lv + value_place[i % 4] + j / kO * 32 * D + i / 4 * 256;
+    else p = lv + value_place[i % 8] + i / 8 * 256;
+    x.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
+    x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (R == 32 ? 16 * D : 32 * D)));
+    return x.v;
+  }
+  // S^T, hidden where it is not seen, the base, and O^T += V^T P^T
+  __device__ void step(const char* lk, const char* lv, int lane, int key0, uint64_t have, const Row& row, float scale2) {
+    constexpr int kAll = kS * kQ, kAhead = 4;
+    x8 k[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead && j < kAll; ++j) k[j] = key_operand(lk, j);
+#pragma unroll
+    for (int t = 0; t < kS; ++t)
+#pragma unroll
+      for (int e = 0; e < kE; ++e) s[t][e] = 0;
+    hold();
+#pragma unroll
+    for (int j = 0; j < kAll; ++j) {
+      s[j / kQ] = T::mfma(k[j % kAhead], q[j % kQ], s[j / kQ]);
+      if (j + kAhead < kAll) k[j % kAhead] = key_operand(lk, j + kAhead);
+      hold();
+    }
+    settle(s);
+    if (have != (uint64_t(1) << 32) - 1 || key0 < row.all_lo || key0 + 31 > row.all_hi) {
+#pragma unroll
+      for (int t = 0; t < kS; ++t)
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          const int i = key_of(t, e, lane);
+          s[t][e] = (have >> i & 1) && key0 + i >= row.lo && key0 + i <= row.hi ? s[t][e] : -__builtin_inff();
+        }
+    }
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int t = 0; t < kS; ++t)
+#pragma unroll
+      for (int e = 0; e < kE; ++e) top = fmaxf(top, s[t][e]);
+    if constexpr (R == 16) top = fmaxf(top, __shfl_xor(top, 16));
+    rebase(top, scale2, m, l, o);
+    const float base = base_of(m);
+    constexpr int kV = R == 32 ? 2 * kO : kO;
+    x8 v[kAhead], w[2];
+#pragma unroll
+    for (int j = 0; j < kAhead && j < kV; ++j) v[j] = value_operand(lv, j);
+    float sum[2] = {0, 0};
+#pragma unroll
+    for (int t = 0; t < kS; ++t)
+#pragma unroll
+      for (int e = 0; e < kE; ++e) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[t][e], scale2, -base));
+        const int at = R == 32 ? e : t * 4 + e;
+        w[at / 8][at % 8] = typename T::elem(x);
+        sum[e % 2] += x;
+      }
+    l += sum[0] + sum[1];
+    hold();
+#pragma unroll
+    for (int j = 0; j < kV; ++j) {
+      o[j % kO] = T::mfma(v[j % kAhead], w[j / kO], o[j % kO]);
+      if (j + kAhead < kV) v[j % kAhead] = value_operand(lv, j + kAhead);
+      hold();
+    }
+  }
+};
+
+// Four waves: WQ on R rows each with the same keys, the others with keys of their own, 32 a wave and step.  Each group
+// of WQ waves has its place in LDS; one that is alone needs no barrier.  Keys and values of the next step are on
+// their way in registers meanwhile, the pages of the one after too.
+template <typename T, int D, int R, int WQ, int SIMD, bool ONE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD))) void attn_few_kernel(AttnArgs a) {
+  typedef Tile<T, D, R> Tl;
+  constexpr int WK = 4 / WQ, kKeys = 32 * WK, kRows = R * WQ, kRowBytes = 2 * D, kKv = 32 * kRowBytes;
+  constexpr int kChunks = D / 8, kWaveRows = 64 / kChunks, kLoads = 32 / WQ / kWaveRows;   // rows of a load; loads of a wave
+  constexpr int kMerge = (WK - 1) * WQ * R * (D + 2) * 4;
   typedef typename T::elem elem;
-  __shared__ __attribute__((aligned(16))) char lds[2 * F::kKv > F::kMerge ? 2 * F::kKv : F::kMerge];
-  char* const lk = lds;
-  char* const lv = lds + F::kKv;
-  const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, n = lane % 32, half = lane / 32;
-  const int wq = wave % WQ, wk = wave / WQ;
+  __shared__ __attribute__((aligned(16))) char lds[2 * WK * kKv > kMerge ? 2 * WK * kKv : kMerge];
+  __shared__ int odd_flag;
+  const int tid = threadIdx.x, lane = tid % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64), wq = wave % WQ, wk = wave / WQ;
   int head, index;
   block_of(a, head, index);
   Piece p;
-  if (!take_piece<F::kRows, F::kKeys>(a, head, index, p)) return;
-  const Row row = row_of(a, p, head, wq * 32 + n);
-  const Steps steps = steps_of<F::kKeys>(a, p);
-  const Places at = places_of<D>(lane);
-  typename T::x8 q[D / 16];
-  load_query<T, D>(a, p, row, half, q);
-  f32x16 o[D / 32];
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) o[i][e] = 0;
-  float m = -__builtin_inff(), l = 0;
+  if (!take_piece<kRows, kKeys>(a, head, index, p)) return;
+  if (tid == 0) odd_flag = 0;
+  __syncthreads();
+  const Row row = row_of<R>(a, p, head, wq * R + lane % R);
+  const Steps steps = steps_of<kKeys>(a, p);
   const int d = a.c.head_dim;
 
   const int32_t* table = a.io.block_table + int64_t(p.req) * a.io.table_req;
-  const auto page_of = [&](int key) {            // -1: none
-    if (key >= p.kv) return -1;
-    const int b = table[a.page.of(key)];
-    return b >= 0 && b < a.c.n_pages ? b : -1;
-  };
   const elem* const kc = static_cast<const elem*>(a.c.k) + head * a.c.k_head;
   const elem* const vc = static_cast<const elem*>(a.c.v) + head * a.c.v_head;
-
-  for (int step = steps.begin; step < steps.end; ++step) {
-    const int key0 = step * F::kKeys;
-    u32x4 kr[F::kLoads], vr[F::kLoads];
+  // Lane r (and r + 32) knows where row r of its group's keys lies; see the kernel for many rows
+  int entry, inside;
+  const auto ask = [&](int step) {
+    int key = (step < steps.end ? step : steps.end - 1) * kKeys + wk * 32 + lane % 32;
+    key = key < p.kv ? key : p.kv - 1;
+    const int at = a.page.of(key);
+    entry = table[at];
+    inside = key - at * int(a.page.d);
+  };
+  const auto there = [&](int step) {
+    return __ballot(lane < 32 && step < steps.end && step * kKeys + wk * 32 + lane < p.kv && entry >= 0 && entry < a.c.n_pages);
+  };
+  const auto rows_at = [&](uint32_t page_stride, uint32_t tok_stride) {
+    const uint32_t b = entry >= 0 && entry < a.c.n_pages ? entry : 0;
+    return uint64_t(b) * page_stride + uint64_t(uint32_t(inside)) * tok_stride;
+  };
+  constexpr uint64_t kAll = (uint64_t(1) << 32) - 1;
+  const int chunk = lane % kChunks, column = chunk * 8 < d ? chunk * 8 : 0, first_row = wq * (32 / WQ);
+  const uint32_t k_lane = 2 * ((ONE ? lane / kChunks : 0) * a.k_tok + column);     // bytes
+  const uint32_t v_lane = 2 * ((ONE ? lane / kChunks : 0) * a.v_tok + column);
+  const auto load = [&](const elem* base, uint64_t rows, uint32_t lane_off, u32x4 (&x)[kLoads]) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      uint64_t where;
+      if constexpr (ONE) {
+        const int r = first_row + i * kWaveRows;
+        where = uint32_t(__builtin_amdgcn_readlane(int(uint32_t(rows)), r)) |
+                uint64_t(uint32_t(__builtin_amdgcn_readlane(int(uint32_t(rows >> 32)), r))) << 32;
+      } else {
+        where = __shfl((unsigned long long)rows, first_row + i * kWaveRows + lane / kChunks);
+      }
+      x[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(base + where) + lane_off);
+    }
+  };
+  char* const lk = lds + wk * 2 * kKv;
+  char* const lv = lk + kKv;
+  // Where load i goes: rows eight apart swap the same chunks
+  constexpr int kPlaces = kWaveRows >= 8 ? 1 : 8 / kWaveRows;
+  int k_place[kPlaces], v_place[kPlaces];
+#pragma unroll
+  for (int i = 0; i < kPlaces; ++i) {
+    const int r = first_row + i * kWaveRows + lane / kChunks;
+    k_place[i] = r * kRowBytes + key_chunk(r, chunk) * 16;
+    v_place[i] = r * kRowBytes + value_chunk<D>(r, chunk) * 16;
+  }
+  const auto store = [&](char* to, const int (&place)[kPlaces], uint64_t have, u32x4 (&x)[kLoads]) {
+    if (have != kAll || d < D) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        if (!(have >> (first_row + i * kWaveRows + lane / kChunks) & 1) || chunk * 8 >= d) x[i] = u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      *reinterpret_cast<u32x4*>(to + place[i % kPlaces] + i / kPlaces * kPlaces * kWaveRows * kRowBytes) = x[i];
+  };
+  const auto watch = [&](int step, const u32x4 (&x)[kLoads]) {   // what careful_piece() is for
+    const int key0 = step * kKeys + wk * 32;
+    if (key0 >= steps.all_lo && key0 + 31 <= steps.all_hi) return;
     bool odd = false;
 #pragma unroll
-    for (int i = 0; i < F::kLoads; ++i) {
-      const int at = i * F::kThreads + tid, r = at / F::kChunks, c = at % F::kChunks, key = key0 + r;
-      const int64_t b = page_of(key), off = key - int(a.page.of(key) * a.page.d);
-      kr[i] = u32x4{0, 0, 0, 0};
-      vr[i] = u32x4{0, 0, 0, 0};
-      if (b >= 0 && c * 8 < d) {
-        kr[i] = *reinterpret_cast<const u32x4*>(kc + b * a.c.k_page + off * a.c.k_tok + c * 8);
-        vr[i] = *reinterpret_cast<const u32x4*>(vc + b * a.c.v_page + off * a.c.v_tok + c * 8);
-      }
-      odd |= odd_value<T>(vr[i]);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < F::kLoads; ++i) {
-      const int at = i * F::kThreads + tid, r = at / F::kChunks, c = at % F::kChunks;
-      *reinterpret_cast<u32x4*>(lk + r * F::kRowBytes + key_chunk(r, c) * 16) = kr[i];
-      *reinterpret_cast<u32x4*>(lv + r * F::kRowBytes + value_chunk<D>(r, c) * 16) = vr[i];
-    }
-    const bool cut = key0 < steps.all_lo || key0 + F::kKeys - 1 > steps.all_hi;
-    const bool watch = __syncthreads_or(odd) && cut;
-    const int wkey = key0 + wk * KW;             // this wave's keys
-    const uint64_t have = __ballot(lane < KW && page_of(wkey + lane) >= 0);
-    f32x16 s[KW / 32];
-    scores<T, D>(lk + wk * KW * F::kRowBytes, at, q, s);
-    hide(s, half, wkey, have, row);
-    rebase(s, a.scale2, m, l, o);
-    if (watch) {
-      careful_piece<T, D, WQ, WK>(kernel_args(), head, index, lds);
-      return;
-    }
-    values<T, D>(lv + wk * KW * F::kRowBytes, at, s, a.scale2, m, l, o);
+    for (int i = 0; i < kLoads; ++i) odd |= odd_value<T>(x[i]);
+    if (odd) odd_flag = 1;
+  };
+  const bool alike = a.k_page == a.v_page && a.k_tok == a.v_tok;
+  u32x4 kr[kLoads], vr[kLoads];
+  const auto load_both = [&] {
+    const uint64_t k_rows = rows_at(a.k_page, a.k_tok);
+    load(kc, k_rows, k_lane, kr);
+    load(vc, alike ? k_rows : rows_at(a.v_page, a.v_tok), v_lane, vr);
+  };
+
+  Tl t;
+  const bool busy = steps.begin < steps.end;
+  uint64_t have = 0;
+  if (busy) {
+    ask(steps.begin);
+    have = there(steps.begin);
+    load_both();
+    ask(steps.begin + 1);
   }
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i) settle(o[i]);
-  l += __shfl_xor(l, 32);
+  t.start(a, p, row, lane);
+  if (busy) {
+    store(lk, k_place, have, kr);
+    store(lv, v_place, have, vr);
+    watch(steps.begin, vr);
+    for (int step = steps.begin; step < steps.end; ++step) {
+      const uint64_t next = there(step + 1);
+      if (step + 1 < steps.end) load_both();
+      ask(step + 2);
+      if constexpr (WQ > 1) __syncthreads();
+      t.step(lk, lv, lane, step * kKeys + wk * 32, have, row, a.scale2);
+      if constexpr (WQ > 1) __syncthreads();
+      if (step + 1 < steps.end) {
+        store(lk, k_place, next, kr);
+        store(lv, v_place, next, vr);
+        watch(step + 1, vr);
+      }
+      have = next;
+    }
+  }
+  settle(t.o);
+  if constexpr (R == 16) t.l += __shfl_xor(t.l, 16);
+  t.l += __shfl_xor(t.l, 32);
 
   // waves that share rows meet in LDS
-  if constexpr (WK > 1) {
-    __syncthreads();
-    float* const mine = reinterpret_cast<float*>(lds) + ((wk - 1) * WQ + wq) * 32 * (D + 2);
-    if (wk > 0) {
-      if (half == 0) {
-        mine[n * 2] = m;
-        mine[n * 2 + 1] = l;
-      }
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) mine[64 + (i * 16 + e) * 64 + lane] = o[i][e];
-    }
-    __syncthreads();
-    if (wk > 0) return;
-    for (int w = 1; w < WK; ++w) {
-      const float* const other = reinterpret_cast<const float*>(lds) + ((w - 1) * WQ + wq) * 32 * (D + 2);
-      const float om = other[n * 2], ol = other[n * 2 + 1];
-      const float next = fmaxf(m, om), base = next > -__builtin_inff() ? next : 0.0f;
-      const float f = __builtin_amdgcn_exp2f(m - base), g = __builtin_amdgcn_exp2f(om - base);
-      m = next;
-      l = l * f + ol * g;
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[i][e] = o[i][e] * f + other[64 + (i * 16 + e) * 64 + lane] * g;
-    }
+  __syncthreads();
+  if (odd_flag) {
+    careful_piece<T, D, kRows, WQ, WK>(kernel_args(), head, index, lds);
+    return;
   }
-  write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * F::kRows + wq * 32 + n, half, m, l, o);
+  float* const mine = reinterpret_cast<float*>(lds) + ((wk - 1) * WQ + wq) * R * (D + 2);
+  if (wk > 0) {
+    if (lane < R) {
+      mine[lane * 2] = t.m;
+      mine[lane * 2 + 1] = t.l;
+    }
+#pragma unroll
+    for (int i = 0; i < Tl::kO; ++i)
+#pragma unroll
+      for (int e = 0; e < Tl::kE; ++e) mine[2 * R + (i * Tl::kE + e) * 64 + lane] = t.o[i][e];
+  }
+  __syncthreads();
+  if (wk > 0) return;
+#pragma unroll 1
+  for (int w = 1; w < WK; ++w) {
+    const float* const other = reinterpret_cast<const float*>(lds) + ((w - 1) * WQ + wq) * R * (D + 2);
+    const float om = other[lane % R * 2], ol = other[lane % R * 2 + 1];
+    const float both = fmaxf(t.m, om), base = base_of(both);
+    const float f = __builtin_amdgcn_exp2f(t.m - base), g = __builtin_amdgcn_exp2f(om - base);
+    t.m = both;
+    t.l = t.l * f + ol * g;
+#pragma unroll
+    for (int i = 0; i < Tl::kO; ++i)
+#pragma unroll
+      for (int e = 0; e < Tl::kE; ++e) t.o[i][e] = t.o[i][e] * f + other[2 * R + (i * Tl::kE + e) * 64 + lane] * g;
+  }
+  write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * kRows + wq * R + lane % R, lane / R, t.m, t.l, t.o);
 }
 
 // ---- many rows --------------------------------------------------------------------------------------
@@ -846,9 +997,9 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
   constexpr uint64_t kAll = KW == 64 ? ~uint64_t(0) : (uint64_t(1) << 32) - 1;
   constexpr int kRow = F::kThreads / F::kChunks, kWaveRows = 64 / F::kChunks;   // rows of a load of the block, of a wave
   const int chunk = tid % F::kChunks, column = chunk * 8 < d ? chunk * 8 : 0;
-  const uint64_t k_lane = uint64_t(ONE ? lane / F::kChunks : 0) * a.k_tok + column;
-  const uint64_t v_lane = uint64_t(ONE ? lane / F::kChunks : 0) * a.v_tok + column;
-  const auto load = [&](const elem* base, uint64_t rows, uint64_t lane_off, u32x4 (&x)[F::kLoads]) {
+  const uint32_t k_lane = 2 * ((ONE ? lane / F::kChunks : 0) * a.k_tok + column);   // bytes
+  const uint32_t v_lane = 2 * ((ONE ? lane / F::kChunks : 0) * a.v_tok + column);
+  const auto load = [&](const elem* base, uint64_t rows, uint32_t lane_off, u32x4 (&x)[F::kLoads]) {
 #pragma unroll
     for (int i = 0; i < F::kLoads; ++i) {
       uint64_t at;
@@ -859,7 +1010,7 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
       } else {
         at = __shfl((unsigned long long)rows, i * kRow + tid / F::kChunks);
       }
-      x[i] = *reinterpret_cast<const u32x4*>(base + at + lane_off);
+      x[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(base + at) + lane_off);
     }
   };
   const int row_in = tid / F::kChunks;             // (kRow is a multiple of eight: loads swap the same chunks)
@@ -945,7 +1096,7 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
       kb = kb1;
     }
     if (watch) {
-      careful_piece<T, D, WQ, 1>(kernel_args(), head, index, lds);
+      careful_piece<T, D, F::kRows, WQ, 1>(kernel_args(), head, index, lds);
       return;
     }
   }
@@ -998,7 +1149,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 
 // How a call runs: the form by the rows of its longest request, pieces by the tiles that it can have
 struct Launch {
-  int form;                      // 0: 32 rows, 1: 64, 2: many
+  int form;                      // 0: up to 16 rows, 1: 32, 2: 64, 3: many
   int rows, keys;                // of a tile and a step
   int64_t pieces;                // of a key head, at most
   bool split;
@@ -1006,8 +1157,9 @@ struct Launch {
 };
 
 constexpr float kLog2e = 1.44269504089f;
-constexpr int kBlocks = 512;     // that a split call aims at
+constexpr int kWide = 3;         // the form of many rows
 constexpr int kUnits = 256;      // compute units
+constexpr int64_t kMostTok = int64_t(1) << 27;   // eight tokens' bytes fit into 32 bits
 constexpr int kMostPieces = 16;  // of a tile of many rows
 
 // Blocks of a compute unit
@@ -1015,13 +1167,21 @@ constexpr int wide_blocks(int D) { return 4 * wide_simd(D) / wide_wq(D); }
 
 int dim_of(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
+constexpr int least_steps(int form) { return form == kWide ? 4 : 2; }
+
+// Pieces of few rows: three for each place that a block has
+int few_target(int form, int D, int n_kv_heads) {
+  const int x = 3 * kUnits * few_simd(form, D) / n_kv_heads;
+  return x < 1 ? 1 : x;
+}
+
 void shape_of(Launch& x, int D) {
-  if (x.form == 2) {
+  if (x.form == kWide) {
     x.rows = 32 * wide_wq(D);
     x.keys = wide_keys(D);
   } else {
-    x.rows = 32 << x.form;
-    x.keys = x.form == 1 || D == 256 ? 64 : 128;
+    x.rows = 16 << x.form;
+    x.keys = x.form == 2 ? 64 : 128;
   }
 }
 
@@ -1030,13 +1190,13 @@ Launch launch_of(int n_req, int64_t n_tokens, int group, int n_kv_heads, int hea
   Launch x;
   const int64_t most = n_tokens < max_len ? n_tokens : max_len;
   const int64_t rows = most * group;
-  x.form = rows <= 32 ? 0 : rows <= 64 ? 1 : 2;
+  x.form = rows <= 16 ? 0 : rows <= 32 ? 1 : rows <= 64 ? 2 : kWide;
   shape_of(x, dim_of(head_dim));
   const int64_t tiles = n_tokens * group / x.rows + n_req;
   const int64_t steps = (int64_t(max_kv) + x.keys - 1) / x.keys;
   x.target = 1;
   x.split = false;
-  if (x.form == 2) {
+  if (x.form == kWide) {
     // Blocks go over the chip in rounds: a tile is cut into as many pieces as leave least of the last one empty.
     // (Requests end inside a tile, each in the middle of one on average.)
     const int64_t about = (n_tokens * group + (n_req - 1) * int64_t(x.rows / 2) + x.rows - 1) / x.rows * n_kv_heads;
@@ -1045,7 +1205,7 @@ Launch launch_of(int n_req, int64_t n_tokens, int group, int n_kv_heads, int hea
     const double length = double(reach) / x.keys;            // steps of a tile
     double best = 1e30;
     int at = 1;
-    for (int n = 1; n <= kMostPieces && (n == 1 || n * kMinSteps <= length) && (n == 1 || about < 2 * slots); ++n) {
+    for (int n = 1; n <= kMostPieces && (n == 1 || n * least_steps(kWide) <= length) && (n == 1 || about < 2 * slots); ++n) {
       // a piece's start and end cost as much as four steps, and its part of the join as much again
       const double time = double((about * n + slots - 1) / slots) * (length / n + (n > 1 ? 8 : 4));
       if (time < best) best = time, at = n;
@@ -1053,8 +1213,8 @@ Launch launch_of(int n_req, int64_t n_tokens, int group, int n_kv_heads, int hea
     x.split = at > 1;
     x.target = int(x.split ? (about * at + n_kv_heads - 1) / n_kv_heads : 1);
   } else {
-    x.target = kBlocks / n_kv_heads < 1 ? 1 : kBlocks / n_kv_heads;
-    x.split = tiles < 2 * x.target && steps > kMinSteps;
+    x.target = few_target(x.form, dim_of(head_dim), n_kv_heads);
+    x.split = tiles < 2 * x.target && steps > least_steps(x.form);
   }
   x.pieces = x.split ? tiles + x.target : tiles;
   return x;
@@ -1066,16 +1226,19 @@ void launch_form(AttnArgs a, const Launch& x, hipStream_t st) {
   const int64_t blocks = x.pieces * a.c.n_kv_heads;
   for (a.block0 = 0; a.block0 < blocks; a.block0 += kMost) {
     const uint32_t g = uint32_t(blocks - a.block0 < kMost ? blocks - a.block0 : kMost);
-    if constexpr (FORM == 0) attn_kernel<T, D, 1, D == 256 ? 2 : 4, 32><<<g, D == 256 ? 128 : 256, 0, st>>>(a);
-    else if constexpr (FORM == 1) attn_kernel<T, D, 2, 2, 32><<<g, 256, 0, st>>>(a);
-    else if (a.page.d % (512 / D) == 0)     // the rows of a wave's load are of one page
+    const bool one = a.page.d % (512 / D) == 0;   // the rows of a wave's load are of one page
+    if constexpr (FORM < kWide) {
+      constexpr int R = FORM == 0 ? 16 : 32, WQ = FORM == 2 ? 2 : 1;
+      if (one) attn_few_kernel<T, D, R, WQ, few_simd(FORM, D), true><<<g, 256, 0, st>>>(a);
+      else attn_few_kernel<T, D, R, WQ, few_simd(FORM, D), false><<<g, 256, 0, st>>>(a);
+    } else if (one)
       attn_wide_kernel<T, D, wide_wq(D), wide_simd(D), true><<<g, 64 * wide_wq(D), 0, st>>>(a);
     else attn_wide_kernel<T, D, wide_wq(D), wide_simd(D), false><<<g, 64 * wide_wq(D), 0, st>>>(a);
   }
-  constexpr int kRows = FORM == 2 ? 32 * wide_wq(D) : 32 << FORM;
+  constexpr int kRows = FORM == kWide ? 32 * wide_wq(D) : 16 << FORM;
   a.block0 = 0;
   if (x.split)                                    // few pieces
-    attn_join_kernel<T, D, kRows><<<dim3(uint32_t(blocks), kRows / 32), 256, 0, st>>>(a);
+    attn_join_kernel<T, D, kRows><<<dim3(uint32_t(blocks), (kRows + 31) / 32), 256, 0, st>>>(a);
 }
 
 template <typename T, int D>
@@ -1083,7 +1246,8 @@ void launch_rows(const AttnArgs& a, const Launch& x, hipStream_t st) {
   switch (x.form) {
     case 0: launch_form<T, D, 0>(a, x, st); break;
     case 1: launch_form<T, D, 1>(a, x, st); break;
-    default: launch_form<T, D, 2>(a, x, st); break;
+    case 2: launch_form<T, D, 2>(a, x, st); break;
+    default: launch_form<T, D, kWide>(a, x, st); break;
   }
 }
 
@@ -1127,19 +1291,18 @@ extern "C" int dasc_cache_attn_workspace_bytes(int32_t n_req, int64_t n_tokens, 
   // the largest need of any smaller call: each form at its most tiles
   const int group = n_q_heads / n_kv_heads;
   const int64_t D = dim_of(head_dim);
-  int target = kBlocks / n_kv_heads;
-  if (target < 1) target = 1;
-  for (int form = 0; form < 3; ++form) {
-    if (form > 0 && int64_t(max_len) * group <= (16 << form)) continue;   // no request that takes it
+  for (int form = 0; form <= kWide; ++form) {
+    if (form > 0 && int64_t(max_len) * group <= (8 << form)) continue;    // no request that takes it
     Launch x;
     x.form = form;
     shape_of(x, int(D));
     // (a tile is cut only where there are few tiles)
-    const int64_t tiles = n_tokens * group / x.rows + n_req;
-    const int64_t most = form == 2 ? 2 * (2 * kUnits * wide_blocks(int(D)) / n_kv_heads + 2) : 2 * target;
-    const int64_t pieces = (tiles < most ? tiles : most) * (form == 2 ? kMostPieces + 1 : 1) + (form == 2 ? kMostPieces : target);
+    const int64_t tiles = n_tokens * group / x.rows + n_req, target = few_target(form, int(D), n_kv_heads);
+    const int64_t most = form == kWide ? 2 * (2 * kUnits * wide_blocks(int(D)) / n_kv_heads + 2) : 2 * target;
+    const int64_t pieces = (tiles < most ? tiles : most) * (form == kWide ? kMostPieces + 1 : 1) +
+                           (form == kWide ? kMostPieces : target);
     const int64_t need = pieces * 16 + pieces * n_kv_heads * x.rows * (D + 2) * 4;
-    if (max_kv > kMinSteps * x.keys && size_t(need) > *bytes) *bytes = size_t(need);
+    if (max_kv > least_steps(form) * x.keys && size_t(need) > *bytes) *bytes = size_t(need);
   }
   return DASC_OK;
 }
@@ -1174,8 +1337,8 @@ extern "C" int dasc_cache_attn(const dasc_kv_cache* cache, const dasc_attn_io* i
   AttnArgs a;
   a.c = *cache;
   a.io = *io;
-  for (const int64_t stride : {cache->k_page, cache->k_tok, cache->v_page, cache->v_tok})
-    if (stride > UINT32_MAX) return DASC_E_UNSUPPORTED;
+  if (cache->k_page > UINT32_MAX || cache->v_page > UINT32_MAX || cache->k_tok >= kMostTok || cache->v_tok >= kMostTok)
+    return DASC_E_UNSUPPORTED;
   a.k_page = uint32_t(cache->k_page);
   a.k_tok = uint32_t(cache->k_tok);
   a.v_page = uint32_t(cache->v_page);
@@ -1185,6 +1348,7 @@ extern "C" int dasc_cache_attn(const dasc_kv_cache* cache, const dasc_attn_io* i
   a.page = divisor(cache->page_size);
   a.target = x.target;
   a.split = x.split;
+  a.least = least_steps(x.form);
   a.scale2 = io->scale * kLog2e;
   a.meta = nullptr;
   a.ml = a.part = nullptr;

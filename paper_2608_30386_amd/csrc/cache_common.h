@@ -7,8 +7,6 @@
 
 namespace dasc {
 
-constexpr int kMinSteps = 4;     // steps of keys that a piece of attention has at least
-
 inline bool aligned_to(const void* p, int n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
 // A cache whose rows are aligned to `align` bytes
