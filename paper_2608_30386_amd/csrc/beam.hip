@@ -5,15 +5,15 @@
 // Within a row the order is that of the logits, so a row's tiles each give their n_out best logits and
 // their part of the sum, and one block per request merges them: first each beam's lists, then the beams'.
 //
-// The best n of a tile's keys (logit and token in one 64-bit number, all different) without sorting it:
-// every lane takes its largest key; n lanes of a wave have one at or above the n-th largest of those, so at
-// least n keys of the tile lie at or above it, and only keys in those lanes can be among them.  The n-th
-// largest is found bit by bit with ballots; what is at or above it is gathered in LDS and ranked by
-// comparing all with all.
+// The best n of a tile (logit and token in one 64-bit key, all different) without sorting it: every lane takes its
+// largest logit; n lanes of a wave have one at or above the n-th largest of those, so at least n of the tile lie at
+// or above it.  That is found bit by bit with ballots; what is at or above the largest of the waves' is
+// gathered in LDS, a few times n as a rule, and ranked by comparing all with all.
 
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "cache_common.h"
 #include "launch_common.h"
@@ -55,13 +55,23 @@ __device__ inline float unordered(uint32_t k) {
 __device__ inline uint64_t key_of(float x, uint32_t token) { return (uint64_t(ordered(x)) << 32) | (0xFFFFFFFFu - token); }
 __device__ inline uint32_t token_of(uint64_t key) { return 0xFFFFFFFFu - uint32_t(key); }
 
-// The largest number that at least n of the wave's keys reach (0 if fewer than n are not 0); exactly n
-// reach it where keys differ.
-__device__ inline uint64_t reached_by(uint64_t key, int n) {
+// The largest number that at least n of the wave's keys reach (0 if fewer than n are not 0), bit by bit from the
+// first in which the keys differ; of different keys just n reach it.
+template <typename U>
+__device__ inline U reached_by(U key, int n) {
   if (__popcll(__ballot(key != 0)) < n) return 0;
-  uint64_t t = 0;
-  for (int bit = 63; bit >= 0; --bit) {
-    const uint64_t x = t | (uint64_t(1) << bit);
+  U all = key, any = key;
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) {
+    all &= U(__shfl_xor((std::conditional_t<sizeof(U) == 8, unsigned long long, unsigned>)all, s));
+    any |= U(__shfl_xor((std::conditional_t<sizeof(U) == 8, unsigned long long, unsigned>)any, s));
+  }
+  const U differ = all ^ any;
+  if (differ == 0) return all;
+  int bit = sizeof(U) == 8 ? 63 - __builtin_clzll(differ) : 31 - __builtin_clz(uint32_t(differ));
+  U t = bit + 1 < int(sizeof(U)) * 8 ? any >> (bit + 1) << (bit + 1) : 0;
+  for (; bit >= 0; --bit) {
+    const U x = t | (U(1) << bit);
     const int c = __popcll(__ballot(key >= x));
     if (c >= n) t = x;
     if (c == n) break;
@@ -69,18 +79,12 @@ __device__ inline uint64_t reached_by(uint64_t key, int n) {
   return t;
 }
 
-// e^x for x <= 0 in 64 bits: 2^n e^r with r at most ln 2 / 2, the exponential's series to r^13 / 13!
-// (the first term left out is below 2^-57)
+// e^x for x <= 0 in 64 bits, to 2^-36: 2^n e^r with r at most ln 2 / 2, the exponential's series to r^9 / 9!
+// (the first term left out is below 2^-36 of the sum, and n ln 2 good to 2^-43)
 __device__ inline double exp64(double x) {
-  if (x < -700.0) return 0.0;
   const double n = rint(x * 1.4426950408889634074);
-  double r = fma(n, -0.69314718055994530942, x);           // ln 2 rounded, and what that leaves of it
-  r = fma(n, -2.3190468138462996e-17, r);
-  double p = 1.0 / 6227020800.0;
-  p = fma(p, r, 1.0 / 479001600.0);
-  p = fma(p, r, 1.0 / 39916800.0);
-  p = fma(p, r, 1.0 / 3628800.0);
-  p = fma(p, r, 1.0 / 362880.0);
+  const double r = fma(n, -0.69314718055994530942, x);
+  double p = 1.0 / 362880.0;
   p = fma(p, r, 1.0 / 40320.0);
   p = fma(p, r, 1.0 / 5040.0);
   p = fma(p, r, 1.0 / 720.0);
@@ -90,14 +94,44 @@ __device__ inline double exp64(double x) {
   p = fma(p, r, 0.5);
   p = fma(p, r, 1.0);
   p = fma(p, r, 1.0);
-  return __longlong_as_double(__double_as_longlong(p) + (int64_t(n) << 52));
+  return __builtin_amdgcn_ldexp(p, n > -2000.0 ? int(n) : -2000);
+}
+
+// A list of c different keys cut to its n largest, of which there are more: the n-th largest bit by bit, the block
+// counting.  For rows with many equal logits, or with the large ones in a few lanes.
+constexpr int kRanked = 512;
+__device__ inline int narrow_list(uint64_t* list, int c, int n, int* count) {
+  uint64_t mine[kTile / kThreads], t = 0;
+#pragma unroll
+  for (int i = 0; i < kTile / kThreads; ++i) mine[i] = int(i * kThreads + threadIdx.x) < c ? list[i * kThreads + threadIdx.x] : 0;
+  for (int bit = 63; bit >= 0; --bit) {
+    const uint64_t x = t | (uint64_t(1) << bit);
+    __syncthreads();
+    if (threadIdx.x == 0) *count = 0;
+    __syncthreads();
+    int some = 0;
+#pragma unroll
+    for (int i = 0; i < kTile / kThreads; ++i) some += __popcll(__ballot(mine[i] >= x));
+    if (threadIdx.x % 64 == 0 && some) atomicAdd(count, some);
+    __syncthreads();
+    if (*count >= n) t = x;
+    if (*count == n) break;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) *count = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kTile / kThreads; ++i)
+    if (mine[i] >= t) list[atomicAdd(count, 1)] = mine[i];
+  __syncthreads();
+  return *count;
 }
 
 // A tile of a row: its largest logit, the sum of exponentials against it, its n_out best keys.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void beam_scan_kernel(BeamArgs a) {
   __shared__ uint64_t list[kTile];
-  __shared__ uint64_t limit[kThreads / 64];
+  __shared__ uint32_t limit[kThreads / 64];
   __shared__ float top[kThreads / 64];
   __shared__ double part[kThreads / 64];
   __shared__ int count;
@@ -119,30 +153,25 @@ __global__ __launch_bounds__(kThreads) void beam_scan_kernel(BeamArgs a) {
     if (!(x[i] < inf)) x[i] = -inf;
     m = fmaxf(m, x[i]);
   }
-  uint64_t best = 0;
-#pragma unroll
-  for (int i = 0; i < 16; ++i)                         // the lane's largest, the lowest token of equal ones
-    if (x[i] == m && m > -inf && best == 0) best = key_of(m, base + i % 8 + i / 8 * (kTile / 2));
-  const uint64_t t = reached_by(best, a.n_out);
+  // n_out lanes of a wave have a logit at or above its floor, so the block has n_out at or above each
+  const uint32_t t = reached_by<uint32_t>(m > -inf ? ordered(m) : 0, a.n_out);
   float wm = m;
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) wm = fmaxf(wm, __shfl_xor(wm, s));
   if (tid % 64 == 0) limit[wave] = t, top[wave] = wm;
   if (tid == 0) count = 0;
   __syncthreads();
-  uint64_t floor_key = 1;
+  uint32_t low = ordered(-inf) + 1;
   float bm = -inf;
 #pragma unroll
   for (int i = 0; i < kThreads / 64; ++i) {
-    floor_key = limit[i] > floor_key ? limit[i] : floor_key;
+    low = limit[i] > low ? limit[i] : low;
     bm = fmaxf(bm, top[i]);
   }
-  if (best >= floor_key) {
+  if (ordered(m) >= low) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const uint64_t key = x[i] > -inf ? key_of(x[i], base + i % 8 + i / 8 * (kTile / 2)) : 0;
-      if (key >= floor_key) list[atomicAdd(&count, 1)] = key;
-    }
+    for (int i = 0; i < 16; ++i)
+      if (ordered(x[i]) >= low) list[atomicAdd(&count, 1)] = key_of(x[i], base + i % 8 + i / 8 * (kTile / 2));
   }
   double sum = bad ? __longlong_as_double(0x7FF8000000000000) : 0.0;
 #pragma unroll
@@ -159,8 +188,9 @@ __global__ __launch_bounds__(kThreads) void beam_scan_kernel(BeamArgs a) {
     a.sums[at] = all;
     a.tops[at] = bm;
   }
-  const int c = count;
+  int c = count;
   uint64_t* out = a.keys + at * a.n_out;
+  if (c > kRanked) c = narrow_list(list, c, a.n_out, &count);
   for (int i = tid; i < c; i += kThreads) {
     const uint64_t key = list[i];
     int rank = 0;
@@ -213,7 +243,7 @@ __global__ __launch_bounds__(kPickWaves * 64) void beam_pick_kernel(BeamArgs a) 
         k[i] = j < total ? keys[j] : 0;
         best = k[i] > best ? k[i] : best;
       }
-      uint64_t t = reached_by(best, n);
+      uint64_t t = reached_by<uint64_t>(best, n);
       if (t == 0) t = 1;
       int c = 0;
 #pragma unroll
@@ -309,26 +339,24 @@ struct MoveArgs {
 };
 
 // A thread has one word of every slot of a group: it loads all of them, then stores all of them, so no order
-// of the moves matters.
+// of the moves matters.  The indices are the same for a wave, so that the addresses take no vector registers.
 template <typename V, int M>
 __global__ __launch_bounds__(256) void move_kernel(MoveArgs a) {
-  const int64_t w = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  const uint32_t w = blockIdx.x * 256 + threadIdx.x;
   if (w >= a.words) return;
-  const int32_t* src = a.src + blockIdx.y * a.src_group;
-  const int32_t* dst = a.dst + blockIdx.y * a.dst_group;
+  typedef const __attribute__((address_space(4))) int32_t* list_t;
+  const list_t src = list_t(uintptr_t(a.src + blockIdx.y * a.src_group)), dst = list_t(uintptr_t(a.dst + blockIdx.y * a.dst_group));
+  const auto moved = [&](int j) {
+    const int s = src[j], d = dst[j];
+    return s >= 0 && s < a.n_slots && d >= 0 && d < a.n_slots && s != d;
+  };
   V x[M];
 #pragma unroll
-  for (int j = 0; j < M; ++j) {
-    const int s = j < a.m ? src[j] : -1, d = j < a.m ? dst[j] : -1;
-    if (s >= 0 && s < a.n_slots && d >= 0 && d < a.n_slots && s != d)
-      x[j] = reinterpret_cast<const V*>(a.pool + s * a.stride)[w];
-  }
+  for (int j = 0; j < M; ++j)
+    if (j < a.m && moved(j)) x[j] = reinterpret_cast<const V*>(a.pool + src[j] * a.stride)[w];
 #pragma unroll
-  for (int j = 0; j < M; ++j) {
-    const int s = j < a.m ? src[j] : -1, d = j < a.m ? dst[j] : -1;
-    if (s >= 0 && s < a.n_slots && d >= 0 && d < a.n_slots && s != d)
-      reinterpret_cast<V*>(a.pool + d * a.stride)[w] = x[j];
-  }
+  for (int j = 0; j < M; ++j)
+    if (j < a.m && moved(j)) __builtin_nontemporal_store(x[j], reinterpret_cast<V*>(a.pool + dst[j] * a.stride) + w);
 }
 
 template <typename V, int M>

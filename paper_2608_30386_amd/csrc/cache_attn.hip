@@ -160,11 +160,12 @@ __device__ inline Cut cut_of(const AttnArgs& a, int r) {
 template <int ROWS, int KEYS>
 __device__ inline bool locate(const AttnArgs& a, int index, Piece& p) {
   const int lane = threadIdx.x % 64;
+  const Cut first = cut_of<ROWS, KEYS>(a, lane);
   int64_t per = int64_t(1) << 40;         // steps of a piece
   if (a.split) {
     uint64_t all = 0;
     for (int r0 = 0; r0 < a.io.n_req; r0 += 64) {
-      const Cut c = cut_of<ROWS, KEYS>(a, r0 + lane);
+      const Cut c = r0 ? cut_of<ROWS, KEYS>(a, r0 + lane) : first;
       all += uint64_t(c.tiles) * uint64_t(c.steps);
     }
 #pragma unroll
@@ -187,7 +188,7 @@ __device__ inline bool locate(const AttnArgs& a, int index, Piece& p) {
     p.rows = left < ROWS ? left : ROWS;
   };
   if (!a.split && a.io.n_req <= 64) {     // whole tiles: the longest request's first
-    const Cut c = cut_of<ROWS, KEYS>(a, lane);
+    const Cut& c = first;
     int64_t before = 0;
     for (int j = 0; j < a.io.n_req; ++j) {
       const int steps = __builtin_amdgcn_readlane(c.steps, j), tiles = __builtin_amdgcn_readlane(c.tiles, j);
@@ -201,7 +202,7 @@ __device__ inline bool locate(const AttnArgs& a, int index, Piece& p) {
   }
   int64_t before = 0;
   for (int r0 = 0; r0 < a.io.n_req; r0 += 64) {
-    const Cut c = cut_of<ROWS, KEYS>(a, r0 + lane);
+    const Cut c = r0 ? cut_of<ROWS, KEYS>(a, r0 + lane) : first;
     const int splits = a.split ? int((c.steps + per - 1) / per) : 1;
     const int64_t mine = int64_t(c.tiles) * splits;
     int64_t upto = mine;
@@ -239,8 +240,7 @@ struct Form {
 constexpr int wide_wq(int D) { return D == 256 ? DASC_WQ256 : D == 128 ? DASC_WQ128 : DASC_WQ64; }
 constexpr int wide_simd(int D) { return D == 256 ? DASC_SIMD256 : D == 128 ? DASC_SIMD128 : DASC_SIMD64; }
 constexpr int wide_keys(int D) { return D == 256 ? 32 : D == 128 ? DASC_KW128 : DASC_KW64; }
-constexpr int few_keys(int wk) { return 32 * wk; }
-constexpr int few_simd(int form, int D) { return form == 0 ? (D == 256 ? 1 : 2) : D == 64 ? 2 : 1; }   // waves of a SIMD, blocks of a CU
+constexpr int few_simd(int form, int D) { return D == 256 && form == 0 ? 1 : 2; }   // waves of a SIMD, blocks of a CU
 
 // Where 16-byte chunk c of row r lies: lanes of a read that take the same chunk of many rows (keys), or a few
 // chunks of four rows (values), meet different banks
@@ -531,17 +531,16 @@ __device__ inline Steps steps_of(const AttnArgs& a, const Piece& p) {
 }
 
 // A piece from start to end with care for values that are not finite, for the kernels below, whose loops have no
-// register to spare for it.  WQ waves of 32 rows, and WK on the same ones, of which the first does the work.
-template <typename T, int D, int ROWS, int WQ, int WK>
+// register to spare for it.  Waves that have no 32 rows of their own help to load.
+template <typename T, int D, int ROWS, int KEYS, int WAVES>
 __device__ __attribute__((noinline)) void careful_piece(const AttnArgs* args, int head, int index, char* lds) {
-  constexpr int KW = 32, kThreads = 64 * WQ * WK, kChunks = D / 8;
+  constexpr int KW = 32, kThreads = 64 * WAVES, kChunks = D / 8, WQ = (ROWS + 31) / 32, per = KEYS / KW;
   typedef typename T::elem elem;
   const AttnArgs a = *args;
   const int tid = threadIdx.x, lane = tid % 64, n = lane % 32, half = lane / 32, wave = tid / 64 % WQ;
   Piece p;
-  if (!locate<ROWS, WK == 1 ? wide_keys(D) : few_keys(WK)>(a, index, p)) return;
-  const Steps steps = steps_of<WK == 1 ? wide_keys(D) : few_keys(WK)>(a, p);
-  const int per = (WK == 1 ? wide_keys(D) : few_keys(WK)) / KW;
+  if (!locate<ROWS, KEYS>(a, index, p)) return;
+  const Steps steps = steps_of<KEYS>(a, p);
   const Places at = places_of<D>(lane);
   const Row row = row_of(a, p, head, wave * 32 + n);
   typename T::x8 q[D / 16];
@@ -595,33 +594,32 @@ __device__ inline const AttnArgs* kernel_args() {
 
 // ---- few rows -------------------------------------------------------------------------------------
 
-// A tile of 32 keys and R = 16 or 32 rows.  Of 16 rows, on 16 x 16 x 32 products: lane (g, n) = (lane / 16, lane % 16)
-// has keys 4 g + {0..3} of each 16 of row n, so both tiles of S^T again form the operand P^T, keys 4 g + {0..3} and
+// A tile of 32 keys and 16 rows, on 16 x 16 x 32 products: lane (g, n) = (lane / 16, lane % 16) has keys
+// 4 g + {0..3} of each 16 of row n, so both tiles of S^T again form the operand P^T, keys 4 g + {0..3} and
 // 16 + 4 g + {0..3} of a product.
-template <typename T, int D, int R>
+template <typename T, int D>
 struct Tile {
-  typedef std::conditional_t<R == 32, f32x16, f32x4> Acc;
-  static constexpr int kS = 32 / R, kE = R == 32 ? 16 : 4, kO = D / R, kQ = R == 32 ? D / 16 : D / 32;
+  static constexpr int kO = D / 16, kQ = D / 32;
   typedef typename T::x8 x8;
-  typename T::x8 q[kQ];
-  Acc s[kS], o[kO];
+  x8 q[kQ];
+  f32x4 o[kO];
   float m, l;
-  int key_place[R == 32 ? 4 : 2], value_place[R == 32 ? 4 : 8];
+  int key_place[2], value_place[8];
 
   __device__ void start(const AttnArgs& a, const Piece& p, const Row& row, int lane) {
-    const int n = lane % R, g = lane / R;
+    const int n = lane % 16, g = lane / 16;
 #pragma unroll
-    for (int i = 0; i < (R == 32 ? 4 : 2); ++i) key_place[i] = n * 2 * D + key_chunk(n, i * (64 / R) + g) * 16;
-    const int r = 4 * g + lane % 16 / 4;
+    for (int i = 0; i < 2; ++i) key_place[i] = n * 2 * D + key_chunk(n, 4 * i + g) * 16;
+    const int r = 4 * g + n / 4;
 #pragma unroll
-    for (int i = 0; i < (R == 32 ? 4 : 8); ++i) {
-      const int c = i * R + (R == 32 ? lane % 32 / 16 * 16 : 0) + lane % 4 * 4;
+    for (int i = 0; i < 8; ++i) {
+      const int c = i * 16 + lane % 4 * 4;
       value_place[i] = r * 2 * D + value_chunk<D>(r, c / 8) * 16 + c % 8 * 2;
     }
     const auto* at = static_cast<const typename T::elem*>(a.io.q) + (int64_t(p.tok0) + row.tok) * a.io.q_tok + row.qh * a.io.q_head;
 #pragma unroll
     for (int i = 0; i < kQ; ++i) {
-      const int c = (i * (64 / R) + g) * 8;
+      const int c = (4 * i + g) * 8;
       u32x4 v = {0, 0, 0, 0};
       if (row.real && c < a.c.head_dim) v = *reinterpret_cast<const u32x4*>(at + c);
       q[i] = __builtin_bit_cast(x8, v);
@@ -631,36 +629,30 @@ struct Tile {
 #pragma unroll
     for (int i = 0; i < kO; ++i)
 #pragma unroll
-      for (int e = 0; e < kE; ++e) o[i][e] = 0;
+      for (int e = 0; e < 4; ++e) o[i][e] = 0;
   }
-  __device__ static int key_of(int t, int e, int lane) {
-    return R == 32 ? 8 * (e / 4) + 4 * (lane / 32) + e % 4 : 16 * t + 4 * (lane / 16) + e;
-  }
-  __device__ x8 key_operand(const char* lk, int j) const {      // of product j: tile j / kQ, channels j % kQ
+  __device__ x8 key_operand(const char* lk, int j) const {      // of product j: keys 16 (j / kQ) .., channels j % kQ
     const int t = j / kQ, i = j % kQ;
-    if constexpr (R == 32) return *reinterpret_cast<const x8*>(lk + key_place[i % 4] + i / 4 * 128);
-    else return *reinterpret_cast<const x8*>(lk + key_place[i % 2] + i / 2 * 128 + t * 32 * D);
+    return *reinterpret_cast<const x8*>(lk + key_place[i % 2] + i / 2 * 128 + t * 32 * D);
   }
-  __device__ x8 value_operand(const char* lv, int j) const {    // of product j: R = 32: keys j / kO, columns j % kO
+  __device__ x8 value_operand(const char* lv, int i) const {    // columns 16 i ..
     union { s16x4 h[2]; x8 v; } x;
-    const int i = j % kO;
-    const char* p;
-    if constexpr (R == 32) p = lv + value_place[i % 4] + j / kO * 32 * D + i / 4 * 256;
-    else p = lv + value_place[i % 8] + i / 8 * 256;
+    const char* p = lv + value_place[i % 8] + i / 8 * 256;
     x.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
-    x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (R == 32 ? 16 * D : 32 * D)));
+    x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 32 * D));
     return x.v;
   }
   // S^T, hidden where it is not seen, the base, and O^T += V^T P^T
   __device__ void step(const char* lk, const char* lv, int lane, int key0, uint64_t have, const Row& row, float scale2) {
-    constexpr int kAll = kS * kQ, kAhead = 4;
+    constexpr int kAll = 2 * kQ, kAhead = 4;
     x8 k[kAhead];
+    f32x4 s[2];
 #pragma unroll
-    for (int j = 0; j < kAhead && j < kAll; ++j) k[j] = key_operand(lk, j);
+    for (int j = 0; j < kAhead; ++j) k[j] = key_operand(lk, j);
 #pragma unroll
-    for (int t = 0; t < kS; ++t)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int e = 0; e < kE; ++e) s[t][e] = 0;
+      for (int e = 0; e < 4; ++e) s[t][e] = 0;
     hold();
 #pragma unroll
     for (int j = 0; j < kAll; ++j) {
@@ -671,53 +663,49 @@ struct Tile {
     settle(s);
     if (have != (uint64_t(1) << 32) - 1 || key0 < row.all_lo || key0 + 31 > row.all_hi) {
 #pragma unroll
-      for (int t = 0; t < kS; ++t)
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < kE; ++e) {
-          const int i = key_of(t, e, lane);
+        for (int e = 0; e < 4; ++e) {
+          const int i = 16 * t + 4 * (lane / 16) + e;
           s[t][e] = (have >> i & 1) && key0 + i >= row.lo && key0 + i <= row.hi ? s[t][e] : -__builtin_inff();
         }
     }
     float top = -__builtin_inff();
 #pragma unroll
-    for (int t = 0; t < kS; ++t)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int e = 0; e < kE; ++e) top = fmaxf(top, s[t][e]);
-    if constexpr (R == 16) top = fmaxf(top, __shfl_xor(top, 16));
-    rebase(top, scale2, m, l, o);
+      for (int e = 0; e < 4; ++e) top = fmaxf(top, s[t][e]);
+    rebase(fmaxf(top, __shfl_xor(top, 16)), scale2, m, l, o);
     const float base = base_of(m);
-    constexpr int kV = R == 32 ? 2 * kO : kO;
-    x8 v[kAhead], w[2];
+    x8 v[kAhead], w;
 #pragma unroll
-    for (int j = 0; j < kAhead && j < kV; ++j) v[j] = value_operand(lv, j);
+    for (int j = 0; j < kAhead; ++j) v[j] = value_operand(lv, j);
     float sum[2] = {0, 0};
 #pragma unroll
-    for (int t = 0; t < kS; ++t)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int e = 0; e < kE; ++e) {
+      for (int e = 0; e < 4; ++e) {
         const float x = __builtin_amdgcn_exp2f(fmaf(s[t][e], scale2, -base));
-        const int at = R == 32 ? e : t * 4 + e;
-        w[at / 8][at % 8] = typename T::elem(x);
+        w[t * 4 + e] = typename T::elem(x);
         sum[e % 2] += x;
       }
     l += sum[0] + sum[1];
     hold();
 #pragma unroll
-    for (int j = 0; j < kV; ++j) {
-      o[j % kO] = T::mfma(v[j % kAhead], w[j / kO], o[j % kO]);
-      if (j + kAhead < kV) v[j % kAhead] = value_operand(lv, j + kAhead);
+    for (int j = 0; j < kO; ++j) {
+      o[j] = T::mfma(v[j % kAhead], w, o[j]);
+      if (j + kAhead < kO) v[j % kAhead] = value_operand(lv, j + kAhead);
       hold();
     }
   }
 };
 
-// Four waves: WQ on R rows each with the same keys, the others with keys of their own, 32 a wave and step.  Each group
+// Four waves: WQ on 16 rows each with the same keys, the others with keys of their own, 32 a wave and step.  Each group
 // of WQ waves has its place in LDS; one that is alone needs no barrier.  Keys and values of the next step are on
 // their way in registers meanwhile, the pages of the one after too.
-template <typename T, int D, int R, int WQ, int SIMD, bool ONE>
+template <typename T, int D, int WQ, int SIMD, bool ONE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD))) void attn_few_kernel(AttnArgs a) {
-  typedef Tile<T, D, R> Tl;
-  constexpr int WK = 4 / WQ, kKeys = 32 * WK, kRows = R * WQ, kRowBytes = 2 * D, kKv = 32 * kRowBytes;
+  constexpr int R = 16, WK = 4 / WQ, kKeys = 32 * WK, kRows = R * WQ, kRowBytes = 2 * D, kKv = 32 * kRowBytes;
   constexpr int kChunks = D / 8, kWaveRows = 64 / kChunks, kLoads = 32 / WQ / kWaveRows;   // rows of a load; loads of a wave
   constexpr int kMerge = (WK - 1) * WQ * R * (D + 2) * 4;
   typedef typename T::elem elem;
@@ -809,7 +797,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD)
     load(vc, alike ? k_rows : rows_at(a.v_page, a.v_tok), v_lane, vr);
   };
 
-  Tl t;
+  Tile<T, D> t;
   const bool busy = steps.begin < steps.end;
   uint64_t have = 0;
   if (busy) {
@@ -823,6 +811,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD)
     store(lk, k_place, have, kr);
     store(lv, v_place, have, vr);
     watch(steps.begin, vr);
+    // (else the first product of every step would wait for the queries' loads, and so for all that came after)
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      u32x4 x = __builtin_bit_cast(u32x4, t.q[i]);
+      asm volatile("" : "+v"(x));
+      t.q[i] = __builtin_bit_cast(typename T::x8, x);
+    }
     for (int step = steps.begin; step < steps.end; ++step) {
       const uint64_t next = there(step + 1);
       if (step + 1 < steps.end) load_both();
@@ -839,40 +834,43 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD)
     }
   }
   settle(t.o);
-  if constexpr (R == 16) t.l += __shfl_xor(t.l, 16);
+  t.l += __shfl_xor(t.l, 16);
   t.l += __shfl_xor(t.l, 32);
 
   // waves that share rows meet in LDS
   __syncthreads();
   if (odd_flag) {
-    careful_piece<T, D, kRows, WQ, WK>(kernel_args(), head, index, lds);
+    careful_piece<T, D, kRows, kKeys, 4>(kernel_args(), head, index, lds);
     return;
   }
-  float* const mine = reinterpret_cast<float*>(lds) + ((wk - 1) * WQ + wq) * R * (D + 2);
-  if (wk > 0) {
-    if (lane < R) {
-      mine[lane * 2] = t.m;
-      mine[lane * 2 + 1] = t.l;
+  if constexpr (WK > 1) {
+    const auto part = [&](int w) { return reinterpret_cast<float*>(lds) + ((w - 1) * WQ + wq) * R * (D + 2); };
+    if (wk > 0) {
+      float* const mine = part(wk);
+      if (lane < R) {
+        mine[lane * 2] = t.m;
+        mine[lane * 2 + 1] = t.l;
+      }
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(mine + 2 * R + (i * 64 + lane) * 4) = t.o[i];
     }
-#pragma unroll
-    for (int i = 0; i < Tl::kO; ++i)
-#pragma unroll
-      for (int e = 0; e < Tl::kE; ++e) mine[2 * R + (i * Tl::kE + e) * 64 + lane] = t.o[i][e];
-  }
-  __syncthreads();
-  if (wk > 0) return;
+    __syncthreads();
+    if (wk > 0) return;
 #pragma unroll 1
-  for (int w = 1; w < WK; ++w) {
-    const float* const other = reinterpret_cast<const float*>(lds) + ((w - 1) * WQ + wq) * R * (D + 2);
-    const float om = other[lane % R * 2], ol = other[lane % R * 2 + 1];
-    const float both = fmaxf(t.m, om), base = base_of(both);
-    const float f = __builtin_amdgcn_exp2f(t.m - base), g = __builtin_amdgcn_exp2f(om - base);
-    t.m = both;
-    t.l = t.l * f + ol * g;
+    for (int w = 1; w < WK; ++w) {
+      const float* const other = part(w);
+      const float om = other[lane % R * 2], ol = other[lane % R * 2 + 1];
+      const float both = fmaxf(t.m, om), base = base_of(both);
+      const float f = __builtin_amdgcn_exp2f(t.m - base), g = __builtin_amdgcn_exp2f(om - base);
+      t.m = both;
+      t.l = t.l * f + ol * g;
 #pragma unroll
-    for (int i = 0; i < Tl::kO; ++i)
+      for (int i = 0; i < D / 16; ++i) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(other + 2 * R + (i * 64 + lane) * 4);
 #pragma unroll
-      for (int e = 0; e < Tl::kE; ++e) t.o[i][e] = t.o[i][e] * f + other[2 * R + (i * Tl::kE + e) * 64 + lane] * g;
+        for (int e = 0; e < 4; ++e) t.o[i][e] = t.o[i][e] * f + x[e] * g;
+      }
+    }
   }
   write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * kRows + wq * R + lane % R, lane / R, t.m, t.l, t.o);
 }
@@ -1096,7 +1094,7 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
       kb = kb1;
     }
     if (watch) {
-      careful_piece<T, D, F::kRows, WQ, 1>(kernel_args(), head, index, lds);
+      careful_piece<T, D, F::kRows, F::kKeys, WQ>(kernel_args(), head, index, lds);
       return;
     }
   }
@@ -1105,43 +1103,57 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
   write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * F::kRows + wave * 32 + n, half, m, l, o);
 }
 
-// The pieces of a split tile: o = sum 2^(m_i - m) O_i / sum 2^(m_i - m) l_i
+// The pieces of a split tile: o = sum 2^(m_i - m) O_i / sum 2^(m_i - m) l_i.  A wave has a row, lane i the weight of
+// piece i (of 64 at a time).
+constexpr int kJoinRows = 16;                    // of a block
 template <typename T, int D, int ROWS>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   typedef typename T::elem elem;
-  constexpr int kLanes = D / 4;                  // of a row
+  constexpr int V = D / 64;                      // columns of a lane
+  typedef float fv __attribute__((ext_vector_type(V)));
+  typedef elem ev __attribute__((ext_vector_type(V)));
   int head, index;
   block_of(a, head, index);
-  const int heads = a.c.n_kv_heads;
+  const int heads = a.c.n_kv_heads, lane = threadIdx.x % 64;
   const int4 t = a.meta[index];                  // request, first row, rows, pieces
   if (t.w < 2) return;
-  const int c = threadIdx.x % kLanes * 4, n = int(a.io.n_tokens), G = a.group.d;
+  const int c = lane * V, n = int(a.io.n_tokens), G = a.group.d;
   int tok0 = a.io.cu_seqlens[t.x];
   tok0 = tok0 < 0 ? 0 : tok0 > n ? n : tok0;
-  const int r1 = int(blockIdx.y) * 32 + 32 < t.z ? blockIdx.y * 32 + 32 : t.z;
-  for (int r = blockIdx.y * 32 + threadIdx.x / kLanes; r < r1; r += 256 / kLanes) {
+  const int end = int(blockIdx.y + 1) * kJoinRows < t.z ? (blockIdx.y + 1) * kJoinRows : t.z;
+  for (int r = blockIdx.y * kJoinRows + threadIdx.x / 64; r < end; r += 4) {
     const auto slot = [&](int i) { return (int64_t(index + i) * heads + head) * ROWS + r; };
-    float m = -__builtin_inff(), l = 0;
-    for (int i = 0; i < t.w; ++i) m = fmaxf(m, a.ml[slot(i) * 2]);
-    const float base = m > -__builtin_inff() ? m : 0.0f;
-    float4 o = make_float4(0, 0, 0, 0);
-    for (int i = 0; i < t.w; ++i) {
-      const float f = __builtin_amdgcn_exp2f(a.ml[slot(i) * 2] - base);
-      const float4 x = *reinterpret_cast<const float4*>(a.part + slot(i) * D + c);
-      l += f * a.ml[slot(i) * 2 + 1];
-      o.x = fmaf(f, x.x, o.x);
-      o.y = fmaf(f, x.y, o.y);
-      o.z = fmaf(f, x.z, o.z);
-      o.w = fmaf(f, x.w, o.w);
+    const auto stats = [&](int i) { return *reinterpret_cast<const float2*>(a.ml + slot(i) * 2); };   // m, l
+    float2 own = lane < t.w ? stats(lane) : make_float2(-__builtin_inff(), 0.0f);
+    float m = own.x;
+    for (int i = 64 + lane; i < t.w; i += 64) m = fmaxf(m, stats(i).x);
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) m = fmaxf(m, __shfl_xor(m, s));
+    const float base = base_of(m);
+    float l = 0;
+    fv o = 0;
+    for (int i0 = 0; i0 < t.w; i0 += 64) {
+      if (i0 > 0) own = i0 + lane < t.w ? stats(i0 + lane) : make_float2(-__builtin_inff(), 0.0f);
+      const float f = __builtin_amdgcn_exp2f(own.x - base);
+      l += f * own.y;
+      const int some = t.w - i0 < 64 ? t.w - i0 : 64;
+#pragma unroll 4
+      for (int i = 0; i < some; ++i) {
+        const fv x = *reinterpret_cast<const fv*>(a.part + slot(i0 + i) * D + c);
+        o += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i)) * x;
+      }
     }
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) l += __shfl_xor(l, s);
     const int tok = int(a.group.of(t.y + r)), qh = head * G + t.y + r - tok * G;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    typedef elem e4 __attribute__((ext_vector_type(4)));
-    const e4 x = {elem(o.x * inv), elem(o.y * inv), elem(o.z * inv), elem(o.w * inv)};
     const int64_t at = int64_t(tok0) + tok;
+    ev x;
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] = elem(o[e] * inv);
     if (c < a.c.head_dim)
-      *reinterpret_cast<e4*>(static_cast<elem*>(a.io.o) + at * a.io.o_tok + qh * a.io.o_head + c) = x;
-    if (a.io.lse && c == 0) a.io.lse[at * a.io.lse_tok + qh * a.io.lse_head] = m * 0.69314718056f + logf(l);
+      *reinterpret_cast<ev*>(static_cast<elem*>(a.io.o) + at * a.io.o_tok + qh * a.io.o_head + c) = x;
+    if (a.io.lse && lane == 0) a.io.lse[at * a.io.lse_tok + qh * a.io.lse_head] = m * 0.69314718056f + logf(l);
   }
 }
 
@@ -1167,11 +1179,11 @@ constexpr int wide_blocks(int D) { return 4 * wide_simd(D) / wide_wq(D); }
 
 int dim_of(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
-constexpr int least_steps(int form) { return form == kWide ? 4 : 2; }
+constexpr int least_steps(int form) { return form == kWide ? 4 : 1; }
 
-// Pieces of few rows: three for each place that a block has
+// Pieces of few rows that a call aims at: two for each place that a block has
 int few_target(int form, int D, int n_kv_heads) {
-  const int x = 3 * kUnits * few_simd(form, D) / n_kv_heads;
+  const int x = 2 * kUnits * few_simd(form, D) / n_kv_heads;
   return x < 1 ? 1 : x;
 }
 
@@ -1181,7 +1193,7 @@ void shape_of(Launch& x, int D) {
     x.keys = wide_keys(D);
   } else {
     x.rows = 16 << x.form;
-    x.keys = x.form == 2 ? 64 : 128;
+    x.keys = 128 >> x.form;
   }
 }
 
@@ -1228,9 +1240,9 @@ void launch_form(AttnArgs a, const Launch& x, hipStream_t st) {
     const uint32_t g = uint32_t(blocks - a.block0 < kMost ? blocks - a.block0 : kMost);
     const bool one = a.page.d % (512 / D) == 0;   // the rows of a wave's load are of one page
     if constexpr (FORM < kWide) {
-      constexpr int R = FORM == 0 ? 16 : 32, WQ = FORM == 2 ? 2 : 1;
-      if (one) attn_few_kernel<T, D, R, WQ, few_simd(FORM, D), true><<<g, 256, 0, st>>>(a);
-      else attn_few_kernel<T, D, R, WQ, few_simd(FORM, D), false><<<g, 256, 0, st>>>(a);
+      constexpr int WQ = 1 << FORM;
+      if (one) attn_few_kernel<T, D, WQ, few_simd(FORM, D), true><<<g, 256, 0, st>>>(a);
+      else attn_few_kernel<T, D, WQ, few_simd(FORM, D), false><<<g, 256, 0, st>>>(a);
     } else if (one)
       attn_wide_kernel<T, D, wide_wq(D), wide_simd(D), true><<<g, 64 * wide_wq(D), 0, st>>>(a);
     else attn_wide_kernel<T, D, wide_wq(D), wide_simd(D), false><<<g, 64 * wide_wq(D), 0, st>>>(a);
@@ -1238,7 +1250,7 @@ void launch_form(AttnArgs a, const Launch& x, hipStream_t st) {
   constexpr int kRows = FORM == kWide ? 32 * wide_wq(D) : 16 << FORM;
   a.block0 = 0;
   if (x.split)                                    // few pieces
-    attn_join_kernel<T, D, kRows><<<dim3(uint32_t(blocks), (kRows + 31) / 32), 256, 0, st>>>(a);
+    attn_join_kernel<T, D, kRows><<<dim3(uint32_t(blocks), (kRows + kJoinRows - 1) / kJoinRows), 256, 0, st>>>(a);
 }
 
 template <typename T, int D>
