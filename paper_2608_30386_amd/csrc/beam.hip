@@ -13,7 +13,6 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
-#include <type_traits>
 
 #include "cache_common.h"
 #include "launch_common.h"
@@ -55,28 +54,34 @@ __device__ inline float unordered(uint32_t k) {
 __device__ inline uint64_t key_of(float x, uint32_t token) { return (uint64_t(ordered(x)) << 32) | (0xFFFFFFFFu - token); }
 __device__ inline uint32_t token_of(uint64_t key) { return 0xFFFFFFFFu - uint32_t(key); }
 
-// The largest number that at least n of the wave's keys reach (0 if fewer than n are not 0), bit by bit from the
-// first in which the keys differ; of different keys just n reach it.
-template <typename U>
-__device__ inline U reached_by(U key, int n) {
+// The largest number that at least n of the wave's keys reach (0 if fewer than n are not 0), bit by bit; of
+// different keys just n reach it.
+__device__ inline uint32_t reached_by(uint32_t key, int n) {
   if (__popcll(__ballot(key != 0)) < n) return 0;
-  U all = key, any = key;
+  uint32_t all = key, any = key;
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) {
-    all &= U(__shfl_xor((std::conditional_t<sizeof(U) == 8, unsigned long long, unsigned>)all, s));
-    any |= U(__shfl_xor((std::conditional_t<sizeof(U) == 8, unsigned long long, unsigned>)any, s));
+    all &= uint32_t(__shfl_xor(int(all), s));
+    any |= uint32_t(__shfl_xor(int(any), s));
   }
-  const U differ = all ^ any;
+  const uint32_t differ = all ^ any;      // from the first bit in which they differ
   if (differ == 0) return all;
-  int bit = sizeof(U) == 8 ? 63 - __builtin_clzll(differ) : 31 - __builtin_clz(uint32_t(differ));
-  U t = bit + 1 < int(sizeof(U)) * 8 ? any >> (bit + 1) << (bit + 1) : 0;
+  int bit = 31 - __builtin_clz(differ);
+  uint32_t t = bit < 31 ? any >> (bit + 1) << (bit + 1) : 0;
   for (; bit >= 0; --bit) {
-    const U x = t | (U(1) << bit);
+    const uint32_t x = t | (1u << bit);
     const int c = __popcll(__ballot(key >= x));
     if (c >= n) t = x;
     if (c == n) break;
   }
   return t;
+}
+__device__ inline uint64_t reached_by(uint64_t key, int n) {
+  const uint32_t hi = uint32_t(key >> 32), t = reached_by(hi, n);
+  if (t == 0) return 0;
+  const int above = __popcll(__ballot(hi > t));           // the lower half decides between those that are equal
+  const uint32_t lo = reached_by(hi == t ? uint32_t(key) : 0u, n - above);
+  return (uint64_t(t) << 32) | (__popcll(__ballot(hi >= t)) == n ? 0u : lo);
 }
 
 // e^x for x <= 0 in 64 bits, to 2^-36: 2^n e^r with r at most ln 2 / 2, the exponential's series to r^9 / 9!
@@ -97,13 +102,13 @@ __device__ inline double exp64(double x) {
   return __builtin_amdgcn_ldexp(p, n > -2000.0 ? int(n) : -2000);
 }
 
-// A list of c different keys cut to its n largest, of which there are more: the n-th largest bit by bit, the block
-// counting.  For rows with many equal logits, or with the large ones in a few lanes.
-constexpr int kRanked = 512;
-__device__ inline int narrow_list(uint64_t* list, int c, int n, int* count) {
-  uint64_t mine[kTile / kThreads], t = 0;
-#pragma unroll
-  for (int i = 0; i < kTile / kThreads; ++i) mine[i] = int(i * kThreads + threadIdx.x) < c ? list[i * kThreads + threadIdx.x] : 0;
+constexpr int kRanked = 512;             // keys that are ranked at most
+
+// The block's n-th largest key, bit by bit, the block counting: for tiles with many equal logits, or with the large
+// ones in a few lanes.  keys: of this thread, all different.
+template <int N>
+__device__ inline uint64_t block_reached_by(const uint64_t (&keys)[N], int n, int* count) {
+  uint64_t t = 0;
   for (int bit = 63; bit >= 0; --bit) {
     const uint64_t x = t | (uint64_t(1) << bit);
     __syncthreads();
@@ -111,26 +116,20 @@ __device__ inline int narrow_list(uint64_t* list, int c, int n, int* count) {
     __syncthreads();
     int some = 0;
 #pragma unroll
-    for (int i = 0; i < kTile / kThreads; ++i) some += __popcll(__ballot(mine[i] >= x));
+    for (int i = 0; i < N; ++i) some += __popcll(__ballot(keys[i] >= x));
     if (threadIdx.x % 64 == 0 && some) atomicAdd(count, some);
     __syncthreads();
-    if (*count >= n) t = x;
-    if (*count == n) break;
+    const int c = *count;
+    if (c >= n) t = x;
+    if (c == n) break;
   }
-  __syncthreads();
-  if (threadIdx.x == 0) *count = 0;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kTile / kThreads; ++i)
-    if (mine[i] >= t) list[atomicAdd(count, 1)] = mine[i];
-  __syncthreads();
-  return *count;
+  return t;
 }
 
 // A tile of a row: its largest logit, the sum of exponentials against it, its n_out best keys.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void beam_scan_kernel(BeamArgs a) {
-  __shared__ uint64_t list[kTile];
+  __shared__ uint64_t list[kRanked];
   __shared__ uint32_t limit[kThreads / 64];
   __shared__ float top[kThreads / 64];
   __shared__ double part[kThreads / 64];
@@ -154,7 +153,7 @@ __global__ __launch_bounds__(kThreads) void beam_scan_kernel(BeamArgs a) {
     m = fmaxf(m, x[i]);
   }
   // n_out lanes of a wave have a logit at or above its floor, so the block has n_out at or above each
-  const uint32_t t = reached_by<uint32_t>(m > -inf ? ordered(m) : 0, a.n_out);
+  const uint32_t t = reached_by(m > -inf ? ordered(m) : 0u, a.n_out);
   float wm = m;
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) wm = fmaxf(wm, __shfl_xor(wm, s));
@@ -171,7 +170,10 @@ __global__ __launch_bounds__(kThreads) void beam_scan_kernel(BeamArgs a) {
   if (ordered(m) >= low) {
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-      if (ordered(x[i]) >= low) list[atomicAdd(&count, 1)] = key_of(x[i], base + i % 8 + i / 8 * (kTile / 2));
+      if (ordered(x[i]) >= low) {
+        const int at = atomicAdd(&count, 1);
+        if (at < kRanked) list[at] = key_of(x[i], base + i % 8 + i / 8 * (kTile / 2));
+      }
   }
   double sum = bad ? __longlong_as_double(0x7FF8000000000000) : 0.0;
 #pragma unroll
@@ -190,10 +192,24 @@ __global__ __launch_bounds__(kThreads) void beam_scan_kernel(BeamArgs a) {
   }
   int c = count;
   uint64_t* out = a.keys + at * a.n_out;
-  if (c > kRanked) c = narrow_list(list, c, a.n_out, &count);
+  if (c > kRanked) {                       // more than fit: the n_out best alone
+    uint64_t keys[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) keys[i] = x[i] > -inf ? key_of(x[i], base + i % 8 + i / 8 * (kTile / 2)) : 0;
+    const uint64_t last = block_reached_by(keys, a.n_out, &count);
+    __syncthreads();
+    if (tid == 0) count = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (keys[i] >= last) list[atomicAdd(&count, 1)] = keys[i];
+    __syncthreads();
+    c = count;
+  }
   for (int i = tid; i < c; i += kThreads) {
     const uint64_t key = list[i];
     int rank = 0;
+#pragma unroll 8
     for (int j = 0; j < c; ++j) rank += list[j] > key;
     if (rank < a.n_out) out[rank] = key;
   }
@@ -209,7 +225,7 @@ __device__ inline double unordered64(uint64_t k) {
 }
 
 __global__ __launch_bounds__(kPickWaves * 64) void beam_pick_kernel(BeamArgs a) {
-  __shared__ uint64_t list[kPickWaves][64 * kPickKeys];
+  __shared__ uint64_t list[kPickWaves][64 * kPickKeys], top[kPickWaves][64];
   __shared__ uint64_t score[kMaxBeams * kMaxOut], logit[kMaxBeams * kMaxOut];   // of each beam's best
   const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, n = a.n_out;
   const int r = blockIdx.x;
@@ -243,7 +259,7 @@ __global__ __launch_bounds__(kPickWaves * 64) void beam_pick_kernel(BeamArgs a) 
         k[i] = j < total ? keys[j] : 0;
         best = k[i] > best ? k[i] : best;
       }
-      uint64_t t = reached_by<uint64_t>(best, n);
+      uint64_t t = reached_by(best, n);
       if (t == 0) t = 1;
       int c = 0;
 #pragma unroll
@@ -252,27 +268,16 @@ __global__ __launch_bounds__(kPickWaves * 64) void beam_pick_kernel(BeamArgs a) 
         if (k[i] >= t) mine[c + __popcll(in & ((uint64_t(1) << lane) - 1))] = k[i];
         c += __popcll(in);
       }
-      // ranked: the lane of a rank gets its key
       dasc_wy::wave_lds_sync();
-      uint64_t key[kPickKeys];
-      int rank[kPickKeys];
-#pragma unroll
-      for (int i = 0; i < kPickKeys; ++i) {
-        const int j = i * 64 + lane;
-        key[i] = j < c ? mine[j] : 0;
-        rank[i] = j < c ? 0 : 64 * kPickKeys;
-      }
-      for (int j = 0; j < c; ++j) {
-        const uint64_t other = mine[j];
-#pragma unroll
-        for (int i = 0; i < kPickKeys; ++i) rank[i] += other > key[i];
+      for (int i = lane; i < c; i += 64) {          // ranked, a key a lane
+        const uint64_t key = mine[i];
+        int rank = 0;
+#pragma unroll 8
+        for (int j = 0; j < c; ++j) rank += mine[j] > key;
+        if (rank < n) top[wave][rank] = key;
       }
       dasc_wy::wave_lds_sync();
-#pragma unroll
-      for (int i = 0; i < kPickKeys; ++i)
-        if (rank[i] < n) mine[rank[i]] = key[i];
-      dasc_wy::wave_lds_sync();
-      carried = lane < n && lane < c ? mine[lane] : 0;
+      carried = lane < n && lane < c ? top[wave][lane] : 0;
     }
     const bool live = start > -__builtin_inf() && start < __builtin_inf() && lse == lse;
     if (lane < n) {
@@ -293,6 +298,7 @@ __global__ __launch_bounds__(kPickWaves * 64) void beam_pick_kernel(BeamArgs a) 
     if (s == 0) continue;
     const int b = i / n;
     int rank = 0;
+#pragma unroll 8
     for (int j = 0; j < total; ++j) {
       const uint64_t o = score[j];
       if (o > s || (o == s && j < i)) ++rank;   // a beam's list is in order of logit and token
