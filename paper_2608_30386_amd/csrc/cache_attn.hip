@@ -14,8 +14,9 @@
 // lengths are.  Pieces of a split tile leave (m, l, O) in the workspace, and a second kernel joins them.
 //
 // What is not seen must not reach a result: its weight is 0, but 0 times an infinity or NaN is NaN.  Positions
-// beyond a request or of no page are put into LDS as zeros; where a tile's mask cuts through its positions
-// and a value in it is not finite, the products are made one by one (careful()).
+// beyond a request or of no page are put into LDS as zeros.  A block that finds a value that is not finite where some
+// of its rows see the position and some do not starts again, a token at a time, with what that one does not
+// see as zeros: right, but slow.
 
 #include <hip/hip_runtime.h>
 
@@ -240,7 +241,7 @@ struct Form {
 constexpr int wide_wq(int D) { return D == 256 ? DASC_WQ256 : D == 128 ? DASC_WQ128 : DASC_WQ64; }
 constexpr int wide_simd(int D) { return D == 256 ? DASC_SIMD256 : D == 128 ? DASC_SIMD128 : DASC_SIMD64; }
 constexpr int wide_keys(int D) { return D == 256 ? 32 : D == 128 ? DASC_KW128 : DASC_KW64; }
-constexpr int few_simd(int form, int D) { return D == 256 && form == 0 ? 1 : 2; }   // waves of a SIMD, blocks of a CU
+constexpr int few_simd(int form, int D) { return D == 256 && form < 2 ? 1 : 2; }   // waves of a SIMD, blocks of a CU
 
 // Where 16-byte chunk c of row r lies: lanes of a read that take the same chunk of many rows (keys), or a few
 // chunks of four rows (values), meet different banks
@@ -370,7 +371,16 @@ __device__ inline void hide(f32x16 (&s)[NS], int half, int key0, uint64_t have, 
 // The row's running base m of the weights 2^(s - m), sum l (of this half's keys) and output O, before scores
 // with maximum `top` (of this half's) join them.  The base follows the maximum only where that has left it by more
 // than 2^8 in some row: weights up to 2^8 lose nothing, and most steps leave O alone.
-template <typename V, int NO>
+// A wave that has a SIMD to itself has 256 accumulation registers beside its others, which products read and write
+// directly.  O stays there if it is put there wherever it was last touched by other arithmetic; else the compiler
+// moves all of it there and back in every step.
+template <bool ACC, typename V, int N>
+__device__ inline void in_acc(V (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if constexpr (ACC) asm volatile("" : "+a"(x[i]));
+}
+template <bool ACC, typename V, int NO>
 __device__ inline void rebase(float top, float scale2, float& m, float& l, V (&o)[NO]) {
   constexpr int kE = sizeof(V) / 4;
   top = fmaxf(top, __shfl_xor(top, 32)) * scale2;
@@ -384,9 +394,10 @@ __device__ inline void rebase(float top, float scale2, float& m, float& l, V (&o
     for (int i = 0; i < NO; ++i)
 #pragma unroll
       for (int e = 0; e < kE; ++e) o[i][e] *= shrink;
+    in_acc<ACC>(o);
   }
 }
-template <int NS, int NO>
+template <bool ACC, int NS, int NO>
 __device__ inline void rebase(f32x16 (&s)[NS], float scale2, float& m, float& l, f32x16 (&o)[NO]) {
   settle(s);
   float top = -__builtin_inff();
@@ -394,7 +405,7 @@ __device__ inline void rebase(f32x16 (&s)[NS], float scale2, float& m, float& l,
   for (int t = 0; t < NS; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
-  rebase(top, scale2, m, l, o);
+  rebase<ACC>(top, scale2, m, l, o);
 }
 
 // Scores to weights, eight keys of each half: rounded to the type as an operand, their sum in fp32
@@ -419,57 +430,6 @@ __device__ inline typename T::x8 value_operand(const char* lv, const Places& at,
   x.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
   x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * D));
   return x.v;
-}
-
-// O^T += V^T P^T where a value that some rows do not see is not finite.  Such values count as 0 in the product, and
-// another product counts, for each row and column, those that the row sees: infinities in ones, negative ones
-// in 128s, NaN in 16384s.  They are added after.
-template <typename T, int D, int NS>
-__device__ inline void careful(const char* lv, const Places& at, int half, int key0, uint64_t have, const Row& row,
-                               const f32x16 (&s)[NS], float scale2, float m, float& l, f32x16 (&o)[D / 32]) {
-  typedef short s16x8 __attribute__((ext_vector_type(8)));
-  typedef typename T::x8 x8;
-  const short top = short(T::kExp & 0xFFFFu);
-  x8 all[NS][2];
-#pragma unroll
-  for (int t = 0; t < NS; ++t)
-#pragma unroll
-    for (int u = 0; u < 2; ++u) all[t][u] = weights<T>(s, t, u, scale2, base_of(m), l);
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i) {
-    f32x16 odd;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) odd[e] = 0;
-#pragma unroll
-    for (int t = 0; t < NS; ++t)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        __builtin_amdgcn_sched_barrier(0);
-        const s16x8 v = __builtin_bit_cast(s16x8, value_operand<T, D>(lv, at, t * 32 + u * 16, i));
-        s16x8 fine;
-        x8 kind, seen;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int k = key_at(t, 8 * u + e, half);
-          const bool in = (have >> k & 1) && key0 + k >= row.lo && key0 + k <= row.hi, is = (v[e] & top) == top;
-          seen[e] = typename T::elem(in ? 1.0f : 0.0f);
-          fine[e] = is ? short(0) : v[e];
-          kind[e] = typename T::elem(!is ? 0.0f : v[e] == top ? 1.0f : v[e] == short(top | 0x8000) ? 128.0f : 16384.0f);
-        }
-        o[i] = T::mfma(__builtin_bit_cast(x8, fine), all[t][u], o[i]);
-        odd = T::mfma(kind, seen, odd);
-      }
-    __builtin_amdgcn_sched_barrier(0);
-    settle(o[i]);
-    settle(odd);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int n = int(odd[e]);
-      const float inf = __builtin_inff();
-      o[i][e] += ((n & 127) ? inf : 0.0f) + ((n >> 7 & 127) ? -inf : 0.0f) + (n >> 14 ? __builtin_nanf("") : 0.0f);
-    }
-  }
-  __builtin_amdgcn_sched_barrier(0);
 }
 
 // A row's result: to the workspace if its tile is split, else to the output.  g: the lane's part of the row, columns
@@ -530,66 +490,21 @@ __device__ inline Steps steps_of(const AttnArgs& a, const Piece& p) {
           last.lo, first.hi};
 }
 
-// A piece from start to end with care for values that are not finite, for the kernels below, whose loops have no
-// register to spare for it.  Waves that have no 32 rows of their own help to load.
-template <typename T, int D, int ROWS, int KEYS, int WAVES>
-__device__ __attribute__((noinline)) void careful_piece(const AttnArgs* args, int head, int index, char* lds) {
-  constexpr int KW = 32, kThreads = 64 * WAVES, kChunks = D / 8, WQ = (ROWS + 31) / 32, per = KEYS / KW;
-  typedef typename T::elem elem;
-  const AttnArgs a = *args;
-  const int tid = threadIdx.x, lane = tid % 64, n = lane % 32, half = lane / 32, wave = tid / 64 % WQ;
-  Piece p;
-  if (!locate<ROWS, KEYS>(a, index, p)) return;
-  const Steps steps = steps_of<KEYS>(a, p);
-  const Places at = places_of<D>(lane);
-  const Row row = row_of(a, p, head, wave * 32 + n);
-  typename T::x8 q[D / 16];
-  load_query<T, D>(a, p, row, half, q);
-  f32x16 o[D / 32];
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) o[i][e] = 0;
-  float m = -__builtin_inff(), l = 0;
-  const int32_t* table = a.io.block_table + int64_t(p.req) * a.io.table_req;
-  const elem* const kc = static_cast<const elem*>(a.c.k) + head * a.c.k_head;
-  const elem* const vc = static_cast<const elem*>(a.c.v) + head * a.c.v_head;
-  const auto page_of = [&](int key) {
-    if (key >= p.kv) return -1;
-    const int b = table[a.page.of(key)];
-    return b >= 0 && b < a.c.n_pages ? b : -1;
-  };
-#pragma unroll 1
-  for (int step = steps.begin * per; step < steps.end * per; ++step) {
-    const int key0 = step * KW;
-    __syncthreads();
-#pragma unroll 1
-    for (int i = tid; i < KW * kChunks; i += kThreads) {
-      const int r = i / kChunks, c = i % kChunks, key = key0 + r;
-      const int64_t b = page_of(key), off = key - int(a.page.of(key) * a.page.d);
-      u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
-      if (b >= 0 && c * 8 < a.c.head_dim) {
-        k = *reinterpret_cast<const u32x4*>(kc + b * a.c.k_page + off * a.c.k_tok + c * 8);
-        v = *reinterpret_cast<const u32x4*>(vc + b * a.c.v_page + off * a.c.v_tok + c * 8);
-      }
-      *reinterpret_cast<u32x4*>(lds + r * 2 * D + key_chunk(r, c) * 16) = k;
-      *reinterpret_cast<u32x4*>(lds + KW * 2 * D + r * 2 * D + value_chunk<D>(r, c) * 16) = v;
-    }
-    __syncthreads();
-    const uint64_t have = __ballot(lane < KW && page_of(key0 + lane) >= 0);
-    f32x16 s[1];
-    scores<T, D>(lds, at, q, s);
-    hide(s, half, key0, have, row);
-    rebase(s, a.scale2, m, l, o);
-    careful<T, D>(lds + KW * 2 * D, at, half, key0, have, row, s, a.scale2, m, l, o);
+// The positions of `step` (its first at key0, `n` of them, a bit each) that the token taken alone sees; all if none is
+struct Alone { int tok, lo, hi; };                  // tok: -1: none
+__device__ inline bool taken(const Alone& x, int key) { return x.tok < 0 || (key >= x.lo && key <= x.hi); }
+// After a pass over a tile: whether another has to follow, over the next of its tokens alone
+__device__ inline bool next_alone(const AttnArgs& a, const Piece& p, bool odd, Alone& x) {
+  if (x.tok < 0) {
+    if (!odd) return false;
+    x.tok = int(a.group.of(p.row0));
+  } else if (++x.tok > int(a.group.of(p.row0 + p.rows - 1))) {
+    return false;
   }
-  if (tid / 64 >= WQ) return;
-  settle(o);
-  l += __shfl_xor(l, 32);
-  write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * ROWS + wave * 32 + n, half, m, l, o);
-}
-__device__ inline const AttnArgs* kernel_args() {
-  return (const AttnArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  const Sight s = sight(a, p, x.tok);
+  x.lo = s.lo;
+  x.hi = s.hi;
+  return true;
 }
 
 // ---- few rows -------------------------------------------------------------------------------------
@@ -597,7 +512,7 @@ __device__ inline const AttnArgs* kernel_args() {
 // A tile of 32 keys and 16 rows, on 16 x 16 x 32 products: lane (g, n) = (lane / 16, lane % 16) has keys
 // 4 g + {0..3} of each 16 of row n, so both tiles of S^T again form the operand P^T, keys 4 g + {0..3} and
 // 16 + 4 g + {0..3} of a product.
-template <typename T, int D>
+template <typename T, int D, bool ACC>
 struct Tile {
   static constexpr int kO = D / 16, kQ = D / 32;
   typedef typename T::x8 x8;
@@ -630,6 +545,7 @@ struct Tile {
     for (int i = 0; i < kO; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[i][e] = 0;
+    in_acc<ACC>(o);
   }
   __device__ x8 key_operand(const char* lk, int j) const {      // of product j: keys 16 (j / kQ) .., channels j % kQ
     const int t = j / kQ, i = j % kQ;
@@ -675,7 +591,7 @@ struct Tile {
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) top = fmaxf(top, s[t][e]);
-    rebase(fmaxf(top, __shfl_xor(top, 16)), scale2, m, l, o);
+    rebase<ACC>(fmaxf(top, __shfl_xor(top, 16)), scale2, m, l, o);
     const float base = base_of(m);
     x8 v[kAhead], w;
 #pragma unroll
@@ -726,6 +642,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD)
   const int32_t* table = a.io.block_table + int64_t(p.req) * a.io.table_req;
   const elem* const kc = static_cast<const elem*>(a.c.k) + head * a.c.k_head;
   const elem* const vc = static_cast<const elem*>(a.c.v) + head * a.c.v_head;
+  Alone alone = {-1, 0, 0};
   // Lane r (and r + 32) knows where row r of its group's keys lies; see the kernel for many rows
   int entry, inside;
   const auto ask = [&](int step) {
@@ -736,7 +653,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD)
     inside = key - at * int(a.page.d);
   };
   const auto there = [&](int step) {
-    return __ballot(lane < 32 && step < steps.end && step * kKeys + wk * 32 + lane < p.kv && entry >= 0 && entry < a.c.n_pages);
+    const int key = step * kKeys + wk * 32 + lane;
+    return __ballot(lane < 32 && step < steps.end && key < p.kv && entry >= 0 && entry < a.c.n_pages && taken(alone, key));
   };
   const auto rows_at = [&](uint32_t page_stride, uint32_t tok_stride) {
     const uint32_t b = entry >= 0 && entry < a.c.n_pages ? entry : 0;
@@ -781,9 +699,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD)
     for (int i = 0; i < kLoads; ++i)
       *reinterpret_cast<u32x4*>(to + place[i % kPlaces] + i / kPlaces * kPlaces * kWaveRows * kRowBytes) = x[i];
   };
-  const auto watch = [&](int step, const u32x4 (&x)[kLoads]) {   // what careful_piece() is for
+  const auto watch = [&](int step, const u32x4 (&x)[kLoads]) {
     const int key0 = step * kKeys + wk * 32;
-    if (key0 >= steps.all_lo && key0 + 31 <= steps.all_hi) return;
+    if (alone.tok >= 0 || (key0 >= steps.all_lo && key0 + 31 <= steps.all_hi)) return;
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) odd |= odd_value<T>(x[i]);
@@ -797,8 +715,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD)
     load(vc, alike ? k_rows : rows_at(a.v_page, a.v_tok), v_lane, vr);
   };
 
-  Tile<T, D> t;
+  Tile<T, D, SIMD == 1> t;
   const bool busy = steps.begin < steps.end;
+  do {
   uint64_t have = 0;
   if (busy) {
     ask(steps.begin);
@@ -839,10 +758,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD)
 
   // waves that share rows meet in LDS
   __syncthreads();
-  if (odd_flag) {
-    careful_piece<T, D, kRows, kKeys, 4>(kernel_args(), head, index, lds);
-    return;
-  }
+  const bool odd = odd_flag;
   if constexpr (WK > 1) {
     const auto part = [&](int w) { return reinterpret_cast<float*>(lds) + ((w - 1) * WQ + wq) * R * (D + 2); };
     if (wk > 0) {
@@ -855,24 +771,29 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD)
       for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(mine + 2 * R + (i * 64 + lane) * 4) = t.o[i];
     }
     __syncthreads();
-    if (wk > 0) return;
+    if (wk == 0) {
 #pragma unroll 1
-    for (int w = 1; w < WK; ++w) {
-      const float* const other = part(w);
-      const float om = other[lane % R * 2], ol = other[lane % R * 2 + 1];
-      const float both = fmaxf(t.m, om), base = base_of(both);
-      const float f = __builtin_amdgcn_exp2f(t.m - base), g = __builtin_amdgcn_exp2f(om - base);
-      t.m = both;
-      t.l = t.l * f + ol * g;
+      for (int w = 1; w < WK; ++w) {
+        const float* const other = part(w);
+        const float om = other[lane % R * 2], ol = other[lane % R * 2 + 1];
+        const float both = fmaxf(t.m, om), base = base_of(both);
+        const float f = __builtin_amdgcn_exp2f(t.m - base), g = __builtin_amdgcn_exp2f(om - base);
+        t.m = both;
+        t.l = t.l * f + ol * g;
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(other + 2 * R + (i * 64 + lane) * 4);
+        for (int i = 0; i < D / 16; ++i) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(other + 2 * R + (i * 64 + lane) * 4);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) t.o[i][e] = t.o[i][e] * f + x[e] * g;
+          for (int e = 0; e < 4; ++e) t.o[i][e] = t.o[i][e] * f + x[e] * g;
+        }
       }
     }
   }
-  write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * kRows + wq * R + lane % R, lane / R, t.m, t.l, t.o);
+  if (wk == 0 && (alone.tok < 0 ? !odd : row.tok == alone.tok))
+    write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * kRows + wq * R + lane % R, lane / R, t.m, t.l, t.o);
+  if (!next_alone(a, p, odd, alone)) return;
+  __syncthreads();                                 // LDS is free again
+  } while (true);
 }
 
 // ---- many rows --------------------------------------------------------------------------------------
@@ -932,7 +853,7 @@ __device__ inline void advance(const char* lk, const char* lv, const Places& at,
     }
     hold();
   }
-  rebase(top, scale2, m, l, o);
+  rebase<D == 256>(top, scale2, m, l, o);
   s[0] = next[0];
 }
 
@@ -960,16 +881,11 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
   const int w0 = wave * 32, r0 = w0 < p.rows ? w0 : p.rows - 1, r1 = w0 + 31 < p.rows ? w0 + 31 : p.rows - 1;
   const int first = sight(a, p, int(a.group.of(p.row0 + r0))).lo / F::kKeys;
   const int end_hi = sight(a, p, int(a.group.of(p.row0 + r1))).hi, last = end_hi < 0 ? -1 : end_hi / F::kKeys;
-  typename T::x8 q[D / 16];
-  load_query<T, D>(a, p, row, half, q);
-  f32x16 o[D / 32], s[1];
-  float m = -__builtin_inff(), l = 0;
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) o[i][e] = 0;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) s[0][e] = -__builtin_inff();
+  Alone alone = {-1, 0, 0};
+  // A pass over the tile, of all its rows or for the token that is taken alone; whether a value was met that calls
+  // for the latter.  (Two copies, so that the first has no register to spare for the others' loop.)
+  const auto pass = [&](auto single) -> bool {
+  constexpr bool kAlone = decltype(single)::value;
   const int d = a.c.head_dim;
 
   const int32_t* table = a.io.block_table + int64_t(p.req) * a.io.table_req;
@@ -986,7 +902,8 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
     inside = key - at * int(a.page.d);
   };
   const auto there = [&](int step) {               // the positions of the step that have a page
-    return __ballot(lane < KW && step < steps.end && step * F::kKeys + lane < p.kv && entry >= 0 && entry < a.c.n_pages);
+    const int key = step * F::kKeys + lane;
+    return __ballot(lane < KW && step < steps.end && key < p.kv && entry >= 0 && entry < a.c.n_pages && (!kAlone || taken(alone, key)));
   };
   const auto rows_at = [&](uint32_t page_stride, uint32_t tok_stride) {
     const uint32_t b = entry >= 0 && entry < a.c.n_pages ? entry : 0;
@@ -1026,7 +943,8 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
   // Whether the values of a step have to be watched: some row of the block does not see some of its positions, and
   // a value is not finite.  The block meets.
   const auto meet = [&](int step, const u32x4 (&x)[F::kLoads]) {
-    if (step >= steps.end || (step * F::kKeys >= steps.all_lo && step * F::kKeys + F::kKeys - 1 <= steps.all_hi)) {
+    if (kAlone || step >= steps.end ||
+        (step * F::kKeys >= steps.all_lo && step * F::kKeys + F::kKeys - 1 <= steps.all_hi)) {
       __syncthreads();
       return false;
     }
@@ -1036,6 +954,18 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
     return __syncthreads_or(odd) != 0;
   };
 
+  typename T::x8 q[D / 16];
+  load_query<T, D>(a, p, row, half, q);
+  f32x16 o[D / 32], s[1];
+  float m = -__builtin_inff(), l = 0;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[i][e] = 0;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) s[0][e] = -__builtin_inff();
+  in_acc<D == 256>(o);
+  bool watch = false;
   if (steps.begin < steps.end) {
     u32x4 kr[F::kLoads], vr[F::kLoads];
     const bool alike = a.k_page == a.v_page && a.k_tok == a.v_tok;
@@ -1059,11 +989,11 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
     load(kc, k_rows, k_lane, kr);
     v_rows = v_next;
     store(lds + F::kKv + k_place, have1, kr);
-    bool watch = meet(steps.begin, vr);
+    watch = meet(steps.begin, vr);
     if (!watch) {
       scores<T, D>(lds, at, q, s);
       hide(s, half, steps.begin * F::kKeys, have & 0xFFFFFFFFu, row);
-      rebase(s, a.scale2, m, l, o);
+      rebase<D == 256>(s, a.scale2, m, l, o);
     }
     const auto mask_of = [&](int step, uint64_t all, int t) {
       return [&, step, all, t](f32x16 (&x)[1]) {
@@ -1093,14 +1023,20 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
       have1 = have2;
       kb = kb1;
     }
-    if (watch) {
-      careful_piece<T, D, F::kRows, F::kKeys, WQ>(kernel_args(), head, index, lds);
-      return;
-    }
   }
   settle(o);
   l += __shfl_xor(l, 32);
-  write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * F::kRows + wave * 32 + n, half, m, l, o);
+  if (kAlone ? row.tok == alone.tok : !watch)
+    write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * F::kRows + wave * 32 + n, half, m, l, o);
+  return watch;
+  };
+  const bool odd = pass(std::false_type{});
+  if (!odd) return;
+#pragma unroll 1
+  while (next_alone(a, p, odd, alone)) {
+    __syncthreads();                               // LDS is free again
+    (void)pass(std::true_type{});
+  }
 }
 
 // The pieces of a split tile: o = sum 2^(m_i - m) O_i / sum 2^(m_i - m) l_i.  A wave has a row, lane i the weight of
@@ -1137,11 +1073,17 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
       const float f = __builtin_amdgcn_exp2f(own.x - base);
       l += f * own.y;
       const int some = t.w - i0 < 64 ? t.w - i0 : 64;
-#pragma unroll 4
-      for (int i = 0; i < some; ++i) {
-        const fv x = *reinterpret_cast<const fv*>(a.part + slot(i0 + i) * D + c);
-        o += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i)) * x;
+      const auto piece = [&](int i) { return *reinterpret_cast<const fv*>(a.part + slot(i0 + i) * D + c); };
+      const auto weight = [&](int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i)); };
+      int i = 0;
+      for (; i + 4 <= some; i += 4) {
+        const fv x0 = piece(i), x1 = piece(i + 1), x2 = piece(i + 2), x3 = piece(i + 3);
+        o += weight(i) * x0;
+        o += weight(i + 1) * x1;
+        o += weight(i + 2) * x2;
+        o += weight(i + 3) * x3;
       }
+      for (; i < some; ++i) o += weight(i) * piece(i);
     }
 #pragma unroll
     for (int s = 1; s < 64; s *= 2) l += __shfl_xor(l, s);
