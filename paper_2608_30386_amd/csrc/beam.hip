@@ -39,7 +39,7 @@ struct BeamArgs {
   double* sums;          // [rows, tiles]: of e^(x - max), NaN if the tile holds NaN or +inf
   float* tops;           // [rows, tiles]: max
   uint64_t* keys;        // [rows, tiles, n_out], descending, 0: none
-  int64_t row0;
+  int64_t row0;          // first row (scan), or request (pick), of a launch
   int32_t n_req, beams, vocab, n_out, tiles;
 };
 
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(kPickWaves * 64) void beam_pick_kernel(BeamArgs a) 
   __shared__ uint64_t list[kPickWaves][64 * kPickKeys], top[kPickWaves][64];
   __shared__ uint64_t score[kMaxBeams * kMaxOut], logit[kMaxBeams * kMaxOut];   // of each beam's best
   const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, n = a.n_out;
-  const int r = blockIdx.x;
+  const int r = int(a.row0) + blockIdx.x;                  // the request
   for (int b = wave; b < a.beams; b += kPickWaves) {
     const int64_t row = int64_t(r) * a.beams + b;
     // the row's log-sum
@@ -445,7 +445,9 @@ extern "C" int dasc_beam_select(int32_t n_req, int32_t beams, int64_t vocab, int
     case DASC_DTYPE_F16: launch_scan<f16_t>(a, st); break;
     default: launch_scan<float>(a, st); break;
   }
-  beam_pick_kernel<<<n_req, kPickWaves * 64, 0, st>>>(a);
+  constexpr int kReqPerLaunch = 1 << 20;   // a grid counts threads in 32 bits
+  for (a.row0 = 0; a.row0 < n_req; a.row0 += kReqPerLaunch)
+    beam_pick_kernel<<<n_req - a.row0 < kReqPerLaunch ? uint32_t(n_req - a.row0) : kReqPerLaunch, kPickWaves * 64, 0, st>>>(a);
   return launch_status();
 }
 

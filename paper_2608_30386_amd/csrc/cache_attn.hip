@@ -1254,7 +1254,7 @@ extern "C" int dasc_cache_attn_workspace_bytes(int32_t n_req, int64_t n_tokens, 
     const int64_t tiles = n_tokens * group / x.rows + n_req, target = few_target(form, int(D), n_kv_heads);
     const int64_t most = form == kWide ? 2 * (2 * kUnits * wide_blocks(int(D)) / n_kv_heads + 2) : 2 * target;
     const int64_t pieces = (tiles < most ? tiles : most) * (form == kWide ? kMostPieces + 1 : 1) +
-                           (form == kWide ? kMostPieces : target);
+                           (form == kWide ? 2 * kMostPieces : target);
     const int64_t need = pieces * 16 + pieces * n_kv_heads * x.rows * (D + 2) * 4;
     if (max_kv > least_steps(form) * x.keys && size_t(need) > *bytes) *bytes = size_t(need);
   }
