@@ -29,17 +29,6 @@
 #include "output_rows.h"
 #include "wy_ops.h"
 
-#ifndef DASC_WQ256
-#define DASC_SIMD256 1
-#define DASC_WQ256 4
-#define DASC_SIMD128 2
-#define DASC_WQ128 8
-#define DASC_SIMD64 2
-#define DASC_WQ64 4
-#define DASC_KW128 64
-#define DASC_KW64 64
-#endif
-
 namespace dasc {
 namespace {
 
@@ -238,9 +227,9 @@ struct Form {
 };
 
 // Tiles of many rows: waves of 32 rows each, waves of a SIMD, keys of a step
-constexpr int wide_wq(int D) { return D == 256 ? DASC_WQ256 : D == 128 ? DASC_WQ128 : DASC_WQ64; }
-constexpr int wide_simd(int D) { return D == 256 ? DASC_SIMD256 : D == 128 ? DASC_SIMD128 : DASC_SIMD64; }
-constexpr int wide_keys(int D) { return D == 256 ? 32 : D == 128 ? DASC_KW128 : DASC_KW64; }
+constexpr int wide_wq(int D) { return D == 128 ? 8 : 4; }
+constexpr int wide_simd(int D) { return D == 256 ? 1 : 2; }
+constexpr int wide_keys(int D) { return D == 256 ? 32 : 64; }
 constexpr int few_simd(int form, int D) { return D == 256 && form < 2 ? 1 : 2; }   // waves of a SIMD, blocks of a CU
 
 // Where 16-byte chunk c of row r lies: lanes of a read that take the same chunk of many rows (keys), or a few
@@ -718,81 +707,81 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD)
   Tile<T, D, SIMD == 1> t;
   const bool busy = steps.begin < steps.end;
   do {
-  uint64_t have = 0;
-  if (busy) {
-    ask(steps.begin);
-    have = there(steps.begin);
-    load_both();
-    ask(steps.begin + 1);
-  }
-  t.start(a, p, row, lane);
-  if (busy) {
-    store(lk, k_place, have, kr);
-    store(lv, v_place, have, vr);
-    watch(steps.begin, vr);
-    // (else the first product of every step would wait for the queries' loads, and so for all that came after)
+    uint64_t have = 0;
+    if (busy) {
+      ask(steps.begin);
+      have = there(steps.begin);
+      load_both();
+      ask(steps.begin + 1);
+    }
+    t.start(a, p, row, lane);
+    if (busy) {
+      store(lk, k_place, have, kr);
+      store(lv, v_place, have, vr);
+      watch(steps.begin, vr);
+      // (else the first product of every step would wait for the queries' loads, and so for all that came after)
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-      u32x4 x = __builtin_bit_cast(u32x4, t.q[i]);
-      asm volatile("" : "+v"(x));
-      t.q[i] = __builtin_bit_cast(typename T::x8, x);
-    }
-    for (int step = steps.begin; step < steps.end; ++step) {
-      const uint64_t next = there(step + 1);
-      if (step + 1 < steps.end) load_both();
-      ask(step + 2);
-      if constexpr (WQ > 1) __syncthreads();
-      t.step(lk, lv, lane, step * kKeys + wk * 32, have, row, a.scale2);
-      if constexpr (WQ > 1) __syncthreads();
-      if (step + 1 < steps.end) {
-        store(lk, k_place, next, kr);
-        store(lv, v_place, next, vr);
-        watch(step + 1, vr);
+      for (int i = 0; i < D / 32; ++i) {
+        u32x4 x = __builtin_bit_cast(u32x4, t.q[i]);
+        asm volatile("" : "+v"(x));
+        t.q[i] = __builtin_bit_cast(typename T::x8, x);
       }
-      have = next;
+      for (int step = steps.begin; step < steps.end; ++step) {
+        const uint64_t next = there(step + 1);
+        if (step + 1 < steps.end) load_both();
+        ask(step + 2);
+        if constexpr (WQ > 1) __syncthreads();
+        t.step(lk, lv, lane, step * kKeys + wk * 32, have, row, a.scale2);
+        if constexpr (WQ > 1) __syncthreads();
+        if (step + 1 < steps.end) {
+          store(lk, k_place, next, kr);
+          store(lv, v_place, next, vr);
+          watch(step + 1, vr);
+        }
+        have = next;
+      }
     }
-  }
-  settle(t.o);
-  t.l += __shfl_xor(t.l, 16);
-  t.l += __shfl_xor(t.l, 32);
+    settle(t.o);
+    t.l += __shfl_xor(t.l, 16);
+    t.l += __shfl_xor(t.l, 32);
 
-  // waves that share rows meet in LDS
-  __syncthreads();
-  const bool odd = odd_flag;
-  if constexpr (WK > 1) {
-    const auto part = [&](int w) { return reinterpret_cast<float*>(lds) + ((w - 1) * WQ + wq) * R * (D + 2); };
-    if (wk > 0) {
-      float* const mine = part(wk);
-      if (lane < R) {
-        mine[lane * 2] = t.m;
-        mine[lane * 2 + 1] = t.l;
-      }
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(mine + 2 * R + (i * 64 + lane) * 4) = t.o[i];
-    }
+    // waves that share rows meet in LDS
     __syncthreads();
-    if (wk == 0) {
+    const bool odd = odd_flag;
+    if constexpr (WK > 1) {
+      const auto part = [&](int w) { return reinterpret_cast<float*>(lds) + ((w - 1) * WQ + wq) * R * (D + 2); };
+      if (wk > 0) {
+        float* const mine = part(wk);
+        if (lane < R) {
+          mine[lane * 2] = t.m;
+          mine[lane * 2 + 1] = t.l;
+        }
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(mine + 2 * R + (i * 64 + lane) * 4) = t.o[i];
+      }
+      __syncthreads();
+      if (wk == 0) {
 #pragma unroll 1
-      for (int w = 1; w < WK; ++w) {
-        const float* const other = part(w);
-        const float om = other[lane % R * 2], ol = other[lane % R * 2 + 1];
-        const float both = fmaxf(t.m, om), base = base_of(both);
-        const float f = __builtin_amdgcn_exp2f(t.m - base), g = __builtin_amdgcn_exp2f(om - base);
-        t.m = both;
-        t.l = t.l * f + ol * g;
+        for (int w = 1; w < WK; ++w) {
+          const float* const other = part(w);
+          const float om = other[lane % R * 2], ol = other[lane % R * 2 + 1];
+          const float both = fmaxf(t.m, om), base = base_of(both);
+          const float f = __builtin_amdgcn_exp2f(t.m - base), g = __builtin_amdgcn_exp2f(om - base);
+          t.m = both;
+          t.l = t.l * f + ol * g;
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(other + 2 * R + (i * 64 + lane) * 4);
+          for (int i = 0; i < D / 16; ++i) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(other + 2 * R + (i * 64 + lane) * 4);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) t.o[i][e] = t.o[i][e] * f + x[e] * g;
+            for (int e = 0; e < 4; ++e) t.o[i][e] = t.o[i][e] * f + x[e] * g;
+          }
         }
       }
     }
-  }
-  if (wk == 0 && (alone.tok < 0 ? !odd : row.tok == alone.tok))
-    write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * kRows + wq * R + lane % R, lane / R, t.m, t.l, t.o);
-  if (!next_alone(a, p, odd, alone)) return;
-  __syncthreads();                                 // LDS is free again
+    if (wk == 0 && (alone.tok < 0 ? !odd : row.tok == alone.tok))
+      write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * kRows + wq * R + lane % R, lane / R, t.m, t.l, t.o);
+    if (!next_alone(a, p, odd, alone)) return;
+    __syncthreads();                                 // LDS is free again
   } while (true);
 }
 
@@ -885,150 +874,150 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
   // A pass over the tile, of all its rows or for the token that is taken alone; whether a value was met that calls
   // for the latter.  (Two copies, so that the first has no register to spare for the others' loop.)
   const auto pass = [&](auto single) -> bool {
-  constexpr bool kAlone = decltype(single)::value;
-  const int d = a.c.head_dim;
+    constexpr bool kAlone = decltype(single)::value;
+    const int d = a.c.head_dim;
 
-  const int32_t* table = a.io.block_table + int64_t(p.req) * a.io.table_req;
-  const elem* const kc = static_cast<const elem*>(a.c.k) + head * a.c.k_head;
-  const elem* const vc = static_cast<const elem*>(a.c.v) + head * a.c.v_head;
-  // Lane r of a wave knows where row r of a step lies.  Its entry of the table is asked for a step ahead, and looked
-  // at when it is there.  Loads have no branch: what is not there is loaded from page 0 and put into LDS as zeros.
-  int entry, inside;                               // of the step to be loaded next: the entry, the place in the page
-  const auto ask = [&](int step) {
-    int key = (step < steps.end ? step : steps.end - 1) * F::kKeys + lane % KW;
-    key = key < p.kv ? key : p.kv - 1;
-    const int at = a.page.of(key);
-    entry = table[at];
-    inside = key - at * int(a.page.d);
-  };
-  const auto there = [&](int step) {               // the positions of the step that have a page
-    const int key = step * F::kKeys + lane;
-    return __ballot(lane < KW && step < steps.end && key < p.kv && entry >= 0 && entry < a.c.n_pages && (!kAlone || taken(alone, key)));
-  };
-  const auto rows_at = [&](uint32_t page_stride, uint32_t tok_stride) {
-    const uint32_t b = entry >= 0 && entry < a.c.n_pages ? entry : 0;
-    return uint64_t(b) * page_stride + uint64_t(uint32_t(inside)) * tok_stride;
-  };
-  constexpr uint64_t kAll = KW == 64 ? ~uint64_t(0) : (uint64_t(1) << 32) - 1;
-  constexpr int kRow = F::kThreads / F::kChunks, kWaveRows = 64 / F::kChunks;   // rows of a load of the block, of a wave
-  const int chunk = tid % F::kChunks, column = chunk * 8 < d ? chunk * 8 : 0;
-  const uint32_t k_lane = 2 * ((ONE ? lane / F::kChunks : 0) * a.k_tok + column);   // bytes
-  const uint32_t v_lane = 2 * ((ONE ? lane / F::kChunks : 0) * a.v_tok + column);
-  const auto load = [&](const elem* base, uint64_t rows, uint32_t lane_off, u32x4 (&x)[F::kLoads]) {
-#pragma unroll
-    for (int i = 0; i < F::kLoads; ++i) {
-      uint64_t at;
-      if constexpr (ONE) {                         // the rows of a wave's load follow the first, in its page
-        const int r = i * kRow + wave * kWaveRows;
-        at = uint32_t(__builtin_amdgcn_readlane(int(uint32_t(rows)), r)) |
-             uint64_t(uint32_t(__builtin_amdgcn_readlane(int(uint32_t(rows >> 32)), r))) << 32;
-      } else {
-        at = __shfl((unsigned long long)rows, i * kRow + tid / F::kChunks);
-      }
-      x[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(base + at) + lane_off);
-    }
-  };
-  const int row_in = tid / F::kChunks;             // (kRow is a multiple of eight: loads swap the same chunks)
-  const int k_place = row_in * F::kRowBytes + key_chunk(row_in, chunk) * 16;
-  const int v_place = row_in * F::kRowBytes + value_chunk<D>(row_in, chunk) * 16;
-  const auto store = [&](char* to, uint64_t have, u32x4 (&x)[F::kLoads]) {
-    if (have != kAll || d < D) {
-#pragma unroll
-      for (int i = 0; i < F::kLoads; ++i)
-        if (!(have >> (i * kRow + row_in) & 1) || chunk * 8 >= d) x[i] = u32x4{0, 0, 0, 0};
-    }
-#pragma unroll
-    for (int i = 0; i < F::kLoads; ++i) *reinterpret_cast<u32x4*>(to + i * kRow * F::kRowBytes) = x[i];
-  };
-  // Whether the values of a step have to be watched: some row of the block does not see some of its positions, and
-  // a value is not finite.  The block meets.
-  const auto meet = [&](int step, const u32x4 (&x)[F::kLoads]) {
-    if (kAlone || step >= steps.end ||
-        (step * F::kKeys >= steps.all_lo && step * F::kKeys + F::kKeys - 1 <= steps.all_hi)) {
-      __syncthreads();
-      return false;
-    }
-    bool odd = false;
-#pragma unroll
-    for (int i = 0; i < F::kLoads; ++i) odd |= odd_value<T>(x[i]);
-    return __syncthreads_or(odd) != 0;
-  };
-
-  typename T::x8 q[D / 16];
-  load_query<T, D>(a, p, row, half, q);
-  f32x16 o[D / 32], s[1];
-  float m = -__builtin_inff(), l = 0;
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) o[i][e] = 0;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) s[0][e] = -__builtin_inff();
-  in_acc<D == 256>(o);
-  bool watch = false;
-  if (steps.begin < steps.end) {
-    u32x4 kr[F::kLoads], vr[F::kLoads];
-    const bool alike = a.k_page == a.v_page && a.k_tok == a.v_tok;
-    uint64_t k_rows, v_rows, v_next;               // of the keys to be loaded next, of the values, and after them
-    const auto find = [&] {
-      k_rows = rows_at(a.k_page, a.k_tok);
-      v_next = alike ? k_rows : rows_at(a.v_page, a.v_tok);
+    const int32_t* table = a.io.block_table + int64_t(p.req) * a.io.table_req;
+    const elem* const kc = static_cast<const elem*>(a.c.k) + head * a.c.k_head;
+    const elem* const vc = static_cast<const elem*>(a.c.v) + head * a.c.v_head;
+    // Lane r of a wave knows where row r of a step lies.  Its entry of the table is asked for a step ahead, and looked
+    // at when it is there.  Loads have no branch: what is not there is loaded from page 0 and put into LDS as zeros.
+    int entry, inside;                               // of the step to be loaded next: the entry, the place in the page
+    const auto ask = [&](int step) {
+      int key = (step < steps.end ? step : steps.end - 1) * F::kKeys + lane % KW;
+      key = key < p.kv ? key : p.kv - 1;
+      const int at = a.page.of(key);
+      entry = table[at];
+      inside = key - at * int(a.page.d);
     };
-    // have: of the present step; have1, have2: of the two after
-    ask(steps.begin);
-    uint64_t have = there(steps.begin), have1, have2;
-    find();
-    ask(steps.begin + 1);
-    load(kc, k_rows, k_lane, kr);
-    load(vc, v_next, v_lane, vr);
-    store(lds + k_place, have, kr);
-    store(lds_v + v_place, have, vr);
-    have1 = there(steps.begin + 1);
-    find();
-    ask(steps.begin + 2);
-    load(kc, k_rows, k_lane, kr);
-    v_rows = v_next;
-    store(lds + F::kKv + k_place, have1, kr);
-    watch = meet(steps.begin, vr);
-    if (!watch) {
-      scores<T, D>(lds, at, q, s);
-      hide(s, half, steps.begin * F::kKeys, have & 0xFFFFFFFFu, row);
-      rebase<D == 256>(s, a.scale2, m, l, o);
-    }
-    const auto mask_of = [&](int step, uint64_t all, int t) {
-      return [&, step, all, t](f32x16 (&x)[1]) {
-        hide(x, half, step * F::kKeys + t * 32, all >> (32 * t) & 0xFFFFFFFFu, row);
+    const auto there = [&](int step) {               // the positions of the step that have a page
+      const int key = step * F::kKeys + lane;
+      return __ballot(lane < KW && step < steps.end && key < p.kv && entry >= 0 && entry < a.c.n_pages && (!kAlone || taken(alone, key)));
+    };
+    const auto rows_at = [&](uint32_t page_stride, uint32_t tok_stride) {
+      const uint32_t b = entry >= 0 && entry < a.c.n_pages ? entry : 0;
+      return uint64_t(b) * page_stride + uint64_t(uint32_t(inside)) * tok_stride;
+    };
+    constexpr uint64_t kAll = KW == 64 ? ~uint64_t(0) : (uint64_t(1) << 32) - 1;
+    constexpr int kRow = F::kThreads / F::kChunks, kWaveRows = 64 / F::kChunks;   // rows of a load of the block, of a wave
+    const int chunk = tid % F::kChunks, column = chunk * 8 < d ? chunk * 8 : 0;
+    const uint32_t k_lane = 2 * ((ONE ? lane / F::kChunks : 0) * a.k_tok + column);   // bytes
+    const uint32_t v_lane = 2 * ((ONE ? lane / F::kChunks : 0) * a.v_tok + column);
+    const auto load = [&](const elem* base, uint64_t rows, uint32_t lane_off, u32x4 (&x)[F::kLoads]) {
+#pragma unroll
+      for (int i = 0; i < F::kLoads; ++i) {
+        uint64_t at;
+        if constexpr (ONE) {                         // the rows of a wave's load follow the first, in its page
+          const int r = i * kRow + wave * kWaveRows;
+          at = uint32_t(__builtin_amdgcn_readlane(int(uint32_t(rows)), r)) |
+               uint64_t(uint32_t(__builtin_amdgcn_readlane(int(uint32_t(rows >> 32)), r))) << 32;
+        } else {
+          at = __shfl((unsigned long long)rows, i * kRow + tid / F::kChunks);
+        }
+        x[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(base + at) + lane_off);
+      }
+    };
+    const int row_in = tid / F::kChunks;             // (kRow is a multiple of eight: loads swap the same chunks)
+    const int k_place = row_in * F::kRowBytes + key_chunk(row_in, chunk) * 16;
+    const int v_place = row_in * F::kRowBytes + value_chunk<D>(row_in, chunk) * 16;
+    const auto store = [&](char* to, uint64_t have, u32x4 (&x)[F::kLoads]) {
+      if (have != kAll || d < D) {
+#pragma unroll
+        for (int i = 0; i < F::kLoads; ++i)
+          if (!(have >> (i * kRow + row_in) & 1) || chunk * 8 >= d) x[i] = u32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int i = 0; i < F::kLoads; ++i) *reinterpret_cast<u32x4*>(to + i * kRow * F::kRowBytes) = x[i];
+    };
+    // Whether the values of a step have to be watched: some row of the block does not see some of its positions, and
+    // a value is not finite.  The block meets.
+    const auto meet = [&](int step, const u32x4 (&x)[F::kLoads]) {
+      if (kAlone || step >= steps.end ||
+          (step * F::kKeys >= steps.all_lo && step * F::kKeys + F::kKeys - 1 <= steps.all_hi)) {
+        __syncthreads();
+        return false;
+      }
+      bool odd = false;
+#pragma unroll
+      for (int i = 0; i < F::kLoads; ++i) odd |= odd_value<T>(x[i]);
+      return __syncthreads_or(odd) != 0;
+    };
+
+    typename T::x8 q[D / 16];
+    load_query<T, D>(a, p, row, half, q);
+    f32x16 o[D / 32], s[1];
+    float m = -__builtin_inff(), l = 0;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[i][e] = 0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[0][e] = -__builtin_inff();
+    in_acc<D == 256>(o);
+    bool watch = false;
+    if (steps.begin < steps.end) {
+      u32x4 kr[F::kLoads], vr[F::kLoads];
+      const bool alike = a.k_page == a.v_page && a.k_tok == a.v_tok;
+      uint64_t k_rows, v_rows, v_next;               // of the keys to be loaded next, of the values, and after them
+      const auto find = [&] {
+        k_rows = rows_at(a.k_page, a.k_tok);
+        v_next = alike ? k_rows : rows_at(a.v_page, a.v_tok);
       };
-    };
-    int kb = 0;                                    // the buffer of the present step's keys
-    for (int step = steps.begin; step < steps.end && !watch; ++step) {
-      const char* const lv = lds_v + ((step - steps.begin) & 1) * F::kKv;
-      const int kb1 = kb + 1 == kKeyBuffers ? 0 : kb + 1, kb2 = kb1 + 1 == kKeyBuffers ? 0 : kb1 + 1;
-      have2 = there(step + 2);
+      // have: of the present step; have1, have2: of the two after
+      ask(steps.begin);
+      uint64_t have = there(steps.begin), have1, have2;
       find();
+      ask(steps.begin + 1);
       load(kc, k_rows, k_lane, kr);
-      load(vc, v_rows, v_lane, vr);
+      load(vc, v_next, v_lane, vr);
+      store(lds + k_place, have, kr);
+      store(lds_v + v_place, have, vr);
+      have1 = there(steps.begin + 1);
+      find();
+      ask(steps.begin + 2);
+      load(kc, k_rows, k_lane, kr);
       v_rows = v_next;
-      ask(step + 3);
-      if (step + 1 >= first && step <= last) {     // else nothing of this step or the next is seen by the wave
-        if constexpr (NS == 2)
-          advance<T, D>(lds + kb * F::kKv + 32 * F::kRowBytes, lv, at, q, a.scale2, s, m, l, o, mask_of(step, have, 1));
-        advance<T, D>(lds + kb1 * F::kKv, lv + (NS - 1) * 32 * F::kRowBytes, at, q, a.scale2, s, m, l, o,
-                      mask_of(step + 1, have1, 0));
+      store(lds + F::kKv + k_place, have1, kr);
+      watch = meet(steps.begin, vr);
+      if (!watch) {
+        scores<T, D>(lds, at, q, s);
+        hide(s, half, steps.begin * F::kKeys, have & 0xFFFFFFFFu, row);
+        rebase<D == 256>(s, a.scale2, m, l, o);
       }
-      store(lds + kb2 * F::kKv + k_place, have2, kr);
-      store(lds_v + ((step + 1 - steps.begin) & 1) * F::kKv + v_place, have1, vr);
-      watch = meet(step + 1, vr);
-      have = have1;
-      have1 = have2;
-      kb = kb1;
+      const auto mask_of = [&](int step, uint64_t all, int t) {
+        return [&, step, all, t](f32x16 (&x)[1]) {
+          hide(x, half, step * F::kKeys + t * 32, all >> (32 * t) & 0xFFFFFFFFu, row);
+        };
+      };
+      int kb = 0;                                    // the buffer of the present step's keys
+      for (int step = steps.begin; step < steps.end && !watch; ++step) {
+        const char* const lv = lds_v + ((step - steps.begin) & 1) * F::kKv;
+        const int kb1 = kb + 1 == kKeyBuffers ? 0 : kb + 1, kb2 = kb1 + 1 == kKeyBuffers ? 0 : kb1 + 1;
+        have2 = there(step + 2);
+        find();
+        load(kc, k_rows, k_lane, kr);
+        load(vc, v_rows, v_lane, vr);
+        v_rows = v_next;
+        ask(step + 3);
+        if (step + 1 >= first && step <= last) {     // else nothing of this step or the next is seen by the wave
+          if constexpr (NS == 2)
+            advance<T, D>(lds + kb * F::kKv + 32 * F::kRowBytes, lv, at, q, a.scale2, s, m, l, o, mask_of(step, have, 1));
+          advance<T, D>(lds + kb1 * F::kKv, lv + (NS - 1) * 32 * F::kRowBytes, at, q, a.scale2, s, m, l, o,
+                        mask_of(step + 1, have1, 0));
+        }
+        store(lds + kb2 * F::kKv + k_place, have2, kr);
+        store(lds_v + ((step + 1 - steps.begin) & 1) * F::kKv + v_place, have1, vr);
+        watch = meet(step + 1, vr);
+        have = have1;
+        have1 = have2;
+        kb = kb1;
+      }
     }
-  }
-  settle(o);
-  l += __shfl_xor(l, 32);
-  if (kAlone ? row.tok == alone.tok : !watch)
-    write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * F::kRows + wave * 32 + n, half, m, l, o);
-  return watch;
+    settle(o);
+    l += __shfl_xor(l, 32);
+    if (kAlone ? row.tok == alone.tok : !watch)
+      write_row<T, D>(a, p, row, (int64_t(index) * a.c.n_kv_heads + head) * F::kRows + wave * 32 + n, half, m, l, o);
+    return watch;
   };
   const bool odd = pass(std::false_type{});
   if (!odd) return;
