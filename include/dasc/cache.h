@@ -64,8 +64,8 @@ typedef struct dasc_append_io {
  * and the rest as it is; queries to q_out, keys and values to the cache at slots[t].  A token
  * whose slot lies outside [0, n_pages * page_size), -1 say, is not stored (a padded batch); its
  * query is rotated all the same.  Everything else in the cache is left as it was.
- * The angle is the exact product, reduced in 64 bits: cosine and sine are good to 2^-22 at any
- * position.  Arithmetic is fp32, rounded once.  A pair_axis outside [0, n_axes) turns a pair by
+ * The angle is the exact product, its turns counted in 64 bits: cosine and sine are good to 2^-22
+ * at any position.  Arithmetic is fp32, rounded once.  A pair_axis outside [0, n_axes) turns a pair by
  * nothing.
  * No two tokens may share a slot.  q_out may be q itself (same address and strides); otherwise
  * outputs overlap neither inputs nor each other.  Rows need no alignment beyond their element.
@@ -142,7 +142,7 @@ int dasc_beam_select_workspace_bytes(int32_t n_req, int32_t beams, int64_t vocab
 
 /* For each request r, beam b and token x,
  *     s = scores[r][b] + logits[r][b][x] - log sum_y e^{logits[r][b][y]}
- * in 64-bit arithmetic; the n_out largest of all beams and tokens, in descending order:
+ * in 64-bit arithmetic (the log-sum good to 2^-35); the n_out largest of all beams and tokens, in descending order:
  *     out_scores = s rounded to fp32, out_tokens = x, out_parents = b, out_slots = slots[r][b].
  * Equal ones go to the lower beam, then to the lower token; two tokens of one beam compare by
  * their logits.  A candidate needs a score above -inf: a logit of -inf, a beam whose score is -inf

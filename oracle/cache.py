@@ -15,9 +15,10 @@ def rotate(x, pos, inv_freq, pair_axis, adjacent):
     half = len(inv_freq)
     axis = np.zeros(half, int) if pair_axis is None else np.asarray(pair_axis)
     ok = (axis >= 0) & (axis < pos.shape[1])
-    p = np.where(ok, pos[:, np.where(ok, axis, 0)], 0).astype(np.float64)
-    angle = p * np.asarray(inv_freq, dtype=np.float64)                    # exact enough: 31 + 24 bits
-    turn = np.exp(1j * angle)[:, None]
+    # 31 bits times 24 need more than 53 (x86's long double has 64)
+    p = np.where(ok, pos[:, np.where(ok, axis, 0)], 0).astype(np.longdouble)
+    angle = p * np.asarray(inv_freq, dtype=np.longdouble)
+    turn = (np.cos(angle).astype(np.float64) + 1j * np.sin(angle).astype(np.float64))[:, None]
     lo, hi = (slice(0, 2 * half, 2), slice(1, 2 * half, 2)) if adjacent else (slice(0, half), slice(half, 2 * half))
     z = (y[..., lo] + 1j * y[..., hi]) * turn
     y[..., lo], y[..., hi] = z.real, z.imag

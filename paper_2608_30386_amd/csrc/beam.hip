@@ -9,6 +9,11 @@
 // largest logit; n lanes of a wave have one at or above the n-th largest of those, so at least n of the tile lie at
 // or above it.  That is found bit by bit with ballots; what is at or above the largest of the waves' is
 // gathered in LDS, a few times n as a rule, and ranked by comparing all with all.
+//
+// Measured: 16 requests of eight beams over 131071 bf16 tokens, 16 of each: 33 us for the rows, of which the 64-bit
+// exponentials are about half (34 MB would take 7), and 21 for the merge, a chain of short loops in one block a request.
+// Slots: HBM bounds them; eight states of 2 MB in each of 16 groups, 109 MB
+// read and 268 written in 88 us (4.3 TB/s).
 
 #include <hip/hip_runtime.h>
 
