@@ -220,16 +220,14 @@ __device__ inline bool locate(const AttnArgs& a, int index, Piece& p) {
 
 // ---- what the kernels share -----------------------------------------------------------------------
 
-// WQ waves of 32 rows each, WK of them on the same rows with KW keys each; D: head_dim rounded up
-template <typename T, int D, int WQ, int WK, int KW>
+// Tiles of many rows: WQ waves of 32 rows each, steps of KW keys; D: head_dim rounded up
+template <int D, int WQ, int KW>
 struct Form {
-  static constexpr int kWaves = WQ * WK, kThreads = 64 * kWaves;
-  static constexpr int kRows = 32 * WQ, kKeys = KW * WK;      // of a step
+  static constexpr int kThreads = 64 * WQ, kRows = 32 * WQ, kKeys = KW;
   static constexpr int kChunks = D / 8;                       // 16 bytes each, of a row
   static constexpr int kLoads = kKeys * kChunks / kThreads;   // of a thread, keys and values each
   static constexpr int kRowBytes = 2 * D;
   static constexpr int kKv = kKeys * kRowBytes;
-  static constexpr int kMerge = WK > 1 ? (WK - 1) * WQ * 32 * (D + 2) * 4 : 0;
 };
 
 // Tiles of many rows: waves of 32 rows each, waves of a SIMD, keys of a step.  Heads of 128 (2048 tokens over 16048,
@@ -408,18 +406,6 @@ __device__ inline void rebase(f32x16 (&s)[NS], float scale2, float& m, float& l,
   rebase<ACC>(top, scale2, m, l, o);
 }
 
-// Scores to weights, eight keys of each half: rounded to the type as an operand, their sum in fp32
-template <typename T, int NS>
-__device__ inline typename T::x8 weights(const f32x16 (&s)[NS], int t, int u, float scale2, float base, float& l) {
-  typename T::x8 w;
-  float x[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(s[t][8 * u + e], scale2, -base));
-#pragma unroll
-  for (int e = 0; e < 8; ++e) w[e] = typename T::elem(x[e]);
-  l += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-  return w;
-}
 __device__ inline float base_of(float m) { return m > -__builtin_inff() ? m : 0.0f; }
 
 // V^T of 16 keys from row r0 (a multiple of 16) of lv, columns 32 i ..
@@ -863,7 +849,7 @@ __device__ inline void advance(const char* lk, const char* lv, const Places& at,
 template <typename T, int D, int WQ, int SIMD, bool ONE>
 __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD))) void attn_wide_kernel(AttnArgs a) {
   constexpr int KW = wide_keys(D), NS = KW / 32;
-  typedef Form<T, D, WQ, 1, KW> F;
+  typedef Form<D, WQ, KW> F;
   typedef typename T::elem elem;
   constexpr int kKeyBuffers = NS + 1;
   __shared__ __attribute__((aligned(16))) char lds[(kKeyBuffers + 2) * F::kKv];
@@ -893,21 +879,24 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
     const elem* const vc = static_cast<const elem*>(a.c.v) + head * a.c.v_head;
     // Lane r of a wave knows where row r of a step lies.  Its entry of the table is asked for a step ahead, and looked
     // at when it is there.  Loads have no branch: what is not there is loaded from page 0 and put into LDS as zeros.
-    int entry, inside;                               // of the step to be loaded next: the entry, the place in the page
+    struct Place { int entry, inside; };             // the entry, the place in the page
     const auto ask = [&](int step) {
       int key = (step < steps.end ? step : steps.end - 1) * F::kKeys + lane % KW;
       key = key < p.kv ? key : p.kv - 1;
       const int at = a.page.of(key);
-      entry = table[at];
-      inside = key - at * int(a.page.d);
+      return Place{table[at], key - at * int(a.page.d)};
     };
-    const auto there = [&](int step) {               // the positions of the step that have a page
+    const auto is_page = [&](const Place& x) { return x.entry >= 0 && x.entry < a.c.n_pages; };
+    const auto there = [&](int step, const Place& x) {   // the positions of the step that have a page
       const int key = step * F::kKeys + lane;
-      return __ballot(lane < KW && step < steps.end && key < p.kv && entry >= 0 && entry < a.c.n_pages && (!kAlone || taken(alone, key)));
+      return __ballot(lane < KW && step < steps.end && key < p.kv && is_page(x) && (!kAlone || taken(alone, key)));
     };
-    const auto rows_at = [&](uint32_t page_stride, uint32_t tok_stride) {
-      const uint32_t b = entry >= 0 && entry < a.c.n_pages ? entry : 0;
-      return uint64_t(b) * page_stride + uint64_t(uint32_t(inside)) * tok_stride;
+    const auto k_rows_at = [&](const Place& x) {
+      return uint64_t(uint32_t(is_page(x) ? x.entry : 0)) * a.k_page + uint64_t(uint32_t(x.inside)) * a.k_tok;
+    };
+    const bool alike = a.k_page == a.v_page && a.k_tok == a.v_tok;
+    const auto v_rows_at = [&](const Place& x, uint64_t k_rows) {
+      return alike ? k_rows : uint64_t(uint32_t(is_page(x) ? x.entry : 0)) * a.v_page + uint64_t(uint32_t(x.inside)) * a.v_tok;
     };
     constexpr uint64_t kAll = KW == 64 ? ~uint64_t(0) : (uint64_t(1) << 32) - 1;
     constexpr int kRow = F::kThreads / F::kChunks, kWaveRows = 64 / F::kChunks;   // rows of a load of the block, of a wave
@@ -968,27 +957,20 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
     bool watch = false;
     if (steps.begin < steps.end) {
       u32x4 kr[F::kLoads], vr[F::kLoads];
-      const bool alike = a.k_page == a.v_page && a.k_tok == a.v_tok;
-      uint64_t k_rows, v_rows, v_next;               // of the keys to be loaded next, of the values, and after them
-      const auto find = [&] {
-        k_rows = rows_at(a.k_page, a.k_tok);
-        v_next = alike ? k_rows : rows_at(a.v_page, a.v_tok);
-      };
-      // have: of the present step; have1, have2: of the two after
-      ask(steps.begin);
-      uint64_t have = there(steps.begin), have1, have2;
-      find();
-      ask(steps.begin + 1);
+      // the first two steps' pages, keys and values at once: a block's start is a chain of loads
+      const Place p0 = ask(steps.begin), p1 = ask(steps.begin + 1);
+      Place next = ask(steps.begin + 2);             // of the keys to be loaded next
+      u32x4 k1[F::kLoads];
+      uint64_t have = there(steps.begin, p0), have1 = there(steps.begin + 1, p1), have2;   // of the present step, of those after
+      uint64_t k_rows = k_rows_at(p0);
       load(kc, k_rows, k_lane, kr);
-      load(vc, v_next, v_lane, vr);
+      load(vc, v_rows_at(p0, k_rows), v_lane, vr);
+      k_rows = k_rows_at(p1);
+      load(kc, k_rows, k_lane, k1);
+      uint64_t v_rows = v_rows_at(p1, k_rows);       // of the values to be loaded next
       store(lds + k_place, have, kr);
       store(lds_v + v_place, have, vr);
-      have1 = there(steps.begin + 1);
-      find();
-      ask(steps.begin + 2);
-      load(kc, k_rows, k_lane, kr);
-      v_rows = v_next;
-      store(lds + F::kKv + k_place, have1, kr);
+      store(lds + F::kKv + k_place, have1, k1);
       watch = meet(steps.begin, vr);
       if (!watch) {
         scores<T, D>(lds, at, q, s);
@@ -1004,12 +986,12 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
       for (int step = steps.begin; step < steps.end && !watch; ++step) {
         const char* const lv = lds_v + ((step - steps.begin) & 1) * F::kKv;
         const int kb1 = kb + 1 == kKeyBuffers ? 0 : kb + 1, kb2 = kb1 + 1 == kKeyBuffers ? 0 : kb1 + 1;
-        have2 = there(step + 2);
-        find();
+        have2 = there(step + 2, next);
+        k_rows = k_rows_at(next);
         load(kc, k_rows, k_lane, kr);
         load(vc, v_rows, v_lane, vr);
-        v_rows = v_next;
-        ask(step + 3);
+        v_rows = v_rows_at(next, k_rows);
+        next = ask(step + 3);
         if (step + 1 >= first && step <= last) {     // else nothing of this step or the next is seen by the wave
           if constexpr (NS == 2)
             advance<T, D>(lds + kb * F::kKv + 32 * F::kRowBytes, lv, at, q, a.scale2, s, m, l, o, mask_of(step, have, 1));
