@@ -87,7 +87,7 @@ typedef struct dasc_attn_io {
   void *o;                    /* [n_tokens, n_q_heads, head_dim], the cache's dtype          */
   float *lse;                 /* [n_tokens, n_q_heads], or NULL                              */
   const int32_t *block_table; /* [n_req, table_width]: the pages of each request in order    */
-  const int32_t *cu_seqlens;  /* [n_req + 1]                                                 */
+  const int32_t *cu_seqlens;  /* [n_req + 1], ascending                                      */
   const int32_t *kv_lens;     /* [n_req]: positions of each request, the new tokens included */
   int64_t q_tok, q_head, o_tok, o_head, lse_tok, lse_head, table_req;
   int64_t n_tokens;

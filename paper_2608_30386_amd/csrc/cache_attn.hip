@@ -97,6 +97,7 @@ struct AttnArgs {
   Divisor group, page, heads;
   uint32_t k_page, k_tok, v_page, v_tok;  // the cache's strides of pages and tokens
   int64_t block0;                         // first block of this launch: piece * n_kv_heads + head
+  int64_t pieces;                         // of a key head that there is room for
   int32_t target;                         // pieces of a key head to aim at
   int32_t split;                          // whether tiles may be split
   int32_t least;                          // steps that a piece has at least
@@ -457,12 +458,15 @@ __device__ inline void write_row(const AttnArgs& a, const Piece& p, const Row& r
   if (a.io.lse && g == 0) a.io.lse[t * a.io.lse_tok + row.qh * a.io.lse_head] = m * 0.69314718056f + logf(l);
 }
 
-// The block's piece; false if there is none.  The first block of a split tile says so to those that join.
+// The block's piece; false if there is none.  The first block of a split tile says so to those that join.  (Requests
+// whose rows overlap, which are not allowed, may have more pieces than there is room for: a tile that ends beyond is
+// left out.)
 template <int ROWS, int KEYS>
 __device__ inline bool take_piece(const AttnArgs& a, int head, int index, Piece& p) {
-  const bool any = locate<ROWS, KEYS>(a, index, p);
+  const bool any = locate<ROWS, KEYS>(a, index, p) && int64_t(index) - p.index + p.splits <= a.pieces;
   if (a.split && head == 0 && threadIdx.x == 0)
-    a.meta[index] = any && p.index == 0 && p.splits > 1 ? make_int4(p.req, p.row0, p.rows, p.splits) : make_int4(0, 0, 0, 0);
+    a.meta[index] =
+        any && p.index == 0 && p.splits > 1 ? make_int4(p.req, p.row0, p.rows, p.splits) : make_int4(0, 0, 0, 0);
   return any;
 }
 
@@ -1282,6 +1286,7 @@ extern "C" int dasc_cache_attn(const dasc_kv_cache* cache, const dasc_attn_io* i
   a.group = divisor(group);
   a.heads = divisor(cache->n_kv_heads);
   a.page = divisor(cache->page_size);
+  a.pieces = x.pieces;
   a.target = x.target;
   a.split = x.split;
   a.least = least_steps(x.form);

@@ -197,3 +197,28 @@ def test_a_beam_step():
     D.dasc_move_slots(pool, src[:, :B], slots)
     torch.cuda.synchronize()
     np.testing.assert_array_equal(pool.cpu().numpy().view(np.uint32), want.view(np.uint32))
+
+
+def test_more_rows_than_a_launch_takes():
+    import torch
+
+    announce("beam select: 40000 requests")
+    n, vocab = 40000, 20
+    x, s = rnd(n, 1, vocab, seed=12), -torch.rand(n, 1, device="cuda")
+    top, token, parent, _ = select(x, s, 3)
+    want, at = torch.sort(s.double()[..., None] + torch.log_softmax(x.double(), -1), dim=-1, descending=True, stable=True)
+    assert torch.equal(token, at[:, 0, :3].int()) and (parent == 0).all()
+    assert ((top - want[:, 0, :3]).abs() <= 2.0 ** -23 * want[:, 0, :3].abs()).all()
+
+
+def test_moves_of_many_groups():
+    import torch
+
+    announce("move slots: 3000 groups")
+    groups, m = 3000, 2
+    pool = torch.randn(groups * m, 4, device="cuda")
+    slots = np.random.default_rng(3).permutation(groups * m).reshape(groups, m)
+    want = OC.move_slots(pool.cpu().numpy(), slots[:, ::-1], slots)
+    D.dasc_move_slots(pool, dev_i32(slots[:, ::-1].copy()), dev_i32(slots))
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(pool.cpu().numpy(), want)

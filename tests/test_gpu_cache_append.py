@@ -184,3 +184,20 @@ def test_empty_other_stream_and_graph():
         torch.cuda.synchronize()
         np.testing.assert_array_equal(bits(got), bits(out))
         np.testing.assert_array_equal(bits(keys), bits(c["kc"]))
+
+
+def test_more_tokens_than_a_launch_takes():
+    import torch
+
+    announce("append: 2^20 + 5 tokens")
+    n, page = 2 ** 20 + 5, 1024
+    pages = n // page + 2
+    kc, vc = (torch.zeros(pages, page, 1, 8, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    k, v = (torch.randn(n, 1, 8, device="cuda").bfloat16() for _ in range(2))
+    slots = torch.randperm(pages * page, device="cuda")[:n]
+    D.dasc_cache_append(kc, vc, slots, k, v)
+    torch.cuda.synchronize()
+    assert torch.equal(kc.view(-1, 1, 8)[slots], k) and torch.equal(vc.view(-1, 1, 8)[slots], v)
+    left = torch.ones(pages * page, dtype=torch.bool, device="cuda")
+    left[slots] = False
+    assert not kc.view(-1, 8)[left].any() and not vc.view(-1, 8)[left].any()

@@ -295,3 +295,93 @@ def test_append_then_attend():
     c = dict(reqs=[(T, T)], kc=kc, vc=vc, table=table.cpu().numpy(), cu=np.array([0, T]), kv=np.array([T]),
              dt=torch.bfloat16, dtype="bfloat16", q=qr, page=page, N=T)
     check(c, out, None)
+
+
+@pytest.mark.parametrize("reqs", [[(1, 1 + 37 * i % 700) for i in range(150)], [(1 + i % 30, 40 + i) for i in range(100)],
+                                  [(90 + i % 3, 95 + i) for i in range(70)]], ids=["tokens", "drafts", "prompts"])
+def test_more_requests_than_a_wave_has_lanes(reqs):
+    announce(f"cache attn: {len(reqs)} requests")
+    c = make(reqs, hq=4, hkv=1, d=64, extra=2)
+    run(c)
+    run(c, window=11)
+
+
+@pytest.mark.parametrize("reqs", [[(1, 700), (1, 50)], [(6, 300)], [(100, 260)]], ids=["token", "drafts", "prompt"])
+@pytest.mark.parametrize("page", [5, 16])
+def test_keys_and_values_in_different_orders(reqs, page):
+    import torch
+
+    announce(f"cache attn: keys tokens first, values heads first, {reqs} pages of {page}")
+    c = make(reqs, hq=8, hkv=2, d=128, page=page)
+    c["vc"] = c["vc"].transpose(1, 2).contiguous().transpose(1, 2)
+    assert c["vc"].stride() != c["kc"].stride()
+    wide = torch.randn(c["kc"].shape[0], 3, *c["kc"].shape[1:], device="cuda").to(c["dt"])
+    wide[:, 1] = c["kc"]
+    c["kc"] = wide[:, 1]
+    run(c)
+
+
+@pytest.mark.parametrize("hq,hkv,d,n,kv", [(4, 1, 128, 4, 6000), (8, 1, 256, 5, 3000), (4, 1, 64, 20, 5000),
+                                           (4, 1, 128, 90, 4500), (2, 1, 256, 100, 3000)])
+def test_values_that_are_not_finite_in_split_tiles(hq, hkv, d, n, kv):
+    announce(f"cache attn: odd values over {kv} positions, {n} tokens, d={d}")
+    c = make([(n, kv), (n, n)], hq=hq, hkv=hkv, d=d, loud=3.0)
+    for i, p in ((0, kv - n // 2), (0, kv - 1), (0, 17), (1, n // 3)):
+        c["vc"][c["table"][i, p // 16], p % 16, 0, p % d] = float("nan") if p % 2 else float("inf")
+    run(c)
+    run(c, window=40)
+
+
+def test_more_blocks_than_a_launch_takes():
+    """A token of one position in each of 130 requests, 32768 heads: the output is the value, exactly."""
+    import torch
+
+    announce("cache attn: slices of a launch")
+    n, heads, d = 130, 32768, 8
+    g = torch.Generator("cuda").manual_seed(7)
+    kc, vc, q = (torch.randn(n, heads, d, device="cuda", generator=g).bfloat16() for _ in range(3))
+    o = torch.zeros_like(q)
+    D.dasc_cache_attn(kc[:, None], vc[:, None], dev_i32(np.arange(n)[::-1].copy()[:, None]), dev_i32(np.ones(n)), q, o,
+                      dev_i32(np.arange(n + 1)), 1)
+    torch.cuda.synchronize()
+    assert torch.equal(o, vc.flip(0))
+
+
+def test_two_calls_at_once():
+    import torch
+
+    announce("cache attn: two streams, a workspace each")
+    c = make([(1, 5000), (1, 40)], hq=8, hkv=2, d=128)
+    want, _ = call(c, lse=False)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    need = D.dasc_cache_attn_workspace_bytes(2, 2, 8, 2, 128, 1, 5000)
+    ws = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    o = [torch.empty_like(c["q"]) for _ in range(2)]
+    table, kv, cu = dev_i32(c["table"]), dev_i32(c["kv"]), dev_i32(c["cu"])
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for s, w, out in zip(streams, ws, o):
+            D.dasc_cache_attn(c["kc"], c["vc"], table, kv, c["q"], out, cu, 1, max_kv=5000, workspace=w, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(o[0], want) and torch.equal(o[1], want)
+
+
+def test_rows_that_do_not_ascend_stay_inside():
+    """A request whose rows run backwards is empty; rows that overlap leave the caller's other memory alone."""
+    import torch
+
+    announce("cache attn: cu_seqlens that do not ascend")
+    c = make([(5, 400), (4, 30)], hq=4, hkv=2, d=64)
+    keep = c["cu"]
+    c["cu"] = np.array([9, 0, 9])                # the first is empty, the second has all rows
+    c["kv"] = np.array([400, 30])
+    o, _ = call(c)
+    c["reqs"], c["cu"] = [(0, 400), (9, 30)], np.array([0, 0, 9])
+    want, _ = call(c)
+    assert torch.equal(o, want)
+    c = make([(5, 4000)] * 20, hq=4, hkv=2, d=64)
+    c["cu"] = np.array([0, 100] * 10 + [0])
+    need = D.dasc_cache_attn_workspace_bytes(20, 100, 4, 2, 64, 100, 4000)
+    ws = torch.full((need + 4096,), 77, dtype=torch.uint8, device="cuda")
+    call(c, workspace=ws[:need])
+    assert (ws[need:] == 77).all()
