@@ -11,7 +11,7 @@
 // gathered in LDS, a few times n as a rule, and ranked by comparing all with all.
 //
 // Measured: 16 requests of eight beams over 131071 bf16 tokens, 16 of each: 33 us for the rows, of which the 64-bit
-// exponentials are about half (34 MB would take 7), and 21 for the merge, a chain of short loops in one block a request.
+// exponentials are about half (34 MB would take 7), and 13.5 for the merge, a chain of short loops in one block a request.
 // Slots: HBM bounds them; eight states of 2 MB in each of 16 groups, 109 MB
 // read and 268 written in 88 us (4.3 TB/s).
 
@@ -32,7 +32,7 @@ constexpr int kTile = kThreads * 16;      // tokens of a block
 constexpr int kMaxBeams = 64, kMaxOut = 64;
 constexpr int64_t kMaxVocab = int64_t(1) << 24;
 constexpr int64_t kMaxRows = int64_t(1) << 24;
-constexpr int kPickWaves = 8, kPickKeys = 8;   // waves of a request's block, keys of a lane
+constexpr int kPickWaves = 8, kPickKeys = 10;   // waves of a request's block, keys of a lane
 
 struct BeamArgs {
   const void* logits;
@@ -296,20 +296,23 @@ __global__ __launch_bounds__(kPickWaves * 64) void beam_pick_kernel(BeamArgs a) 
   // all beams' best, ranked: by score, then the lower beam, then by logit and token
   const int total = a.beams * n;
   int valid = 0;
-  for (int i0 = 0; i0 < total; i0 += kPickWaves * 64) {
-    const int i = i0 + tid;
-    if (i >= total) continue;
-    const uint64_t s = score[i];
-    if (s == 0) continue;
-    const int b = i / n;
+  int parts = 1;                                   // threads that share a candidate's comparisons
+  while (parts < 16 && total * parts * 2 <= kPickWaves * 64) parts *= 2;
+  for (int i0 = 0; i0 < total; i0 += kPickWaves * 64 / parts) {
+    const int i = i0 + tid / parts, part = tid % parts;
+    const uint64_t s = i < total ? score[i] : 0;
     int rank = 0;
+    if (s != 0) {
 #pragma unroll 8
-    for (int j = 0; j < total; ++j) {
-      const uint64_t o = score[j];
-      if (o > s || (o == s && j < i)) ++rank;   // a beam's list is in order of logit and token
+      for (int j = part; j < total; j += parts) {
+        const uint64_t o = score[j];
+        if (o > s || (o == s && j < i)) ++rank;    // a beam's list is in order of logit and token
+      }
     }
-    if (rank < n) {
+    for (int m = 1; m < parts; m *= 2) rank += __shfl_xor(rank, m);
+    if (s != 0 && part == 0 && rank < n) {
       const int64_t out = int64_t(r) * n + rank;
+      const int b = i / n;
       a.out_scores[out] = float(unordered64(s));
       a.out_tokens[out] = int32_t(token_of(logit[i]));
       a.out_parents[out] = b;
