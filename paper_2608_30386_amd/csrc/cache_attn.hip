@@ -635,9 +635,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD)
   Alone alone = {-1, 0, 0};
   // Lane r (and r + 32) knows where row r of its group's keys lies; see the kernel for many rows
   int entry, inside;
+  const int stand_in = ONE ? (p.kv - 1) & -kWaveRows : p.kv - 1;   // for positions beyond the last, its page's too
   const auto ask = [&](int step) {
     int key = (step < steps.end ? step : steps.end - 1) * kKeys + wk * 32 + lane % 32;
-    key = key < p.kv ? key : p.kv - 1;
+    key = key < p.kv ? key : stand_in;
     const int at = a.page.of(key);
     entry = table[at];
     inside = key - at * int(a.page.d);
@@ -884,9 +885,12 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
     // Lane r of a wave knows where row r of a step lies.  Its entry of the table is asked for a step ahead, and looked
     // at when it is there.  Loads have no branch: what is not there is loaded from page 0 and put into LDS as zeros.
     struct Place { int entry, inside; };             // the entry, the place in the page
+    constexpr int kRow = F::kThreads / F::kChunks, kWaveRows = 64 / F::kChunks;   // rows of a load of the block, of a wave
+    // for positions beyond the last (with ONE, where the rows after it are of its page too)
+    const int stand_in = ONE ? (p.kv - 1) & -kWaveRows : p.kv - 1;
     const auto ask = [&](int step) {
       int key = (step < steps.end ? step : steps.end - 1) * F::kKeys + lane % KW;
-      key = key < p.kv ? key : p.kv - 1;
+      key = key < p.kv ? key : stand_in;
       const int at = a.page.of(key);
       return Place{table[at], key - at * int(a.page.d)};
     };
@@ -903,7 +907,6 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
       return alike ? k_rows : uint64_t(uint32_t(is_page(x) ? x.entry : 0)) * a.v_page + uint64_t(uint32_t(x.inside)) * a.v_tok;
     };
     constexpr uint64_t kAll = KW == 64 ? ~uint64_t(0) : (uint64_t(1) << 32) - 1;
-    constexpr int kRow = F::kThreads / F::kChunks, kWaveRows = 64 / F::kChunks;   // rows of a load of the block, of a wave
     const int chunk = tid % F::kChunks, column = chunk * 8 < d ? chunk * 8 : 0;
     const uint32_t k_lane = 2 * ((ONE ? lane / F::kChunks : 0) * a.k_tok + column);   // bytes
     const uint32_t v_lane = 2 * ((ONE ? lane / F::kChunks : 0) * a.v_tok + column);

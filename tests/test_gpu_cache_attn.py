@@ -385,3 +385,24 @@ def test_rows_that_do_not_ascend_stay_inside():
     ws = torch.full((need + 4096,), 77, dtype=torch.uint8, device="cuda")
     call(c, workspace=ws[:need])
     assert (ws[need:] == 77).all()
+
+
+@pytest.mark.parametrize("n", [1, 5, 20, 150])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_the_cache_ends_with_its_memory(d, n):
+    """The last position stands at the end of the last page, which ends an allocation of its own: steps go on
+    past it, and what they load in place of the missing positions has to lie inside the cache too."""
+    import torch
+
+    announce(f"end of memory d={d} n={n}")
+    torch.cuda.empty_cache()
+    page, hkv = 16, 2
+    pages = (16 << 20) // (page * hkv * d * 2)               # 16 MiB each of keys and values
+    kc, vc = (torch.randn(pages, page, hkv, d, device="cuda").to(torch.bfloat16) for _ in range(2))
+    need = -(-n // page) + 1
+    for kv in (need * page, need * page - 3):                # (the last one within the page as well)
+        kv = max(kv, n)
+        c = dict(reqs=[(n, kv)], kc=kc, vc=vc, table=np.arange(pages - need, pages)[None], cu=np.array([0, n]),
+                 kv=np.array([kv]), dt=torch.bfloat16, dtype="bfloat16", page=page, N=n,
+                 q=torch.randn(n, 4, d, device="cuda").to(torch.bfloat16))
+        run(c)
