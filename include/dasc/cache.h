@@ -65,7 +65,7 @@ typedef struct dasc_append_io {
  * whose slot lies outside [0, n_pages * page_size), -1 say, is not stored (a padded batch); its
  * query is rotated all the same.  Everything else in the cache is left as it was.
  * The angle is the exact product, its turns counted in 64 bits: cosine and sine are good to 2^-22
- * at any position.  Arithmetic is fp32, rounded once.  A pair_axis outside [0, n_axes) turns a pair by
+ * at any position, for |inv_freq| up to 2^20.  Arithmetic is fp32, rounded once.  A pair_axis outside [0, n_axes) turns a pair by
  * nothing.
  * No two tokens may share a slot.  q_out may be q itself (same address and strides); otherwise
  * outputs overlap neither inputs nor each other.  Rows need no alignment beyond their element.
