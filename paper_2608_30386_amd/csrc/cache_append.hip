@@ -25,13 +25,11 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxHalf = 128;            // pairs of a head
-constexpr int kMaxTokens = 8;            // of a block
 
 struct AppendArgs {
   dasc_kv_cache c;
   dasc_append_io io;
-  int64_t tok0;
-  int32_t tokens;                        // of a block
+  int64_t tok0;                          // first token of a launch
   int32_t parts;                         // blocks that share a token's heads
 };
 
@@ -63,37 +61,34 @@ __device__ inline void turn(double pos, double freq, float& c, float& s) {
 
 template <typename T, int VEC, bool ADJ>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
-  __shared__ float cosine[kMaxTokens * kMaxHalf], sine[kMaxTokens * kMaxHalf];
-  __shared__ int64_t place[kMaxTokens][2];                   // page and place in it; page -1: none
+  __shared__ float cosine[kMaxHalf], sine[kMaxHalf];
+  __shared__ int64_t place[2];                               // page and place in it; page -1: none
   const dasc_append_io& io = a.io;
   const int tid = threadIdx.x, half = io.rot / 2, d = a.c.head_dim;
-  const int64_t t0 = a.tok0 + int64_t(blockIdx.x) * a.tokens;
-  const int n = int(io.n_tokens - t0 < a.tokens ? io.n_tokens - t0 : a.tokens);
-  if (tid < n) {
-    const int64_t slot = io.slots[t0 + tid];
+  const int64_t tok = a.tok0 + blockIdx.x;
+  if (tid == 0) {
+    const int64_t slot = io.slots[tok];
     const bool in = slot >= 0 && slot / a.c.page_size < a.c.n_pages;
-    place[tid][0] = in ? slot / a.c.page_size : -1;
-    place[tid][1] = in ? slot % a.c.page_size : 0;
+    place[0] = in ? slot / a.c.page_size : -1;
+    place[1] = in ? slot % a.c.page_size : 0;
   }
-  for (int i = tid; i < n * half; i += kThreads) {
-    const int t = i / half, p = i % half;
+  for (int p = tid; p < half; p += kThreads) {
     const int axis = io.pair_axis ? io.pair_axis[p] : 0;
     float c = 1.0f, s = 0.0f;
     if (axis >= 0 && axis < io.n_axes)
-      turn(double(io.pos[(t0 + t) * io.pos_tok + axis * io.pos_axis]), double(io.inv_freq[p]), c, s);
-    cosine[i] = c;
-    sine[i] = s;
+      turn(double(io.pos[tok * io.pos_tok + axis * io.pos_axis]), double(io.inv_freq[p]), c, s);
+    cosine[p] = c;
+    sine[p] = s;
   }
   __syncthreads();
   // units of a head of q or k: those of pairs, then those of elements that stay; of v: elements
   const int turned = ADJ ? io.rot / (2 * VEC) : half / VEC;
   const int units = turned + (d - io.rot) / VEC, plain = d / VEC;
   const int hq = io.q ? io.n_q_heads : 0, hk = a.c.n_kv_heads;
-  const int per = (hq + hk) * units + hk * plain;            // of a token
-  for (int i = blockIdx.y * kThreads + tid; i < n * per; i += a.parts * kThreads) {
-    const int t = i / per;
-    int u = i - t * per;
-    const int64_t tok = t0 + t, page = place[t][0], off = place[t][1];
+  const int per = (hq + hk) * units + hk * plain;
+  const int64_t page = place[0], off = place[1];
+  for (int i = blockIdx.y * kThreads + tid; i < per; i += a.parts * kThreads) {
+    int u = i;
     const T* src;
     T* dst;
     bool v = false;
@@ -131,7 +126,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       const int lo = ADJ ? 2 * e : e, hi = ADJ ? 2 * e + 1 : e + VEC;
-      const float c = cosine[t * half + p + e], s = sine[t * half + p + e], g = f[lo], h = f[hi];
+      const float c = cosine[p + e], s = sine[p + e], g = f[lo], h = f[hi];
       f[lo] = fmaf(g, c, -(h * s));
       f[hi] = fmaf(g, s, h * c);
     }
@@ -148,12 +143,11 @@ template <typename T, int VEC, bool ADJ>
 void launch(AppendArgs a, hipStream_t st) {
   constexpr int64_t kBlocks = int64_t(1) << 20;
   const int heads = (a.io.q ? a.io.n_q_heads : 0) + 2 * a.c.n_kv_heads;
-  a.tokens = 1;
   const int work = heads * a.c.head_dim / VEC;
   a.parts = (work + 4 * kThreads - 1) / (4 * kThreads);
   if (a.parts > 32) a.parts = 32;
-  for (; a.tok0 < a.io.n_tokens; a.tok0 += kBlocks * a.tokens) {
-    const int64_t left = (a.io.n_tokens - a.tok0 + a.tokens - 1) / a.tokens;
+  for (; a.tok0 < a.io.n_tokens; a.tok0 += kBlocks) {
+    const int64_t left = a.io.n_tokens - a.tok0;
     append_kernel<T, VEC, ADJ><<<dim3(uint32_t(left < kBlocks ? left : kBlocks), a.parts), kThreads, 0, st>>>(a);
   }
 }
