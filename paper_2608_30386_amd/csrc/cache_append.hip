@@ -8,8 +8,8 @@
 // A block takes a token: its threads first form the cosines and sines of the token's pairs, once for all heads,
 // in LDS, then move the heads in units of eight elements (two of them for pairs that lie apart).
 //
-// HBM bounds it: 8192 tokens of 32 + 8 + 8 heads of 128, 201 MB in 31 us (6.5 TB/s); one block a token and 1024 units.
-// A few tokens take 4.6 us, three dependent loads and a launch.
+// HBM bounds it: 8192 tokens of 32 + 8 + 8 heads of 128, 201 MB in 30.6 us (6.6 TB/s); one block a token and 1024 units.
+// A few tokens take 4.3 us, three dependent loads and a launch.
 
 #include <hip/hip_runtime.h>
 
