@@ -850,13 +850,17 @@ __device__ inline void advance(const char* lk, const char* lv, const Places& at,
 
 // WQ waves of 32 rows each go over the keys together, 32 at a time, a product ahead (advance()).  Keys are in LDS
 // two steps ahead and values one, so the block meets once a step; the loads of both are issued at a step's
-// start and stored at its end.  ONE: a load's rows always lie in one page, whose address is then the same for a wave.
+// start and stored at its end.  No wave may still read what another stores before they meet: between two meetings
+// the present and the next step's keys are read (the present one's before the loop too, for the first scores) and those
+// of the step after them are stored, so keys have three buffers whatever a step's size; values, of which the
+// present step's are read and the next one's stored, have two.  ONE: a load's rows always lie in one page, whose address is
+// then the same for a wave.
 template <typename T, int D, int WQ, int SIMD, bool ONE>
 __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD))) void attn_wide_kernel(AttnArgs a) {
   constexpr int KW = wide_keys(D), NS = KW / 32;
   typedef Form<D, WQ, KW> F;
   typedef typename T::elem elem;
-  constexpr int kKeyBuffers = NS + 1;
+  constexpr int kKeyBuffers = 3;
   __shared__ __attribute__((aligned(16))) char lds[(kKeyBuffers + 2) * F::kKv];
   char* const lds_v = lds + kKeyBuffers * F::kKv;
   const int tid = threadIdx.x, lane = tid % 64, n = lane % 32, half = lane / 32;
