@@ -114,6 +114,9 @@ int dasc_cache_attn_workspace_bytes(int32_t n_req, int64_t n_tokens, int32_t n_q
  * A token that sees nothing (kv_lens[i] < len, say, or pages of -1) gets o = 0 and lse = -inf.
  * What is not seen is not read into a result, whatever it holds (infinities, NaN): the rest of a
  * page, pages of -1, later tokens.
+ * What is seen follows the formulas: a score of NaN makes lse and o NaN, one of +inf makes lse +inf
+ * and o NaN, one of -inf weighs nothing; an infinity or NaN in a value reaches the outputs of its
+ * column (an infinity as NaN where its weight is too small for the cache's dtype).
  * cu_seqlens is clamped to [0, n_tokens], kv_lens to [0, table_width * page_size]; rows of o and
  * lse of tokens that no request takes are not written.  max_len and max_kv choose launch shapes
  * and decide nothing else: a call whose requests are longer is right, but slow.

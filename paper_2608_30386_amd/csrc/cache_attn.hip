@@ -367,6 +367,11 @@ __device__ inline void hide(f32x16 (&s)[NS], int half, int key0, uint64_t have, 
   }
 }
 
+// A base is a finite number, so that none less another is NaN.  A row without a score yet has -kLargest, and weights
+// 2^-inf = 0; one with a score of +inf has kLargest, and the weight 2^inf = inf there: its sum and log-sum are +inf, its
+// output inf / inf = NaN.
+constexpr float kLargest = 0x1.fffffep127f;
+
 // The row's running base m of the weights 2^(s - m), sum l (of this half's keys) and output O, before scores
 // with maximum `top` (of this half's) join them.  The base follows the maximum only where that has left it by more
 // than 2^8 in some row: weights up to 2^8 lose nothing, and most steps leave O alone.
@@ -384,8 +389,8 @@ __device__ inline void rebase(float top, float scale2, float& m, float& l, V (&o
   constexpr int kE = sizeof(V) / 4;
   top = fmaxf(top, __shfl_xor(top, 32)) * scale2;
   if (__any(top > m + 8.0f)) {
-    const float next = fmaxf(m, top);
-    const float shrink = __builtin_amdgcn_exp2f(m - (next > -__builtin_inff() ? next : 0.0f));
+    const float next = fminf(fmaxf(m, top), kLargest);
+    const float shrink = __builtin_amdgcn_exp2f(m - next);
     m = next;
     l *= shrink;
     settle(o);
@@ -406,8 +411,6 @@ __device__ inline void rebase(f32x16 (&s)[NS], float scale2, float& m, float& l,
     for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
   rebase<ACC>(top, scale2, m, l, o);
 }
-
-__device__ inline float base_of(float m) { return m > -__builtin_inff() ? m : 0.0f; }
 
 // V^T of 16 keys from row r0 (a multiple of 16) of lv, columns 32 i ..
 template <typename T, int D>
@@ -529,7 +532,7 @@ struct Tile {
       if (row.real && c < a.c.head_dim) v = *reinterpret_cast<const u32x4*>(at + c);
       q[i] = __builtin_bit_cast(x8, v);
     }
-    m = -__builtin_inff();
+    m = -kLargest;
     l = 0;
 #pragma unroll
     for (int i = 0; i < kO; ++i)
@@ -582,7 +585,6 @@ struct Tile {
 #pragma unroll
       for (int e = 0; e < 4; ++e) top = fmaxf(top, s[t][e]);
     rebase<ACC>(fmaxf(top, __shfl_xor(top, 16)), scale2, m, l, o);
-    const float base = base_of(m);
     x8 v[kAhead], w;
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) v[j] = value_operand(lv, j);
@@ -591,7 +593,7 @@ struct Tile {
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(s[t][e], scale2, -base));
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[t][e], scale2, -m));
         w[t * 4 + e] = typename T::elem(x);
         sum[e % 2] += x;
       }
@@ -767,8 +769,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD)
         for (int w = 1; w < WK; ++w) {
           const float* const other = part(w);
           const float om = other[lane % R * 2], ol = other[lane % R * 2 + 1];
-          const float both = fmaxf(t.m, om), base = base_of(both);
-          const float f = __builtin_amdgcn_exp2f(t.m - base), g = __builtin_amdgcn_exp2f(om - base);
+          const float both = fmaxf(t.m, om);
+          const float f = __builtin_amdgcn_exp2f(t.m - both), g = __builtin_amdgcn_exp2f(om - both);
           t.m = both;
           t.l = t.l * f + ol * g;
 #pragma unroll
@@ -800,7 +802,7 @@ __device__ inline void advance(const char* lk, const char* lv, const Places& at,
   const auto read_v = [&](int j) { return value_operand<T, D>(lv, at, j / kDt * 16, j % kDt); };
   typename T::x8 k[4], v[4], w[2];
   f32x16 next[1];
-  const float base = base_of(m);
+  const float base = m;
   float part[2] = {0, 0};
 #pragma unroll
   for (int j = 0; j < 4; ++j) k[j] = read_k(j);
@@ -957,7 +959,7 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
     typename T::x8 q[D / 16];
     load_query<T, D>(a, p, row, half, q);
     f32x16 o[D / 32], s[1];
-    float m = -__builtin_inff(), l = 0;
+    float m = -kLargest, l = 0;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -1058,12 +1060,11 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
     for (int i = 64 + lane; i < t.w; i += 64) m = fmaxf(m, stats(i).x);
 #pragma unroll
     for (int s = 1; s < 64; s *= 2) m = fmaxf(m, __shfl_xor(m, s));
-    const float base = base_of(m);
     float l = 0;
     fv o = 0;
     for (int i0 = 0; i0 < t.w; i0 += 64) {
       if (i0 > 0) own = i0 + lane < t.w ? stats(i0 + lane) : make_float2(-__builtin_inff(), 0.0f);
-      const float f = __builtin_amdgcn_exp2f(own.x - base);
+      const float f = __builtin_amdgcn_exp2f(own.x - m);
       l += f * own.y;
       const int some = t.w - i0 < 64 ? t.w - i0 : 64;
       const auto piece = [&](int i) { return *reinterpret_cast<const fv*>(a.part + slot(i0 + i) * D + c); };

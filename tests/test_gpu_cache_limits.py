@@ -1,10 +1,12 @@
 """Attention over the paged cache where it can go wrong by its schedule or its number range (GPU).
 
-Tolerances are those of tests/test_gpu_cache_attn.py.
+Tolerances are those of tests/test_gpu_cache_attn.py; what is not finite has to be equal, infinities with their sign.
 """
 
+import numpy as np
 import pytest
 
+from oracle import cache as OC
 from tests.gpu_util import announce
 from tests.test_gpu_cache_attn import call, check, make
 
@@ -27,3 +29,76 @@ def test_waves_of_a_tile_that_leave_steps_out(d, page, dtype):
         for _ in range(10):
             o2, s2 = call(c, window=window)
             assert torch.equal(o, o2) and torch.equal(s, s2)
+
+
+def want(c, i, causal=True, window=0):
+    """The oracle's results of request i (o, lse, weighted mean and sum of |v|, largest scale sum |q k|) and its rows."""
+    import torch
+
+    n, kv, n_pages = c["reqs"][i][0], int(c["kv"][i]), c["kc"].shape[0]
+    rows = slice(int(c["cu"][i]), int(c["cu"][i]) + n)
+    p = np.arange(kv)
+    pages = c["table"][i, p // c["page"]]
+    have = (pages >= 0) & (pages < n_pages)
+    at = torch.tensor(np.where(have, pages, 0), device="cuda"), torch.tensor(p % c["page"], device="cuda")
+    k, v = (x[at].double().cpu().numpy() for x in (c["kc"], c["vc"]))
+    q = c["q"][rows].double().cpu().numpy()
+    return OC.attention(q, k, v, have, n, kv, causal, window, q.shape[2] ** -0.5), rows
+
+
+def strict(c, **how):
+    """check(), and equal values where the result is not finite."""
+    o, s = call(c, **how)
+    mask = {k: v for k, v in how.items() if k in ("causal", "window")}
+    check(c, o, s, **mask)
+    for i in range(len(c["reqs"])):
+        (wo, wl, *_), rows = want(c, i, **mask)
+        for got, exact in ((o[rows], wo), (s[rows], wl)):
+            got = got.double().cpu().numpy()
+            odd = ~np.isfinite(exact)
+            np.testing.assert_array_equal(got[odd], exact[odd])
+            assert np.isfinite(got[~odd]).all()
+
+
+@pytest.mark.parametrize("stale", [float("nan"), float("inf")])
+@pytest.mark.parametrize("page", [7, 16])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("d,hq,hkv", [(64, 4, 2), (128, 8, 1), (256, 4, 2)])
+def test_values_that_are_not_finite_reach_those_that_see_them(d, hq, hkv, dtype, page, stale):
+    announce(f"cache attn: values not finite, d={d} pages of {page} {dtype} {stale}")
+    for reqs in ([(1, 37), (1, 200), (1, 1)], [(6, 90), (4, 33)], [(12, 90), (20, 61)], [(70, 150), (129, 129)]):
+        c = make(reqs, dtype=dtype, hq=hq, hkv=hkv, d=d, page=page, stale=stale, seed=6)
+        strict(c)
+        c["table"][0, 1] = -1                   # a hole
+        if c["table"].shape[1] > 3:
+            c["table"][-1, 2] = c["kc"].shape[0]
+        for i, (n, kv) in enumerate(reqs):      # among the new tokens, of one sign and of both in a column
+            for back, column, value in ((n // 3, d // 2, stale), (n // 2, 3, -stale), (0, d // 2, -stale), (n - 1, 5, stale)):
+                p = kv - 1 - back
+                at = c["table"][i, p // page]
+                if 0 <= at < c["kc"].shape[0]:
+                    c["vc"][at, p % page, hkv - 1, column] = value
+        strict(c)
+        strict(c, window=7)
+        strict(c, causal=False)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("d,page", [(64, 16), (96, 7), (256, 16)])
+@pytest.mark.parametrize("reqs", [[(1, 40), (1, 6000)], [(5, 300)], [(20, 61), (11, 3000)], [(70, 150)], [(100, 4100)]],
+                         ids=lambda r: "-".join(f"{n}of{kv}" for n, kv in r))
+def test_scores_that_are_not_finite(reqs, d, page, dtype):
+    """A score of +inf: its row's log-sum is +inf and its output, inf / inf, NaN; of NaN: both NaN; of -inf: no weight."""
+    announce(f"cache attn: scores not finite {reqs} d={d} {dtype}")
+    for seed, value in enumerate((float("inf"), -float("inf"), float("nan"))):
+        c = make(reqs, dtype=dtype, hq=4, hkv=2, d=d, page=page, seed=20 + seed)
+        for i, (n, kv) in enumerate(reqs):
+            for p in (kv - 1 - n // 2, kv // 3):
+                c["kc"][c["table"][i, p // page], p % page, 0, 5] = value
+        c["q"][0, 1, :] = 0.0                   # 0 times an infinity is NaN
+        strict(c)
+        strict(c, window=9)
+    c = make(reqs, dtype=dtype, hq=4, hkv=2, d=d, page=page, seed=30)
+    c["q"][0, 0, 3] = float("inf")              # scores of both infinities
+    c["q"][-1, 3, 0] = float("nan")
+    strict(c)
