@@ -122,6 +122,8 @@ int dasc_cache_attn_workspace_bytes(int32_t n_req, int64_t n_tokens, int32_t n_q
  * and decide nothing else: a call whose requests are longer is right, but slow.
  * Precision: scores, running maxima and sums are fp32; the weights e^{s - m} are rounded to
  * the cache's dtype before they multiply the values, as the output is after; their sum takes them unrounded.
+ * (fp16: a weight below 2^-21 of its row's largest is off by up to 2^-32 of that.)
+ * Scores are meant to stay below 2^27, where fp32's numbers are 8 apart.
  *   q and o: 16-byte aligned, strides multiples of 8 elements; k and v too.  All strides >= 0.
  *   o must not overlap an input, nor its rows (token, head) each other; lse as o.  Requests may
  *   share pages.

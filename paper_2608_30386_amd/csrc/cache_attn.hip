@@ -54,6 +54,7 @@ struct Bf16 {
   __device__ static f32x4 mfma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   typedef __bf16 elem;
   static constexpr uint32_t kExp = 0x7F807F80u;      // exponents of two elements
+  static constexpr float kLift = 0.0f;               // see rebase()
   __device__ static f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 struct F16 {
@@ -61,6 +62,7 @@ struct F16 {
   __device__ static f32x4 mfma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
   typedef _Float16 elem;
   static constexpr uint32_t kExp = 0x7C007C00u;
+  static constexpr float kLift = 7.0f;
   __device__ static f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 
@@ -372,9 +374,6 @@ __device__ inline void hide(f32x16 (&s)[NS], int half, int key0, uint64_t have, 
 // output inf / inf = NaN.
 constexpr float kLargest = 0x1.fffffep127f;
 
-// The row's running base m of the weights 2^(s - m), sum l (of this half's keys) and output O, before scores
-// with maximum `top` (of this half's) join them.  The base follows the maximum only where that has left it by more
-// than 2^8 in some row: weights up to 2^8 lose nothing, and most steps leave O alone.
 // A wave that has a SIMD to itself has 256 accumulation registers beside its others, which products read and write
 // directly.  O stays there if it is put there wherever it was last touched by other arithmetic; else the compiler
 // moves all of it there and back in every step.
@@ -384,12 +383,21 @@ __device__ inline void in_acc(V (&x)[N]) {
   for (int i = 0; i < N; ++i)
     if constexpr (ACC) asm volatile("" : "+a"(x[i]));
 }
-template <bool ACC, typename V, int NO>
+// The row's running base m of the weights 2^(s - m), sum l (of this half's keys) and output O, before scores with
+// maximum `top` (of this half's, unscaled) join them.  The base follows the maximum only where that has left it by more
+// than 2^8 in some row: most steps leave O alone.  It stands kLift below the maximum then, so a weight is at most
+// 2^(kLift + 8): in fp16, whose numbers end at 2^16 and lose bits below 2^-14, the largest is 2^7 to 2^15, and what has
+// less than 2^-21 of it is off by up to 2^-32 of it.
+template <typename T, bool ACC, typename V, int NO>
 __device__ inline void rebase(float top, float scale2, float& m, float& l, V (&o)[NO]) {
   constexpr int kE = sizeof(V) / 4;
-  top = fmaxf(top, __shfl_xor(top, 32)) * scale2;
-  if (__any(top > m + 8.0f)) {
-    const float next = fminf(fmaxf(m, top), kLargest);
+  constexpr float kMost = T::kLift + 8.0f;
+  top = fmaxf(top, __shfl_xor(top, 32));
+  if (__any(fmaf(top, scale2, -m) > kMost)) {
+    float next = fmaxf(m, fmaf(top, scale2, -T::kLift));
+    // (scores from 2^26 on: a base rounded down may leave more than the largest weight above it)
+    if (fmaf(top, scale2, -next) > kMost) next += fabsf(next) * 0x1p-23f;
+    next = fminf(next, kLargest);
     const float shrink = __builtin_amdgcn_exp2f(m - next);
     m = next;
     l *= shrink;
@@ -401,7 +409,7 @@ __device__ inline void rebase(float top, float scale2, float& m, float& l, V (&o
     in_acc<ACC>(o);
   }
 }
-template <bool ACC, int NS, int NO>
+template <typename T, bool ACC, int NS, int NO>
 __device__ inline void rebase(f32x16 (&s)[NS], float scale2, float& m, float& l, f32x16 (&o)[NO]) {
   settle(s);
   float top = -__builtin_inff();
@@ -409,7 +417,7 @@ __device__ inline void rebase(f32x16 (&s)[NS], float scale2, float& m, float& l,
   for (int t = 0; t < NS; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
-  rebase<ACC>(top, scale2, m, l, o);
+  rebase<T, ACC>(top, scale2, m, l, o);
 }
 
 // V^T of 16 keys from row r0 (a multiple of 16) of lv, columns 32 i ..
@@ -584,7 +592,7 @@ struct Tile {
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) top = fmaxf(top, s[t][e]);
-    rebase<ACC>(fmaxf(top, __shfl_xor(top, 16)), scale2, m, l, o);
+    rebase<T, ACC>(fmaxf(top, __shfl_xor(top, 16)), scale2, m, l, o);
     x8 v[kAhead], w;
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) v[j] = value_operand(lv, j);
@@ -846,7 +854,7 @@ __device__ inline void advance(const char* lk, const char* lv, const Places& at,
     }
     hold();
   }
-  rebase<D == 256>(top, scale2, m, l, o);
+  rebase<T, D == 256>(top, scale2, m, l, o);
   s[0] = next[0];
 }
 
@@ -988,7 +996,7 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
       if (!watch) {
         scores<T, D>(lds, at, q, s);
         hide(s, half, steps.begin * F::kKeys, have & 0xFFFFFFFFu, row);
-        rebase<D == 256>(s, a.scale2, m, l, o);
+        rebase<T, D == 256>(s, a.scale2, m, l, o);
       }
       const auto mask_of = [&](int step, uint64_t all, int t) {
         return [&, step, all, t](f32x16 (&x)[1]) {

@@ -1,6 +1,10 @@
 """Attention over the paged cache where it can go wrong by its schedule or its number range (GPU).
 
 Tolerances are those of tests/test_gpu_cache_attn.py; what is not finite has to be equal, infinities with their sign.
+
+Weights in fp16: the operand is 2^(s - m + 7) with the base m at most 8 below the row's maximum, off by at most 2^-25
+where it is subnormal, so by 2^-32 of the largest weight: 2^-32 sum |v| in the output, and 2^-25 where that is
+subnormal itself.
 """
 
 import numpy as np
@@ -102,3 +106,54 @@ def test_scores_that_are_not_finite(reqs, d, page, dtype):
     c["q"][0, 0, 3] = float("inf")              # scores of both infinities
     c["q"][-1, 3, 0] = float("nan")
     strict(c)
+
+
+@pytest.mark.parametrize("sink", [0, 9001])
+@pytest.mark.parametrize("n,d", [(1, 64), (9, 128), (20, 64), (70, 128), (40, 256)])
+def test_many_small_weights_beside_a_large_one(n, d, sink):
+    """30011 positions, one with 2^25.4 times the others' weight and a value of 0: in fp16 the others are
+    subnormal beside it, and all of the output."""
+    import torch
+
+    announce(f"cache attn: small weights, {n} tokens d={d} sink at {sink}")
+    kv, page = 30011, 16
+    c = make([(n, kv)], dtype="float16", hq=2, hkv=1, d=d, page=page, seed=40)
+    c["kc"][:] = 0
+    c["q"][:] = 0
+    c["q"][..., 1] = 8.0
+    at = (c["table"][0, sink // page], sink % page, 0)
+    c["kc"][at + (1,)] = 25.4 * np.log(2) * d ** 0.5 / 8
+    c["vc"][:] = 0.5 + torch.rand(c["vc"].shape, device="cuda", generator=torch.Generator("cuda").manual_seed(41)).half()
+    c["vc"][at] = 0
+    for over in ({}, dict(max_kv=10)):          # cut into pieces, and whole
+        o, s = call(c, **over)
+        (wo, wl, size, total, big), _ = want(c, 0)
+        ds = 2.0 ** -24 * (d + 8) * big + 2.0 ** -22
+        tol = (2.0 ** -11 * (np.abs(wo) + size) + 2 * (ds[..., None] + kv * 2.0 ** -24) * size + 2.0 ** -32 * total
+               + 2.0 ** -25)
+        err = np.abs(o.double().cpu().numpy() - wo)
+        assert (err <= tol).all(), (over, (err / tol).max())
+        assert (np.abs(s.double().cpu().numpy() - wl) <= ds + kv * 2.0 ** -24 + 2.0 ** -22 * (np.abs(wl) + 1)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("n,d", [(1, 64), (9, 128), (70, 128), (40, 256)])
+def test_far_scores(n, d, dtype):
+    """Scores of 2^26 to 2^27, whose fp32 neighbours are 4 to 8 apart: their rounding decides which positions weigh
+    something, but weights stay numbers of the type and their mean stays among the values, up to a rounding of the
+    weights and one of the output."""
+    import torch
+
+    announce(f"cache attn: far scores, {n} tokens d={d} {dtype}")
+    c = make([(n, 900)], dtype=dtype, hq=2, hkv=1, d=d, seed=50)
+    g = torch.Generator("cuda").manual_seed(51)
+    for x in (c["q"], c["kc"]):
+        x.copy_((torch.rand(x.shape, device="cuda", generator=g) * 100 + 3e3).to(c["dt"]))
+    for sign in (1, -1):
+        c["q"].mul_(sign)
+        for over in ({}, dict(max_kv=10)):
+            o, s = call(c, **over)
+            assert torch.isfinite(s).all() and torch.isfinite(o).all()
+            assert float(o.float().abs().max()) <= float(c["vc"].float().abs().max()) * (1 + torch.finfo(c["dt"]).eps)
+            exact = c["q"].double() @ c["kc"].double().flatten(0, -2).T * d ** -0.5
+            assert ((s.double() - sign * exact.abs().mean()).abs() <= 0.02 * exact.abs().mean()).all()
