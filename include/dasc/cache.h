@@ -31,7 +31,8 @@ extern "C" {
 
 /* One layer's cache: position p of page b, head h, starts at b * _page + p * _tok + h * _head
  * elements, its head_dim elements are contiguous.  Any order of the three is possible: pages
- * with tokens or with heads first, pages of several layers side by side. */
+ * with tokens or with heads first, pages of several layers side by side.  Here and below
+ * any stride from 0 on will do for a dimension of one element. */
 typedef struct dasc_kv_cache {
   void *k, *v;              /* [n_pages, page_size, n_kv_heads, head_dim], dtype            */
   int64_t k_page, k_tok, k_head, v_page, v_tok, v_head;
@@ -73,7 +74,7 @@ typedef struct dasc_append_io {
  * Errors: DASC_E_INVAL (NULL cache, io, k, v, slots or cache arrays; q without q_out or the
  * reverse; rot without pos or inv_freq; a bad dtype or stride; a pointer not aligned to its
  * element; rows of q_out or of the cache that overlap), DASC_E_SHAPE (n_pages, page_size,
- * n_kv_heads, n_axes or, with q, n_q_heads < 1, head_dim < 1 or above 256 or no multiple of 8, rot odd,
+ * n_kv_heads, n_axes or, with q, n_q_heads < 1, head_dim < 8 or above 256 or no multiple of 8, rot odd,
  * negative or above head_dim, n_axes above 8, n_tokens < 0 or above 2^31 - 1, heads above 65536),
  * DASC_E_HIP. */
 int dasc_cache_append(const dasc_kv_cache *cache, const dasc_append_io *io, dasc_stream_t stream);

@@ -163,12 +163,21 @@ void launch_type(const AppendArgs& a, hipStream_t st) {
 }  // namespace
 }  // namespace dasc
 
-extern "C" int dasc_cache_append(const dasc_kv_cache* cache, const dasc_append_io* io, dasc_stream_t stream) {
+extern "C" int dasc_cache_append(const dasc_kv_cache* cache, const dasc_append_io* append, dasc_stream_t stream) {
   using namespace dasc;
-  const int rc = check_cache(cache, 2);
+  if (!cache || !append) return DASC_E_INVAL;
+  AppendArgs a = {};
+  a.c = *cache;
+  a.io = *append;
+  drop_unused(a.c);
+  drop_unused(a.io.n_tokens, {&a.io.q_tok, &a.io.qo_tok, &a.io.k_tok, &a.io.v_tok, &a.io.pos_tok});
+  drop_unused(a.io.n_q_heads, {&a.io.q_head, &a.io.qo_head});
+  drop_unused(a.c.n_kv_heads, {&a.io.k_head, &a.io.v_head});
+  drop_unused(a.io.n_axes, {&a.io.pos_axis});
+  const dasc_kv_cache& c = a.c;
+  const dasc_append_io* const io = &a.io;
+  const int rc = check_cache(&c, 2);
   if (rc != DASC_OK) return rc;
-  if (!io) return DASC_E_INVAL;
-  const dasc_kv_cache& c = *cache;
   if (io->rot < 0 || io->rot % 2 || io->rot > c.head_dim || io->n_axes < 1 || io->n_axes > 8 || io->n_tokens < 0 ||
       io->n_tokens > INT32_MAX || (io->q && (io->n_q_heads < 1 || io->n_q_heads > 65536)))
     return DASC_E_SHAPE;
@@ -190,10 +199,6 @@ extern "C" int dasc_cache_append(const dasc_kv_cache* cache, const dasc_append_i
     return DASC_E_INVAL;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  AppendArgs a;
-  a.c = c;
-  a.io = *io;
-  a.tok0 = 0;
   if (c.dtype == DASC_DTYPE_BF16) launch_type<bf16_t>(a, st);
   else launch_type<f16_t>(a, st);
   return launch_status();

@@ -1263,10 +1263,19 @@ extern "C" int dasc_cache_attn_workspace_bytes(int32_t n_req, int64_t n_tokens, 
   return DASC_OK;
 }
 
-extern "C" int dasc_cache_attn(const dasc_kv_cache* cache, const dasc_attn_io* io, void* workspace,
+extern "C" int dasc_cache_attn(const dasc_kv_cache* given, const dasc_attn_io* attn, void* workspace,
                                size_t workspace_bytes, dasc_stream_t stream) {
   using namespace dasc;
-  if (!io) return DASC_E_INVAL;
+  if (!given || !attn) return DASC_E_INVAL;
+  AttnArgs a;
+  a.c = *given;
+  a.io = *attn;
+  drop_unused(a.c);
+  drop_unused(a.io.n_tokens, {&a.io.q_tok, &a.io.o_tok, &a.io.lse_tok});
+  drop_unused(a.io.n_q_heads, {&a.io.q_head, &a.io.o_head, &a.io.lse_head});
+  drop_unused(a.io.n_req, {&a.io.table_req});
+  const dasc_kv_cache* const cache = &a.c;
+  const dasc_attn_io* const io = &a.io;
   int rc = check_cache(cache, 16);
   if (rc != DASC_OK) return rc;
   rc = check_sizes(io->n_req, io->n_tokens, io->n_q_heads, cache->n_kv_heads, cache->head_dim);
@@ -1290,9 +1299,6 @@ extern "C" int dasc_cache_attn(const dasc_kv_cache* cache, const dasc_attn_io* i
   const int most = io->table_width * cache->page_size;
   const Launch x = launch_of(io->n_req, io->n_tokens, group, cache->n_kv_heads, cache->head_dim, io->max_len,
                              io->max_kv < most ? io->max_kv : most, io->window);
-  AttnArgs a;
-  a.c = *cache;
-  a.io = *io;
   if (cache->k_page > UINT32_MAX || cache->v_page > UINT32_MAX || cache->k_tok >= kMostTok || cache->v_tok >= kMostTok)
     return DASC_E_UNSUPPORTED;
   a.k_page = uint32_t(cache->k_page);

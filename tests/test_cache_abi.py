@@ -214,3 +214,19 @@ def test_the_oracle_keeps_its_identities():
     flat = (z - np.log(np.exp(z).sum(1, keepdims=True)) + np.array([[0.0], [-1.0]])).ravel()
     np.testing.assert_allclose([g[0] for g in got], np.sort(flat)[::-1])
     assert [g[2] * 6 + g[1] for g in got] == np.argsort(-flat).tolist()
+
+
+def test_strides_of_dimensions_of_one_element_do_not_matter():
+    one = dict(n_pages=1, k_page=3, v_page=1 << 40)
+    flat = dict(page_size=1, k_tok=5, v_tok=1 << 30, k_page=128, v_page=128)
+    single = dict(n_kv_heads=1, k_head=3, v_head=9)
+    none = dict(n_tokens=0, q=None, k=None, v=None, slots=None)
+    for c in (one, flat, single):
+        assert append(cache(**c), q_out=None, **none) == E.DASC_OK, c
+        assert attn(cache(**c), n_tokens=0, q=None, o=None) == E.DASC_OK, c
+    # a call that lacks nothing but its workspace
+    big = dict(ws=None, n_tokens=1, max_len=1, max_kv=128 * 16, table_width=128)
+    for odd in (dict(q_tok=257, o_tok=3, lse_tok=0), dict(q_tok=0, o_tok=0)):
+        assert attn(**big, **odd) == E.DASC_E_WORKSPACE, odd
+    assert attn(cache(**single), n_q_heads=1, q_head=3, o_head=1, lse_head=0, **big) == E.DASC_E_WORKSPACE
+    assert attn(cache(**one), **big) == E.DASC_E_WORKSPACE

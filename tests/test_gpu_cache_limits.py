@@ -157,3 +157,25 @@ def test_far_scores(n, d, dtype):
             assert float(o.float().abs().max()) <= float(c["vc"].float().abs().max()) * (1 + torch.finfo(c["dt"]).eps)
             exact = c["q"].double() @ c["kc"].double().flatten(0, -2).T * d ** -0.5
             assert ((s.double() - sign * exact.abs().mean()).abs() <= 0.02 * exact.abs().mean()).all()
+
+
+def test_strides_of_dimensions_of_one_element():
+    """They are never used, so any will do: a token of a row that is no multiple of 8 elements wide, a cache of one page,
+    of pages of one token, of one head."""
+    import torch
+
+    announce("cache attn: strides of single elements")
+    c = make([(1, 9)], hq=4, hkv=2, d=64, page=16)
+    c["kc"], c["vc"] = (x[:1].as_strided((1, 16, 2, 64), (77777, 128, 64, 1)) for x in (c["kc"], c["vc"]))
+    c["table"][:] = 0
+    c["q"] = c["q"].as_strided((1, 4, 64), (259, 64, 1))
+    o, s = call(c, o=torch.zeros(300, dtype=c["dt"], device="cuda").as_strided((1, 4, 64), (13, 64, 1)))
+    check(c, o, s)
+    c = make([(3, 70)], hq=4, hkv=1, d=64, page=1)
+    c["kc"], c["vc"] = (x.as_strided(x.shape, (64, 3, 5, 1)) for x in (c["kc"], c["vc"]))
+    o, s = call(c)
+    check(c, o, s)
+    c = make([(5, 20)], hq=1, hkv=1, d=64)
+    c["q"] = c["q"].as_strided((5, 1, 64), (64, 1, 1))
+    o, s = call(c)
+    check(c, o, s)
