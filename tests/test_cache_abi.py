@@ -230,3 +230,16 @@ def test_strides_of_dimensions_of_one_element_do_not_matter():
         assert attn(**big, **odd) == E.DASC_E_WORKSPACE, odd
     assert attn(cache(**single), n_q_heads=1, q_head=3, o_head=1, lse_head=0, **big) == E.DASC_E_WORKSPACE
     assert attn(cache(**one), **big) == E.DASC_E_WORKSPACE
+
+
+def test_rows_that_end_where_the_next_ones_start():
+    """Three heads 80 elements apart, of 64: 224 elements a token, not 240.  The last row counts with its width alone."""
+    none = dict(n_tokens=0, q=None, k=None, v=None, slots=None)
+    close = dict(n_kv_heads=3, k_head=80, v_head=80, k_tok=224, v_tok=224, k_page=15 * 224 + 224, v_page=3584)
+    assert append(cache(**close), q_out=None, **none) == E.DASC_OK
+    for bad in (dict(k_tok=223), dict(v_page=3583), dict(v_head=63)):
+        assert append(cache(**{**close, **bad}), q_out=None, **none) == E.DASC_E_INVAL, bad
+    big = dict(ws=None, max_len=1, max_kv=128 * 16, table_width=128, n_q_heads=2)
+    for o_tok, o_head, want in ((144, 80, E.DASC_E_WORKSPACE), (136, 80, E.DASC_E_INVAL), (64, 192, E.DASC_E_WORKSPACE),
+                                (64, 184, E.DASC_E_INVAL), (72, 208, E.DASC_E_WORKSPACE)):
+        assert attn(o_tok=o_tok, o_head=o_head, lse=None, **big) == want, (o_tok, o_head)

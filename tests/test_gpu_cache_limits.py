@@ -179,3 +179,16 @@ def test_strides_of_dimensions_of_one_element():
     c["q"] = c["q"].as_strided((5, 1, 64), (64, 1, 1))
     o, s = call(c)
     check(c, o, s)
+
+
+@pytest.mark.parametrize("n", [3, 70])
+def test_rows_that_end_where_the_next_ones_start(n):
+    """Two heads 80 elements apart of 64, tokens 144: the 16 elements between the heads stay as they were."""
+    import torch
+
+    announce(f"cache attn: close rows, {n} tokens")
+    c = make([(n, n + 50)], hq=2, hkv=1, d=64)
+    flat = torch.full((n * 144,), 5.0, dtype=c["dt"], device="cuda")
+    o, s = call(c, o=flat.as_strided((n, 2, 64), (144, 80, 1)))
+    check(c, o, s)
+    assert (flat.as_strided((n, 16), (144, 1), 64) == 5.0).all()
