@@ -305,8 +305,8 @@ __device__ inline void load_query(const AttnArgs& a, const Piece& p, const Row& 
   }
 }
 
-// Key of element e of score tile t, from the wave's first
-__device__ inline int key_at(int t, int e, int half) { return t * 32 + 8 * (e / 4) + 4 * half + e % 4; }
+// Key of element e of the scores, from the wave's first
+__device__ inline int key_at(int e, int half) { return 8 * (e / 4) + 4 * half + e % 4; }
 
 // A lane's places in LDS.  Chunk 2 i + half of row n lies at key[i % 4] + (i / 4) * 128, and of the rows that step
 // 16 u of the keys takes the columns of tile i at value[i % 4] + (i / 4) * 256 (D = 64: value[i]), for rows
@@ -329,43 +329,35 @@ __device__ inline Places places_of(int lane) {
 // time each; so the order of reads, products and arithmetic in the inner loops is the one that is written.
 __device__ inline void hold() { __builtin_amdgcn_sched_barrier(0); }
 
-// S^T = K Q^T of NS tiles of 32 keys, four operands on their way
-template <typename T, int D, int NS>
-__device__ inline void scores(const char* lk, const Places& at, const typename T::x8 (&q)[D / 16], f32x16 (&s)[NS]) {
+// S^T = K Q^T of 32 keys, four operands on their way
+template <typename T, int D>
+__device__ inline void scores(const char* lk, const Places& at, const typename T::x8 (&q)[D / 16], f32x16& s) {
   constexpr int kSteps = D / 16, kAhead = 4;
-  const auto read = [&](int j) {
-    const int t = j / kSteps, i = j % kSteps;
-    return *reinterpret_cast<const typename T::x8*>(lk + at.key[i % 4] + t * 64 * D + i / 4 * 128);
+  const auto read = [&](int i) {
+    return *reinterpret_cast<const typename T::x8*>(lk + at.key[i % 4] + i / 4 * 128);
   };
   typename T::x8 k[kAhead];
 #pragma unroll
   for (int j = 0; j < kAhead; ++j) k[j] = read(j);
 #pragma unroll
-  for (int t = 0; t < NS; ++t)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) s[t][e] = 0;
+  for (int e = 0; e < 16; ++e) s[e] = 0;
   hold();
 #pragma unroll
-  for (int j = 0; j < NS * kSteps; ++j) {
-    s[j / kSteps] = T::mfma(k[j % kAhead], q[j % kSteps], s[j / kSteps]);
-    if (j + kAhead < NS * kSteps) k[j % kAhead] = read(j + kAhead);
+  for (int j = 0; j < kSteps; ++j) {
+    s = T::mfma(k[j % kAhead], q[j], s);
+    if (j + kAhead < kSteps) k[j % kAhead] = read(j + kAhead);
     hold();
   }
 }
 
-// Scores that are not seen become -inf.  have: the positions of the wave that have a page.
-template <int NS>
-__device__ inline void hide(f32x16 (&s)[NS], int half, int key0, uint64_t have, const Row& row) {
-  constexpr uint64_t kAll = NS == 2 ? ~uint64_t(0) : (uint64_t(1) << 32) - 1;
-  if (have == kAll && key0 >= row.all_lo && key0 + NS * 32 - 1 <= row.all_hi) return;
+// Scores that are not seen become -inf.  have: the 32 positions that have a page, a bit each.
+__device__ inline void hide(f32x16& s, int half, int key0, uint32_t have, const Row& row) {
+  if (have == 0xFFFFFFFFu && key0 >= row.all_lo && key0 + 31 <= row.all_hi) return;
   settle(s);
 #pragma unroll
-  for (int t = 0; t < NS; ++t) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int i = key_at(t, e, half);
-      s[t][e] = (have >> i & 1) && key0 + i >= row.lo && key0 + i <= row.hi ? s[t][e] : -__builtin_inff();
-    }
+  for (int e = 0; e < 16; ++e) {
+    const int i = key_at(e, half);
+    s[e] = (have >> i & 1) && key0 + i >= row.lo && key0 + i <= row.hi ? s[e] : -__builtin_inff();
   }
 }
 
@@ -409,14 +401,12 @@ __device__ inline void rebase(float top, float scale2, float& m, float& l, V (&o
     in_acc<ACC>(o);
   }
 }
-template <typename T, bool ACC, int NS, int NO>
-__device__ inline void rebase(f32x16 (&s)[NS], float scale2, float& m, float& l, f32x16 (&o)[NO]) {
+template <typename T, bool ACC, int NO>
+__device__ inline void rebase(f32x16& s, float scale2, float& m, float& l, f32x16 (&o)[NO]) {
   settle(s);
   float top = -__builtin_inff();
 #pragma unroll
-  for (int t = 0; t < NS; ++t)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
+  for (int e = 0; e < 16; ++e) top = fmaxf(top, s[e]);
   rebase<T, ACC>(top, scale2, m, l, o);
 }
 
@@ -491,8 +481,9 @@ __device__ inline Steps steps_of(const AttnArgs& a, const Piece& p) {
           last.lo, first.hi};
 }
 
-// The positions of `step` (its first at key0, `n` of them, a bit each) that the token taken alone sees; all if none is
-struct Alone { int tok, lo, hi; };                  // tok: -1: none
+// A token that is taken alone, and the positions that it sees.  tok: -1: none is
+struct Alone { int tok, lo, hi; };
+// Whether the pass sees position `key`
 __device__ inline bool taken(const Alone& x, int key) { return x.tok < 0 || (key >= x.lo && key <= x.hi); }
 // After a pass over a tile: whether another has to follow, over the next of its tokens alone
 __device__ inline bool next_alone(const AttnArgs& a, const Piece& p, bool odd, Alone& x) {
@@ -804,26 +795,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SIMD, SIMD)
 // is not seen of S(u + 1).
 template <typename T, int D, typename M>
 __device__ inline void advance(const char* lk, const char* lv, const Places& at, const typename T::x8 (&q)[D / 16],
-                               float scale2, f32x16 (&s)[1], float& m, float& l, f32x16 (&o)[D / 32], const M& mask) {
+                               float scale2, f32x16& s, float& m, float& l, f32x16 (&o)[D / 32], const M& mask) {
   constexpr int kSteps = D / 16, kDt = D / 32, kSlice = 16 / kSteps, kMax = 16 / (2 * kDt - 2) + 1;
   const auto read_k = [&](int j) { return *reinterpret_cast<const typename T::x8*>(lk + at.key[j % 4] + j / 4 * 128); };
   const auto read_v = [&](int j) { return value_operand<T, D>(lv, at, j / kDt * 16, j % kDt); };
   typename T::x8 k[4], v[4], w[2];
-  f32x16 next[1];
+  f32x16 next;
   const float base = m;
   float part[2] = {0, 0};
 #pragma unroll
   for (int j = 0; j < 4; ++j) k[j] = read_k(j);
 #pragma unroll
-  for (int e = 0; e < 16; ++e) next[0][e] = 0;
+  for (int e = 0; e < 16; ++e) next[e] = 0;
   hold();
 #pragma unroll
   for (int j = 0; j < kSteps; ++j) {
-    next[0] = T::mfma(k[j % 4], q[j], next[0]);
+    next = T::mfma(k[j % 4], q[j], next);
     if (j + 4 < kSteps) k[j % 4] = read_k(j + 4);
 #pragma unroll
     for (int e = j * kSlice; e < (j + 1) * kSlice; ++e) {
-      const float x = __builtin_amdgcn_exp2f(fmaf(s[0][e], scale2, -base));
+      const float x = __builtin_amdgcn_exp2f(fmaf(s[e], scale2, -base));
       w[e / 8][e % 8] = typename T::elem(x);
       part[e % 2] += x;
     }
@@ -847,15 +838,15 @@ __device__ inline void advance(const char* lk, const char* lv, const Places& at,
     o[j % kDt] = T::mfma(v[j % 4], w[j / kDt], o[j % kDt]);
     if (j + 4 < 2 * kDt) v[j % 4] = read_v(j + 4);
     // two products later the next scores are there, whichever way the branch before went
-    if (j == 1) asm volatile("" : "+v"(next[0]));
+    if (j == 1) asm volatile("" : "+v"(next));
     if (j >= 2) {
 #pragma unroll
-      for (int e = (j - 2) * kMax; e < (j - 1) * kMax && e < 16; ++e) top = fmaxf(top, next[0][e]);
+      for (int e = (j - 2) * kMax; e < (j - 1) * kMax && e < 16; ++e) top = fmaxf(top, next[e]);
     }
     hold();
   }
   rebase<T, D == 256>(top, scale2, m, l, o);
-  s[0] = next[0];
+  s = next;
 }
 
 // WQ waves of 32 rows each go over the keys together, 32 at a time, a product ahead (advance()).  Keys are in LDS
@@ -966,14 +957,14 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
 
     typename T::x8 q[D / 16];
     load_query<T, D>(a, p, row, half, q);
-    f32x16 o[D / 32], s[1];
+    f32x16 o[D / 32], s;
     float m = -kLargest, l = 0;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[i][e] = 0;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[0][e] = -__builtin_inff();
+    for (int e = 0; e < 16; ++e) s[e] = -__builtin_inff();
     in_acc<D == 256>(o);
     bool watch = false;
     if (steps.begin < steps.end) {
@@ -995,12 +986,12 @@ __global__ __launch_bounds__(64 * WQ) __attribute__((amdgpu_waves_per_eu(SIMD, S
       watch = meet(steps.begin, vr);
       if (!watch) {
         scores<T, D>(lds, at, q, s);
-        hide(s, half, steps.begin * F::kKeys, have & 0xFFFFFFFFu, row);
+        hide(s, half, steps.begin * F::kKeys, uint32_t(have), row);
         rebase<T, D == 256>(s, a.scale2, m, l, o);
       }
       const auto mask_of = [&](int step, uint64_t all, int t) {
-        return [&, step, all, t](f32x16 (&x)[1]) {
-          hide(x, half, step * F::kKeys + t * 32, all >> (32 * t) & 0xFFFFFFFFu, row);
+        return [&, step, all, t](f32x16& x) {
+          hide(x, half, step * F::kKeys + t * 32, uint32_t(all >> (32 * t)), row);
         };
       };
       int kb = 0;                                    // the buffer of the present step's keys
