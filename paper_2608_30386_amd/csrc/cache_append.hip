@@ -8,7 +8,8 @@
 // A block takes a token: its threads first form the cosines and sines of the token's pairs, once for all heads,
 // in LDS, then move the heads in units of eight elements (two of them for pairs that lie apart).
 //
-// HBM bounds it: 8192 tokens of 32 + 8 + 8 heads of 128, 201 MB in 30.6 us (6.6 TB/s); one block a token and 1024 units.
+// HBM bounds it: 8192 tokens of 32 + 8 + 8 heads of 128, 201 MB in 39.5 us (5.1 TB/s), where every call has other inputs;
+// 30.6 us on one set, part of which stays in the last-level cache.  One block for a token and 1024 units.
 // A few tokens take 4.3 us, three dependent loads and a launch.
 
 #include <hip/hip_runtime.h>

@@ -20,9 +20,11 @@
 //
 // Measured.  Few rows: HBM bounds it; 64 tokens over 1500 to 10000 positions, 32 heads of 128 on 8 of keys, 1.64 GB in
 // 300 us (5.4 TB/s, where a large copy runs at 4.8).  Many rows: 2048 tokens over 30011 positions, 16 heads of
-// 256, 717 TFLOP/s; over 16048, 32 heads of 128, 930, and of 64, 650 (a large matrix product 1330).  Matrix instructions
-// are busy 13 to 34% of the time, vector instructions 23 to 35%, LDS 15 to 28%: what is left are the waits of a
-// step, the exchange of a row's maximum across the wave, the barrier, the loads' addresses.
+// 256, 727 TFLOP/s; over 16048, 32 heads of 128, 917, and of 64, 654 (a large matrix product 1330).  Matrix instructions
+// are busy 13 to 38% of the time, LDS as long as they: a wave has 32 rows, so each of its products, 32 cycles of its SIMD,
+// reads 1 KB of K or V, and four SIMDs ask for the 128 bytes a cycle that LDS gives (conflicts, a fifth to a quarter of its
+// cycles, come on top).  Reads that are not hidden under products cost matrix time one for one; beside them
+// stand a step's waits, the exchange of a row's maximum across the wave, the barrier, the loads' addresses.
 
 #include <hip/hip_runtime.h>
 
@@ -234,10 +236,10 @@ struct Form {
 };
 
 // Tiles of many rows: waves of 32 rows each, waves of a SIMD, keys of a step.  Heads of 128 (2048 tokens over 16048,
-// us): eight waves and 64 keys 542, four waves twice on a CU with 32 keys 651, eight with 32 keys 705.  Heads of 64:
-// four waves twice on a CU 387, eight 405, three times four 380 with spills (a window of 1000 over 4097 tokens 45, 107
+// us): eight waves and 64 keys 550, four waves twice on a CU with 32 keys 651, eight with 32 keys 705.  Heads of 64:
+// four waves twice on a CU 386, eight 405, three times four 380 with spills (a window of 1000 over 4097 tokens 45, 107
 // and 56).  Heads of 256: a wave has 128 registers of O and 64 of Q, so it has a SIMD to itself (two: 2730 to 4380 us with
-// spills, one: 1450).
+// spills, one: 1433).
 constexpr int wide_wq(int D) { return D == 128 ? 8 : 4; }
 constexpr int wide_simd(int D) { return D == 256 ? 1 : 2; }
 constexpr int wide_keys(int D) { return D == 256 ? 32 : 64; }
@@ -245,7 +247,7 @@ constexpr int wide_keys(int D) { return D == 256 ? 32 : 64; }
 constexpr int few_simd(int form, int D) { return D == 256 && form < 2 ? 1 : 2; }
 
 // Where 16-byte chunk c of row r lies: lanes of a read that take the same chunk of many rows (keys), or a few
-// chunks of four rows (values), meet different banks
+// chunks of four rows (values), are spread over the banks (two cycles of conflicts a product are left, of its eight of LDS)
 __device__ inline int key_chunk(int r, int c) { return c ^ (r & 7); }
 template <int D>
 __device__ inline int value_chunk(int r, int c) {
