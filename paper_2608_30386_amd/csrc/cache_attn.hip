@@ -9,10 +9,10 @@
 // wave has keys 16 s + 4 h + {0..3} and 16 s + 8 + 4 h + {0..3} of step s.  V^T comes from LDS through the
 // transposing read.  The running maximum m and sum l are fp32 and in units of log2.
 //
-// The weights are rounded to the cache's type, as the matrix operand has to be; scores, maxima, sums and O are not, and the
-// sum takes the weights unrounded.  Each is off by at most half a step, independently, so an output's error is that of its own
-// rounding and about as much again: 0.0023 of its norm against 64 bits for bf16 where one rounding of the inputs' exact result
-// gives 0.0017, 0.00027 and 0.0002 for fp16.  A second operand for what the rounding left would double the products with V.
+// The weights are rounded to the cache's type, as the matrix operand has to be; scores, maxima, sums and O are not,
+// and the sum takes the weights unrounded.  Each is off by at most half a step, independently, so an output's error
+// is that of its own rounding and about as much again: 0.0023 of its norm for bf16 and 0.00027 for fp16, where weights of
+// 32 bits give 0.0017 and 0.0002.  A second operand for what the rounding left would double the products with V.
 //
 // Work.  A tile's keys may be split: the pieces of all requests are numbered in order, and every block finds
 // its own from the device's lengths, so that a piece has about the same number of keys whatever the requests'
